@@ -1,5 +1,5 @@
 """ctypes declarations of the C ABI in include/sangam_attn.h, sangam_sched.h,
-sangam_kv.h and sangam_probe.h.
+sangam_kv.h, sangam_kvq.h, sangam_rope.h and sangam_probe.h.
 
 Loads the in-tree ``libsangam_attn.so``; there is no fallback: if the
 library is missing or does not load, importing this module raises.
@@ -46,6 +46,11 @@ EXPORTS = (
     "sangam_kv_plan_rows",
     "sangam_kv_export",
     "sangam_kv_import",
+    "sangam_kvq_forward",
+    "sangam_kvq_export",
+    "sangam_kvq_import",
+    "sangam_rope_plan",
+    "sangam_rope_rotate",
     "sangam_probe_hbm_read",
     "sangam_probe_mfma_bf16",
 )
@@ -81,6 +86,46 @@ class KvDesc(ctypes.Structure):
         ("kv_len", ctypes.c_void_p),
         ("page_indptr", ctypes.c_void_p),
         ("page_ids", ctypes.c_void_p),
+    ]
+
+
+class KvqCache(ctypes.Structure):
+    _fields_ = [
+        ("format", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("pool_pages", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+    ]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("scaling", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("base", ctypes.c_double),
+        ("factor", ctypes.c_double),
+        ("original_len", ctypes.c_double),
+        ("beta_fast", ctypes.c_double),
+        ("beta_slow", ctypes.c_double),
+        ("magnitude", ctypes.c_double),
+    ]
+
+
+class RopeTensor(ctypes.Structure):
+    _fields_ = [
+        ("in_", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("in_row_stride", ctypes.c_int64),
+        ("in_head_stride", ctypes.c_int64),
+        ("out_row_stride", ctypes.c_int64),
+        ("out_head_stride", ctypes.c_int64),
+        ("heads", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
     ]
 
 
@@ -145,6 +190,18 @@ def _load():
     lib.sangam_kv_export.restype = ctypes.c_int32
     lib.sangam_kv_import.argtypes = [P, P, P, P, P, P, P]
     lib.sangam_kv_import.restype = ctypes.c_int32
+    cache = ctypes.POINTER(KvqCache)
+    lib.sangam_kvq_forward.argtypes = [P, P, P, P, P, cache, P, I64, P, P, P, S, P, P]
+    lib.sangam_kvq_forward.restype = ctypes.c_int32
+    lib.sangam_kvq_export.argtypes = [P, P, cache, P, P, P]
+    lib.sangam_kvq_export.restype = ctypes.c_int32
+    lib.sangam_kvq_import.argtypes = [P, P, P, P, cache, P]
+    lib.sangam_kvq_import.restype = ctypes.c_int32
+    tensor = ctypes.POINTER(RopeTensor)
+    lib.sangam_rope_plan.argtypes = [ctypes.POINTER(RopeDesc), P, S, ctypes.POINTER(S)]
+    lib.sangam_rope_plan.restype = ctypes.c_int32
+    lib.sangam_rope_rotate.argtypes = [P, P, tensor, tensor, ctypes.c_int32, ctypes.c_int32, P, I64, ctypes.c_int32, P]
+    lib.sangam_rope_rotate.restype = ctypes.c_int32
     lib.sangam_probe_hbm_read.argtypes = [P, S, P, ctypes.c_int32, P]
     lib.sangam_probe_hbm_read.restype = ctypes.c_int32
     lib.sangam_probe_mfma_bf16.argtypes = [P, ctypes.c_int32, ctypes.c_int32, P]

@@ -1,0 +1,147 @@
+// gfx950 kernels of the attention call over a quantised KV cache and their C
+// ABI entry point (include/sangam_kvq.h).
+//
+// The call, its plans and its tiles are those of attn_fwd.hip (attn_tile in
+// attn_tile.h); what differs is how a cached page gets into a tile. Codes
+// cannot go to LDS as they are: QK^T and PV take bf16 operands, and a code that
+// each wave converted for itself would be converted once per query head of the
+// group. A lane loads whole blocks (32 codes and their scale) of the next stage
+// into registers while the present stage is computed, converts them and writes
+// the bf16 values, which are exact, into the tile that all waves read. The
+// fresh rows of a block pass unquantised, and the tiles that write them back
+// quantise them from LDS.
+#include <hip/hip_runtime.h>
+
+#include "../../include/sangam_kvq.h"
+#include "attn_forward.h"
+#include "attn_tile.h"
+#include "mixed_order.h"
+#include "plan_format.h"
+
+using namespace sangam;
+
+namespace {
+
+template <typename Fmt, int D, int QW, int KW, int QB, int NB, int NSTAGE, bool HEADS_ACROSS>
+__global__ __launch_bounds__(64 * QW * KW, waves_per_simd(QB, false)) void attn_quant_kernel(QuantArgs a) {
+    __shared__ TileShared<2 * NSTAGE * 32 * NB * KW * D * 2> shared;
+    const TileRec t = a.tiles[blockIdx.x];
+    attn_tile<D, QW, KW, QB, NB, NSTAGE, HEADS_ACROSS, 0, QuantCache<Fmt>>(a, t, a.items[t.item], shared);
+}
+
+// Prefill-shaped tiles and MHA block decodes in one launch, as
+// attn_mixed_kernel; tiles of 256 rows are taken as two of 128.
+struct MixedQuantArgs {
+    QuantArgs a;  // tiles: the prefill-shaped ones
+    const TileRec* decode_tiles;
+    MixedOrder order;
+    int32_t wide;
+};
+
+template <typename Fmt, int D>
+__global__ __launch_bounds__(256, 2) void attn_quant_mixed_kernel(MixedQuantArgs m) {
+    __shared__ TileShared<2 * 2 * 64 * D * 2> shared;
+    const MixedBlock b = mixed_block(m.order, blockIdx.x);
+    if (b.index < 0) return;
+    if (b.decode) {
+        const TileRec t = m.decode_tiles[b.index];
+        attn_tile<D, 1, 2, 1, 1, 2, true, 2, QuantCache<Fmt>>(m.a, t, m.a.items[t.item], shared);
+        return;
+    }
+    TileRec t = m.a.tiles[b.index >> m.wide];
+    const ItemRec it = m.a.items[t.item];
+    if (m.wide) t.row0 += kPrefillRows * (b.index & 1);
+    if (t.row0 < it.n) attn_tile<D, 4, 1, 1, 2, 2, false, 0, QuantCache<Fmt>>(m.a, t, it, shared);
+}
+
+template <typename Fmt>
+struct QuantKernels {
+    typedef QuantArgs Args;
+    uint8_t *k_scale, *v_scale;
+
+    Args args(const AttnArgs& base) const {
+        Args a;
+        static_cast<AttnArgs&>(a) = base;
+        a.k_scale = k_scale;
+        a.v_scale = v_scale;
+        return a;
+    }
+
+    template <int D, int QW, int KW, int QB, int NB, bool HA, int NSTAGE = 2>
+    static hipError_t tiles(const Args& args, int n_tiles, hipStream_t stream, LaunchEvents ev) {
+        return launch(reinterpret_cast<const void*>(&attn_quant_kernel<Fmt, D, QW, KW, QB, NB, NSTAGE, HA>),
+                      dim3(unsigned(n_tiles)), unsigned(64 * QW * KW), args, stream, ev);
+    }
+
+    hipError_t mixed(const PlanHeader& h, const Args& args, const TileRec* decodes, const MixedOrder& order,
+                     unsigned blocks, hipStream_t stream, LaunchEvents ev) const {
+        const void* fn = h.d == 64 ? reinterpret_cast<const void*>(&attn_quant_mixed_kernel<Fmt, 64>)
+                                   : reinterpret_cast<const void*>(&attn_quant_mixed_kernel<Fmt, 128>);
+        return launch(fn, dim3(blocks), 256u, MixedQuantArgs{args, decodes, order, h.prefill_rows == kWidePrefillRows},
+                      stream, ev);
+    }
+
+    hipError_t prefill(const PlanHeader& h, const Args& args, hipStream_t stream, LaunchEvents ev, bool* supported) const {
+        *supported = true;
+        if (h.prefill_rows == kWidePrefillRows && h.d == 128)
+            return tiles<128, kWidePrefillQWaves, 1, 1, 4, false>(args, h.n_prefill_tiles, stream, ev);
+        if (h.prefill_rows == kPrefillRows)
+            return h.d == 128 ? tiles<128, kPrefillQWaves, 1, kPrefillQBlocks, 2, false>(args, h.n_prefill_tiles, stream, ev)
+                              : tiles<64, kPrefillQWaves, 1, kPrefillQBlocks, 2, false>(args, h.n_prefill_tiles, stream, ev);
+        *supported = false;
+        return hipSuccess;
+    }
+
+    template <int D>
+    static hipError_t decode_tiles(const PlanHeader& h, const Args& args, hipStream_t stream, LaunchEvents ev, bool* supported) {
+        *supported = true;
+        const int n = h.n_decode_tiles, kw = h.decode_kw, nb = h.decode_nb;
+        if (h.decode_qw == 1 && kw == 2 && nb == 1) return tiles<D, 1, 2, 1, 1, true>(args, n, stream, ev);
+        if (h.decode_qw == 2 && kw == 2 && nb == 2) return tiles<D, 2, 2, 1, 2, true>(args, n, stream, ev);
+        if (kw == 1 && nb == 2) {
+            switch (h.decode_qw) {
+                case 3: return tiles<D, 3, 1, 1, 2, true>(args, n, stream, ev);
+                case 4: return tiles<D, 4, 1, 1, 2, true>(args, n, stream, ev);
+                case 5: return tiles<D, 5, 1, 1, 2, true>(args, n, stream, ev);
+                case 6: return tiles<D, 6, 1, 1, 2, true>(args, n, stream, ev);
+                case 7: return tiles<D, 7, 1, 1, 2, true>(args, n, stream, ev);
+                case 8: return tiles<D, 8, 1, 1, 2, true>(args, n, stream, ev);
+                default: break;
+            }
+        }
+        *supported = false;
+        return hipSuccess;
+    }
+
+    hipError_t decode(const PlanHeader& h, const Args& args, hipStream_t stream, LaunchEvents ev, bool* supported) const {
+        return h.d == 128 ? decode_tiles<128>(h, args, stream, ev, supported) : decode_tiles<64>(h, args, stream, ev, supported);
+    }
+};
+
+template <typename Fmt>
+sangam_status run_quant(const sangam_kvq_cache& cache, const ForwardTensors& c) {
+    return run_forward(QuantKernels<Fmt>{static_cast<uint8_t*>(cache.k_scale), static_cast<uint8_t*>(cache.v_scale)}, c, own_workspace);
+}
+
+}  // namespace
+
+extern "C" sangam_status sangam_kvq_forward(const void* plan_host, const void* plan_dev, const void* q, const void* k_new,
+                                            const void* v_new, const sangam_kvq_cache* cache, const int32_t* page_ids_dev,
+                                            int64_t num_page_ids, void* out, float* lse, void* workspace,
+                                            size_t workspace_bytes, void* stream, void* const* events) {
+    clear_error();
+    if (!cache || !cache->k_scale || !cache->v_scale) {
+        set_error("the cache and its scales must not be NULL");
+        return SANGAM_ERR_INVALID_ARG;
+    }
+    if (!aligned16(cache->k_scale) || !aligned16(cache->v_scale)) {
+        set_error("the cache's scales must be 16-byte aligned");
+        return SANGAM_ERR_ALIGN;
+    }
+    const ForwardTensors c{plan_host, plan_dev, q, k_new, v_new, cache->k, cache->v, cache->pool_pages, page_ids_dev,
+                           num_page_ids, out, lse, workspace, workspace_bytes, stream, events};
+    if (cache->format == SANGAM_KV_E4M3) return run_quant<MxE4m3>(*cache, c);
+    if (cache->format == SANGAM_KV_E2M1) return run_quant<MxE2m1>(*cache, c);
+    set_error("cache format must be SANGAM_KV_E4M3 or SANGAM_KV_E2M1");
+    return SANGAM_ERR_UNSUPPORTED;
+}

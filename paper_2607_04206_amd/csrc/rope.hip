@@ -1,0 +1,244 @@
+// Rotary positions for gfx950 and their C ABI entry point
+// (include/sangam_rope.h).
+//
+// Every element is read once and written once, and a pair needs one sine and
+// one cosine, the same for all heads of a row: the kernel is bound by HBM as
+// long as those are computed once per row and not per head (computed by each
+// thread for its own 8 pairs they would take as long as the memory does). A
+// work-group holds some rows and some heads: it computes the rows' angles into
+// LDS (64-bit product, turns reduced to an eighth there, then fp32), and its
+// threads rotate units of 16 bytes on either side of a pair (halves) or of
+// 16 bytes of pairs (interleaved).
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <string>
+
+#include "../../include/sangam_rope.h"
+#include "rope_format.h"
+
+namespace sangam {
+void set_error(const std::string& msg);
+void clear_error();
+const RopePlanHeader* check_rope_plan(const void* plan);
+}  // namespace sangam
+
+using namespace sangam;
+
+namespace {
+
+struct RopeTensor {
+    const void* in;
+    void* out;
+    int64_t in_row, in_head, out_row, out_head;
+};
+
+struct RopeArgs {
+    RopeTensor t[2];  // q, k
+    const double* turns;
+    const int32_t* positions;
+    int64_t rows;
+    int32_t heads_q;
+    int32_t heads;      // of q and k
+    int32_t rot;
+    int32_t head_dim;
+    int32_t units;      // of a head: rotating ones, then ones to copy
+    int32_t rows_each;  // rows of a work-group
+    int32_t heads_each; // heads of a work-group
+    float size_cos;     // factors on cos and sin
+    float size_sin;
+};
+
+constexpr int kThreads = 256;
+
+// cos and sin of a number of turns given in 64 bits
+__device__ __forceinline__ float2 cos_sin(double turns) {
+    const double quarter = __builtin_rint(4.0 * turns);
+    const float r = float(__builtin_fma(-0.25, quarter, turns));  // |r| <= 1/8
+    float s, c;
+    sincospif(2.0f * r, &s, &c);
+    // quarters mod 4: 4 turns mod 4 is exact in 64 bits, and at most 2^33 here
+    const int q = int(int64_t(quarter)) & 3;
+    const float a = (q & 1) ? s : c, b = (q & 1) ? c : s;
+    return float2{(q == 1 || q == 2) ? -a : a, q >= 2 ? -b : b};
+}
+
+// T: element; V: elements of a vector access (1 where a stride, an address or
+// the number of pairs does not allow whole ones)
+template <typename T, int V, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    extern __shared__ float2 angles[];  // [rows_each][rot / 2]
+    const int half = a.rot / 2;
+    const int64_t row0 = int64_t(blockIdx.x) * a.rows_each;
+    const int nrows = int(a.rows - row0 < a.rows_each ? a.rows - row0 : a.rows_each);
+    const int head0 = int(blockIdx.y) * a.heads_each;
+    const int nheads = min(a.heads_each, a.heads - head0);
+    for (int k = threadIdx.x; k < nrows * half; k += kThreads) {
+        const int r = k / half;
+        const float2 cs = cos_sin(double(a.positions[row0 + r]) * a.turns[k - r * half]);
+        angles[k] = float2{cs.x * a.size_cos, cs.y * a.size_sin};
+    }
+    __syncthreads();
+    const int rotating = INTERLEAVED ? a.rot / (V > 1 ? V : 2) : half / V;
+    const int total = nrows * nheads * a.units;
+    for (int u = threadIdx.x; u < total; u += kThreads) {
+        const int rh = u / a.units, c = u - rh * a.units;
+        const int r = rh / nheads;
+        int h = head0 + rh - r * nheads;
+        const RopeTensor& t = a.t[h >= a.heads_q];
+        if (h >= a.heads_q) h -= a.heads_q;
+        const T* in = static_cast<const T*>(t.in) + (row0 + r) * t.in_row + h * t.in_head;
+        T* out = static_cast<T*>(t.out) + (row0 + r) * t.out_row + h * t.out_head;
+        if (c >= rotating) {  // past the rotating dims
+            const int d = a.rot + (c - rotating) * V;
+            *(Vec*)(out + d) = *(const Vec*)(in + d);
+            continue;
+        }
+        const float2* cs = angles + r * half;
+        if constexpr (INTERLEAVED && V > 1) {
+            const Vec x = *(const Vec*)(in + c * V);
+            Vec y;
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                const float2 w = cs[(c * V + e) / 2];
+                const float x0 = float(x[e]), x1 = float(x[e + 1]);
+                y[e] = T(x0 * w.x - x1 * w.y);
+                y[e + 1] = T(x1 * w.x + x0 * w.y);
+            }
+            *(Vec*)(out + c * V) = y;
+        } else {
+            const int lo = INTERLEAVED ? 2 * c : c * V, hi = INTERLEAVED ? lo + 1 : lo + half;
+            const Vec x = *(const Vec*)(in + lo), z = *(const Vec*)(in + hi);
+            Vec y, w;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float2 k = cs[c * V + e];
+                const float x0 = float(x[e]), x1 = float(z[e]);
+                y[e] = T(x0 * k.x - x1 * k.y);
+                w[e] = T(x1 * k.x + x0 * k.y);
+            }
+            *(Vec*)(out + lo) = y;
+            *(Vec*)(out + hi) = w;
+        }
+    }
+}
+
+template <typename T, int V>
+const void* kernel_of(bool vectors, bool interleaved) {
+    if (vectors)
+        return interleaved ? reinterpret_cast<const void*>(&rope_kernel<T, V, true>)
+                           : reinterpret_cast<const void*>(&rope_kernel<T, V, false>);
+    return interleaved ? reinterpret_cast<const void*>(&rope_kernel<T, 1, true>)
+                       : reinterpret_cast<const void*>(&rope_kernel<T, 1, false>);
+}
+
+sangam_status fail(sangam_status code, const std::string& msg) {
+    set_error(msg);
+    return code;
+}
+
+// Whether no two (row, head) of d elements overlap: the heads of a row side by
+// side and rows apart from them, or the other way round.
+bool apart(int64_t rows, int64_t row_stride, int64_t heads, int64_t head_stride, int64_t d) {
+    if (row_stride < 0 || head_stride < 0) return false;
+    const bool one_row = rows <= 1, one_head = heads <= 1;
+    auto nested = [d](int64_t n, int64_t inner, bool one_inner, int64_t outer, bool one_outer) {
+        if (!one_inner && inner < d) return false;
+        const int64_t span = one_inner ? d : (n - 1) * inner + d;
+        return one_outer || outer >= span;
+    };
+    return nested(heads, head_stride, one_head, row_stride, one_row) || nested(rows, row_stride, one_row, head_stride, one_head);
+}
+
+constexpr int64_t kMaxStride = int64_t(1) << 40;
+
+}  // namespace
+
+extern "C" sangam_status sangam_rope_rotate(const void* plan_host, const void* plan_dev, const sangam_rope_tensor* q,
+                                            const sangam_rope_tensor* k, int32_t head_dim, int32_t dtype,
+                                            const int32_t* positions_dev, int64_t rows, int32_t transpose, void* stream) {
+    clear_error();
+    const RopePlanHeader* h = check_rope_plan(plan_host);
+    if (!h) return fail(SANGAM_ERR_PLAN, "plan_host is not a rotary plan of this library version");
+    if (!q || rows < 0 || rows > INT32_MAX) return fail(SANGAM_ERR_INVALID_ARG, "q must not be NULL and rows must be 0 to 2^31 - 1");
+    if (dtype != SANGAM_DTYPE_BF16 && dtype != SANGAM_DTYPE_FP16 && dtype != SANGAM_DTYPE_FP32)
+        return fail(SANGAM_ERR_UNSUPPORTED, "dtype must be SANGAM_DTYPE_BF16, _FP16 or _FP32");
+    if (head_dim < h->rot_dim || head_dim > kRopeMaxDim)
+        return fail(SANGAM_ERR_INVALID_ARG, "head_dim must be the plan's rot_dim (" + std::to_string(h->rot_dim) + ") to 512");
+    if (transpose != 0 && transpose != 1) return fail(SANGAM_ERR_INVALID_ARG, "transpose must be 0 or 1");
+    const int64_t size = dtype == SANGAM_DTYPE_FP32 ? 4 : 2;
+    const int V = int(16 / size);
+    // vectors: whole ones on each side of the pairs, and every access aligned
+    bool vectors = h->rot_dim % (h->interleaved ? V : 2 * V) == 0 && head_dim % V == 0;
+    bool in_place = true;
+    RopeArgs args{};
+    int heads[2] = {0, 0};
+    for (int i = 0; i < 2; ++i) {
+        const sangam_rope_tensor* t = i ? k : q;
+        if (!t) continue;
+        if (t->heads < 1 || t->heads > (1 << 20)) return fail(SANGAM_ERR_INVALID_ARG, "heads must be 1 to 2^20");
+        heads[i] = t->heads;
+        if (rows == 0) continue;
+        if (!t->in || !t->out) return fail(SANGAM_ERR_INVALID_ARG, "the tensors must not be NULL");
+        if (reinterpret_cast<uintptr_t>(t->in) % size || reinterpret_cast<uintptr_t>(t->out) % size)
+            return fail(SANGAM_ERR_ALIGN, "the tensors must be aligned to their elements");
+        if (t->in_row_stride < 0 || t->in_head_stride < 0 || t->in_row_stride > kMaxStride || t->in_head_stride > kMaxStride ||
+            t->out_row_stride > kMaxStride || t->out_head_stride > kMaxStride)
+            return fail(SANGAM_ERR_INVALID_ARG, "strides must be 0 to 2^40");
+        if (!apart(rows, t->out_row_stride, t->heads, t->out_head_stride, head_dim))
+            return fail(SANGAM_ERR_INVALID_ARG, "rows and heads of the output overlap");
+        if (t->in == t->out && (t->in_row_stride != t->out_row_stride || t->in_head_stride != t->out_head_stride))
+            return fail(SANGAM_ERR_INVALID_ARG, "a tensor rotated in place must keep its strides");
+        for (int64_t stride : {t->in_row_stride, t->in_head_stride, t->out_row_stride, t->out_head_stride}) vectors = vectors && stride % V == 0;
+        vectors = vectors && reinterpret_cast<uintptr_t>(t->in) % 16 == 0 && reinterpret_cast<uintptr_t>(t->out) % 16 == 0;
+        in_place = in_place && t->in == t->out;
+        args.t[i] = RopeTensor{t->in, t->out, t->in_row_stride, t->in_head_stride, t->out_row_stride, t->out_head_stride};
+    }
+    if (rows == 0) return SANGAM_OK;
+    if (!plan_dev || !positions_dev) return fail(SANGAM_ERR_INVALID_ARG, "plan_dev and positions_dev must not be NULL");
+    if (reinterpret_cast<uintptr_t>(plan_dev) & 15u || reinterpret_cast<uintptr_t>(positions_dev) & 3u)
+        return fail(SANGAM_ERR_ALIGN, "plan_dev must be 16-byte and positions_dev 4-byte aligned");
+    const int v = vectors ? V : 1;
+    args.turns = reinterpret_cast<const double*>(static_cast<const uint8_t*>(plan_dev) + h->off_turns);
+    args.heads_q = heads[0];
+    args.heads = heads[0] + heads[1];
+    args.rot = h->rot_dim;
+    args.head_dim = head_dim;
+    const int rotating = h->interleaved ? h->rot_dim / std::max(v, 2) : h->rot_dim / 2 / v;
+    args.units = rotating + (in_place ? 0 : (head_dim - h->rot_dim) / v);
+    args.size_cos = h->magnitude;
+    args.size_sin = transpose ? -h->magnitude : h->magnitude;
+    // A work-group: up to four rows of all heads, fewer rows and then fewer
+    // heads while the launch has under two work-groups per CU and each thread
+    // more than one unit.
+    args.rows_each = 4;
+    args.heads_each = args.heads;
+    auto groups = [&] { return (rows + args.rows_each - 1) / args.rows_each * ((args.heads + args.heads_each - 1) / args.heads_each); };
+    while (groups() < 512 && args.rows_each > 1) args.rows_each /= 2;
+    while (groups() < 512 && int64_t(args.rows_each) * args.heads_each * args.units > kThreads && args.heads_each > 1)
+        args.heads_each = (args.heads_each + 1) / 2;
+    const void* fn = dtype == SANGAM_DTYPE_FP32   ? kernel_of<float, 4>(vectors, h->interleaved)
+                     : dtype == SANGAM_DTYPE_FP16 ? kernel_of<_Float16, 8>(vectors, h->interleaved)
+                                                  : kernel_of<__bf16, 8>(vectors, h->interleaved);
+    void* kargs[] = {&args};
+    const unsigned lds = unsigned(args.rows_each) * unsigned(h->rot_dim / 2) * unsigned(sizeof(float2));
+    const unsigned splits = unsigned((args.heads + args.heads_each - 1) / args.heads_each);
+    // a grid's threads are counted in 32 bits in each direction
+    const int64_t step = ((int64_t(1) << 32) / kThreads - 1) * args.rows_each;  // rows of a launch
+    const RopeTensor first[2] = {args.t[0], args.t[1]};
+    for (int64_t row = 0; row < rows; row += step) {
+        args.rows = std::min(step, rows - row);
+        args.positions = positions_dev + row;
+        for (int i = 0; i < 2; ++i) {
+            args.t[i].in = static_cast<const uint8_t*>(first[i].in) + row * first[i].in_row * size;
+            args.t[i].out = static_cast<uint8_t*>(first[i].out) + row * first[i].out_row * size;
+        }
+        const hipError_t e = hipLaunchKernel(fn, dim3(unsigned((args.rows + args.rows_each - 1) / args.rows_each), splits), dim3(kThreads),
+                                             kargs, lds, static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return fail(SANGAM_ERR_HIP, std::string("rotary launch: ") + hipGetErrorString(e));
+    }
+    return SANGAM_OK;
+}

@@ -1,0 +1,178 @@
+"""Python face of the quantised KV cache (include/sangam_kvq.h): the attention
+call of ``attn`` and the export and import of ``kv`` over pages of 8 or 4 bits a
+value, with the plans of those modules. Argument marshalling only: every step
+runs in the HIP kernels of libsangam_attn.so."""
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass
+from typing import Optional, Sequence, Tuple
+
+import torch
+
+from . import attn, kv
+from ._lib import KvqCache, check, lib
+
+# codes of a format: their C constant, dtype and dims per element
+FORMATS = {"e4m3": (1, torch.float8_e4m3fn, 1), "e2m1": (2, torch.uint8, 2)}
+BLOCK = 32  # consecutive dims of a row that share a scale
+
+
+@dataclass
+class QuantCache:
+    """A pool of quantised pages. k, v: codes, torch.float8_e4m3fn [pages, Hkv,
+    16, D] or, two e2m1 codes to a byte (the even dim in the low half),
+    torch.uint8 [pages, Hkv, 16, D / 2]. k_scale, v_scale: torch.uint8 [pages,
+    Hkv, 16, D / 32], the power of two b of a block standing for 2^(b - 127)
+    (torch.float8_e8m0fnu shows them as numbers). The caller owns the tensors."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    def __post_init__(self):
+        if not isinstance(self.k, torch.Tensor):
+            raise TypeError("k must be a torch.Tensor")
+        by_dtype = {dtype: (name, per) for name, (_, dtype, per) in FORMATS.items()}
+        if self.k.dtype not in by_dtype:
+            raise TypeError(f"k must hold e4m3 codes (torch.float8_e4m3fn) or pairs of e2m1 codes (torch.uint8), got {self.k.dtype}")
+        self.format, per = by_dtype[self.k.dtype]
+        if self.k.dim() != 4 or self.k.shape[2] != 16 or self.k.shape[3] * per not in (64, 128):
+            raise ValueError("k must be [num_pool_pages, Hkv, 16, D] with D 64 or 128 (e2m1: D / 2 bytes)")
+        self.num_pool_pages, self.num_kv_heads = int(self.k.shape[0]), int(self.k.shape[1])
+        self.head_dim = int(self.k.shape[3]) * per
+        dev = self.k.device
+        scales = tuple(self.k.shape[:3]) + (self.head_dim // BLOCK,)
+        for t, name, dtype, shape in ((self.k, "k", self.k.dtype, tuple(self.k.shape)), (self.v, "v", self.k.dtype, tuple(self.k.shape)),
+                                      (self.k_scale, "k_scale", torch.uint8, scales), (self.v_scale, "v_scale", torch.uint8, scales)):
+            attn._need(t, name, dtype, shape, dev)
+
+    def c_cache(self) -> KvqCache:
+        return KvqCache(FORMATS[self.format][0], 0, self.num_pool_pages, self.k.data_ptr(), self.v.data_ptr(),
+                        self.k_scale.data_ptr(), self.v_scale.data_ptr())
+
+
+def empty_cache(num_pool_pages: int, num_kv_heads: int, head_dim: int, *, format: str = "e4m3", device=None) -> QuantCache:
+    """A pool of that many pages, all zero."""
+    if format not in FORMATS:
+        raise ValueError(f"format must be one of {sorted(FORMATS)}, got {format!r}")
+    if head_dim not in (64, 128):
+        raise ValueError(f"head_dim must be 64 or 128, got {head_dim}")
+    _, dtype, per = FORMATS[format]
+    rows = (num_pool_pages, num_kv_heads, 16)
+    codes = [torch.zeros(rows + (head_dim // per,), dtype=torch.uint8, device=device).view(dtype) for _ in range(2)]
+    scales = [torch.zeros(rows + (head_dim // BLOCK,), dtype=torch.uint8, device=device) for _ in range(2)]
+    return QuantCache(*codes, *scales)
+
+
+def _stream(dev: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.cuda.Stream:
+    if dev.type != "cuda":
+        raise ValueError("the quantised cache needs device tensors (a ROCm GPU)")
+    if stream is None:
+        return torch.cuda.current_stream(dev)
+    if stream.device != dev:
+        raise ValueError(f"stream belongs to {stream.device}, the tensors are on {dev}")
+    return stream
+
+
+def _new(shape, dtype, dev, stream: torch.cuda.Stream) -> torch.Tensor:
+    """A tensor that `stream` writes (its memory is not reused before that)."""
+    t = torch.empty(shape, dtype=dtype, device=dev)
+    if stream != torch.cuda.current_stream(dev):
+        t.record_stream(stream)
+    return t
+
+
+def forward(p: attn.Plan, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cache: QuantCache,
+            page_ids: torch.Tensor, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+            workspace: Optional[torch.Tensor] = None, want_lse: bool = True,
+            stream: Optional[torch.cuda.Stream] = None,
+            launch_events: Optional[Sequence[torch.cuda.Event]] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """sangam_kvq_forward on the current (or given) stream: attn.forward over a
+    quantised cache, with a plan of attn.plan. The fresh rows are attended to as
+    they are and written into the pages quantised."""
+    dev = q.device
+    s = _stream(dev, stream)
+    T, Hq, Hkv, D = p.total_q, p.num_q_heads, p.num_kv_heads, p.head_dim
+    attn._need(q, "q", torch.bfloat16, (T, Hq, D), dev)
+    attn._need(k_new, "k_new", torch.bfloat16, (T, Hkv, D), dev)
+    attn._need(v_new, "v_new", torch.bfloat16, (T, Hkv, D), dev)
+    _check_cache(cache, Hkv, D, p.num_pool_pages, dev)
+    attn._need(page_ids, "page_ids", torch.int32, None, dev)
+    if page_ids.dim() != 1 or page_ids.numel() < p.total_pages:
+        raise ValueError(f"page_ids must be a 1-D tensor of at least {p.total_pages} entries "
+                         "(the plan's page table, on the device)")
+    if out is not None:
+        attn._need(out, "out", torch.bfloat16, (T, Hq, D), dev)
+    if lse is not None:
+        attn._need(lse, "lse", torch.float32, (T, Hq), dev)
+    if workspace is not None and (not workspace.is_contiguous() or workspace.device != dev):
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    if launch_events is not None and len(launch_events) != 6:
+        raise ValueError("launch_events needs 6 events (start and stop of 3 launches)")
+    with torch.cuda.device(dev):
+        if p.dev is None or p.dev.device != dev:
+            p.to(dev)
+        if out is None:
+            out = _new((T, Hq, D), torch.bfloat16, dev, s)
+        if lse is None and want_lse:
+            lse = _new((T, Hq), torch.float32, dev, s)
+        if workspace is None and p.workspace_bytes > 0:
+            workspace = _new((p.workspace_bytes,), torch.uint8, dev, s)
+        p.order_after_upload(s)
+        evs = None if launch_events is None else (ctypes.c_void_p * 6)(*[e.cuda_event for e in launch_events])
+        check(lib.sangam_kvq_forward(p.host_ptr(), p.dev.data_ptr(), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+                                     ctypes.byref(cache.c_cache()), page_ids.data_ptr(), int(page_ids.numel()), out.data_ptr(),
+                                     lse.data_ptr() if lse is not None else None,
+                                     workspace.data_ptr() if workspace is not None else None,
+                                     workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                     s.cuda_stream, evs))
+    return out, lse
+
+
+def _check_cache(cache: QuantCache, hkv: int, d: int, pages: int, dev) -> None:
+    if not isinstance(cache, QuantCache):
+        raise TypeError("cache must be a QuantCache")
+    if cache.k.device != dev:
+        raise ValueError(f"the cache must be on {dev}, got {cache.k.device}")
+    if (cache.num_kv_heads, cache.head_dim) != (hkv, d):
+        raise ValueError(f"the plan is for {hkv} KV heads of {d} dims, the cache holds {cache.num_kv_heads} of {cache.head_dim}")
+    if cache.num_pool_pages < pages:
+        raise ValueError(f"the plan addresses {pages} pool pages, the cache holds {cache.num_pool_pages}")
+
+
+def _copy(fn, p: kv.KvPlan, cache: QuantCache, stream, args) -> None:
+    dev = cache.k.device
+    with torch.cuda.device(dev):
+        if p.dev is None or p.dev.device != dev:
+            p.to(dev)
+        check(fn(p.host_ptr(), p.dev.data_ptr(), *args, stream.cuda_stream))
+
+
+def kv_export(p: kv.KvPlan, cache: QuantCache, k_packed: Optional[torch.Tensor] = None,
+              v_packed: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """sangam_kvq_export on the current (or given) stream: the values of the
+    listed requests' rows, bf16, with a plan of kv.plan. Allocates the packed
+    buffers with torch when they are not passed."""
+    dev = cache.k.device
+    s = _stream(dev, stream)
+    _check_cache(cache, p.num_kv_heads, p.head_dim, p.num_pool_pages, dev)
+    shape = (p.rows, p.num_kv_heads, p.head_dim)
+    k_packed, v_packed = (_new(shape, torch.bfloat16, dev, s) if t is None else t for t in (k_packed, v_packed))
+    kv._check_packed(p, k_packed, "k_packed", dev)
+    kv._check_packed(p, v_packed, "v_packed", dev)
+    _copy(lib.sangam_kvq_export, p, cache, s, (ctypes.byref(cache.c_cache()), k_packed.data_ptr(), v_packed.data_ptr()))
+    return k_packed, v_packed
+
+
+def kv_import(p: kv.KvPlan, k_packed: torch.Tensor, v_packed: torch.Tensor, cache: QuantCache,
+              stream: Optional[torch.cuda.Stream] = None) -> None:
+    """sangam_kvq_import on the current (or given) stream: quantises the rows
+    into the listed pages' slots [0, L_i) of the cache."""
+    dev = cache.k.device
+    s = _stream(dev, stream)
+    _check_cache(cache, p.num_kv_heads, p.head_dim, p.num_pool_pages, dev)
+    kv._check_packed(p, k_packed, "k_packed", dev)
+    kv._check_packed(p, v_packed, "v_packed", dev)
+    _copy(lib.sangam_kvq_import, p, cache, s, (k_packed.data_ptr(), v_packed.data_ptr(), ctypes.byref(cache.c_cache())))

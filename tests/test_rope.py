@@ -1,0 +1,304 @@
+"""Rotary positions (include/sangam_rope.h, paper_2607_04206_amd/rope.py).
+
+CPU: the rates of every scaling against the formulas, refusals of the C entries
+and of the Python calls.
+GPU: against the rotation in float64, at every type, layout and kind of stride.
+
+Bar of an element y of a pair (x0, x1), y = m (x0 c - x1 s): the rounding to
+its type, at most eps / 2 of |y| (half the smallest subnormal at least), and
+m (|x0| + |x1|) times the errors in fp32: sine and cosine to 2 ulp (2^-23
+below 1), the reduced angle's rounding (2^-28 turns, 2^-25 rad), the factor m
+(2^-24) and the products and sum (2 * 2^-24), together below 2^-21.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_04206_amd import _lib, rope
+
+TYPES = {torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25, torch.float32: 2.0 ** -150}  # half the smallest subnormal
+
+
+def rates(rot, base=10000.0, scaling="none", factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0, magnitude=None, **_):
+    """f_j and m from the formulas, in float64."""
+    j = np.arange(rot // 2)
+    f = base ** (-2.0 * j / rot)
+    m = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "ntk":
+        f = (base * factor ** (rot / (rot - 2.0))) ** (-2.0 * j / rot)
+    elif scaling == "yarn":
+        turns = original_len * f / (2 * math.pi)
+        g = np.clip((turns - beta_slow) / (beta_fast - beta_slow), 0, 1)
+        f = g * f + (1 - g) * f / factor
+        m = 0.1 * math.log(factor) + 1
+    return f, m if magnitude is None else magnitude
+
+
+def rotated(x, positions, rot, interleaved, transpose=False, **scale):
+    """x [rows, heads, D] (float64) rotated, and the bar's fp32 part."""
+    f, m = rates(rot, **scale)
+    angle = np.asarray(positions, np.float64)[:, None, None] * f
+    c, s = np.cos(angle) * m, np.sin(angle) * m * (-1 if transpose else 1)
+    y, bar = x.copy(), np.zeros_like(x)
+    lo, hi = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    y[..., lo] = x[..., lo] * c - x[..., hi] * s
+    y[..., hi] = x[..., hi] * c + x[..., lo] * s
+    bar[..., lo] = bar[..., hi] = 2.0 ** -21 * m * (np.abs(x[..., lo]) + np.abs(x[..., hi]))
+    return y, bar
+
+
+# ------------------------------------------------------------------ plan (CPU)
+SCALES = [dict(), dict(scaling="linear", factor=4.0), dict(scaling="ntk", factor=8.0, base=500000.0),
+          dict(scaling="yarn", factor=16.0, original_len=4096.0), dict(scaling="yarn", factor=2.0, original_len=100.0, beta_fast=8.0, beta_slow=0.5),
+          dict(magnitude=1.25), dict(scaling="yarn", factor=4.0, original_len=8192.0, magnitude=1.0)]
+
+
+@pytest.mark.parametrize("rot", [4, 6, 64, 128, 512])
+@pytest.mark.parametrize("scale", SCALES)
+def test_rates(rot, scale):
+    p = rope.plan(rot_dim=rot, **scale)
+    f, m = rates(rot, **scale)
+    turns = p.host[256:].view(np.float64)
+    assert turns.shape == (rot // 2,)
+    assert np.allclose(turns, f / (2 * math.pi), rtol=1e-14, atol=0)  # some operations of 2^-53 each, pow() among them
+    assert p.host[24:28].view(np.float32)[0] == np.float32(m)
+
+
+@pytest.mark.parametrize("bad", [dict(rot_dim=0), dict(rot_dim=7), dict(rot_dim=514), dict(rot_dim=-2), dict(base=1.0), dict(base=float("nan")),
+                                 dict(base=float("inf")), dict(scaling="linear", factor=0.5), dict(scaling="linear", factor=float("nan")),
+                                 dict(scaling="ntk", factor=2.0, rot_dim=2), dict(scaling="yarn", factor=2.0),
+                                 dict(scaling="yarn", factor=2.0, original_len=64.0, beta_fast=1.0, beta_slow=1.0),
+                                 dict(scaling="yarn", factor=2.0, original_len=64.0, beta_slow=-1.0), dict(magnitude=float("inf"))])
+def test_plan_refuses(bad):
+    with pytest.raises(_lib.SangamError) as e:
+        rope.plan(**{**dict(rot_dim=64), **bad})
+    assert e.value.status == -1 and str(e.value)
+
+
+def test_plan_refuses_in_python_and_by_size():
+    for bad in (dict(scaling="cubic"), dict(magnitude=0.0), dict(magnitude=-1.0)):
+        with pytest.raises(ValueError):
+            rope.plan(rot_dim=64, **bad)
+    d = _lib.RopeDesc(64, 0, 0, 0, 10000.0)
+    used = ctypes.c_size_t(0)
+    f = _lib.lib.sangam_rope_plan
+    assert f(ctypes.byref(d), None, 0, ctypes.byref(used)) == -5 and used.value == 256 + 32 * 8
+    assert f(None, None, 0, ctypes.byref(used)) == -1 and f(ctypes.byref(d), None, 0, None) == -1
+    d.scaling = 9
+    assert f(ctypes.byref(d), None, 0, ctypes.byref(used)) == -1
+    d.scaling, d.interleaved = 0, 2
+    assert f(ctypes.byref(d), None, 0, ctypes.byref(used)) == -1
+
+
+def _tensor(**over):
+    t = dict(in_=4096, out=4096, in_row_stride=256, in_head_stride=64, out_row_stride=256, out_head_stride=64, heads=4, reserved=0)
+    t.update(over)
+    return _lib.RopeTensor(*[t[n] for n, _ in _lib.RopeTensor._fields_])
+
+
+@pytest.mark.parametrize("over,call,status", [
+    (dict(), dict(plan=None), -8), (dict(), dict(q=None), -1), (dict(), dict(dtype=3), -2), (dict(), dict(head_dim=32), -1),
+    (dict(), dict(head_dim=1024), -1), (dict(), dict(rows=-1), -1), (dict(), dict(rows=1 << 31), -1), (dict(), dict(transpose=2), -1),
+    (dict(), dict(positions=None), -1), (dict(), dict(plan_dev=None), -1), (dict(), dict(plan_dev=4104), -6), (dict(), dict(positions=4098), -6),
+    (dict(in_=None), {}, -1), (dict(out=None), {}, -1), (dict(in_=4097, out=1 << 20), {}, -6), (dict(heads=0), {}, -1),
+    (dict(in_row_stride=-256, out=1 << 20), {}, -1), (dict(out_row_stride=-256, in_row_stride=-256), {}, -1),
+    (dict(out=1 << 20, out_head_stride=63), {}, -1), (dict(out=1 << 20, out_row_stride=255), {}, -1), (dict(out=1 << 20, out_row_stride=0), {}, -1),
+    (dict(out_row_stride=512), {}, -1)])  # in place with other strides
+def test_rotate_refuses(over, call, status):
+    # fake device addresses: every check fails before any HIP call
+    p = rope.plan(rot_dim=64)
+    a = dict(plan=p.host_ptr(), plan_dev=4096, q=ctypes.byref(_tensor(**over)), head_dim=64, dtype=0, positions=4096, rows=10, transpose=0)
+    a.update(call)
+    got = _lib.lib.sangam_rope_rotate(a["plan"], a["plan_dev"], a["q"], None, a["head_dim"], a["dtype"], a["positions"], a["rows"], a["transpose"], None)
+    assert got == status and _lib.lib.sangam_last_error()
+
+
+def test_no_rows_is_no_launch():
+    p = rope.plan(rot_dim=64)
+    q = _tensor(in_=None, out=None)
+    assert _lib.lib.sangam_rope_rotate(p.host_ptr(), None, ctypes.byref(q), ctypes.byref(q), 64, 0, None, 0, 0, None) == 0
+
+
+def test_overlaps_are_seen():
+    x = torch.zeros(10, 6, 8)
+    assert not rope._overlap(x[:, :2], x[:, 2:4]) and not rope._overlap(x[:, 2:4], x[:, :2]) and not rope._overlap(x[:5], x[5:])
+    assert rope._overlap(x[:, :2], x[:, 1:3]) and rope._overlap(x, x) and rope._overlap(x[:5], x[4:])
+    assert rope._overlap(x[:, 4:6], x[1:, 4:6]) and not rope._overlap(x[:, 4:6], x[1:, :2])
+    assert rope._overlap(x, x.transpose(0, 1)) and not rope._overlap(x, torch.zeros(10, 6, 8))
+
+
+# ------------------------------------------------------------------------ GPU
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    return torch.device("cuda:0")
+
+
+def check(got, x, positions, rot, interleaved, **kw):
+    want, bar = rotated(x.double().cpu().numpy(), positions.cpu().numpy(), rot, interleaved, **kw)
+    bar += np.maximum(torch.finfo(x.dtype).eps / 2 * (np.abs(want) + bar), TYPES[x.dtype])
+    bar[..., rot:] = 0.0  # passes unchanged
+    d = np.abs(got.double().cpu().numpy() - want)
+    bad = np.flatnonzero((d > bar).reshape(-1))
+    if len(bad):
+        at = np.unravel_index(bad[0], d.shape)
+        pytest.fail(f"{len(bad)} of {d.size} off, the first at {at}: {got[at].item()}, not {want[at]} to {bar[at]:.2e}", pytrace=False)
+
+
+def inputs(rows, hq, hkv, d, dtype, dev, seed=0, far=10000):
+    g = torch.Generator(device=dev).manual_seed(seed + rows)
+    draw = lambda h: torch.randn(rows, h, d, generator=g, device=dev).to(dtype)  # noqa: E731
+    return draw(hq), draw(hkv), torch.randint(0, far, (rows,), generator=g, device=dev, dtype=torch.int32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rows,hq,hkv,d,rot", [(1, 32, 32, 128, 128), (5, 1, 1, 64, 64), (33, 28, 4, 128, 64), (130, 8, 2, 64, 16), (7, 3, 1, 256, 192),
+                                               (6, 5, 2, 100, 34), (3, 2, 2, 64, 2), (2, 4, 1, 512, 512), (3000, 4, 4, 64, 48), (9, 3, 2, 80, 80), (11, 3, 2, 37, 24)])
+def test_shapes(dev, dtype, interleaved, rows, hq, hkv, d, rot):
+    print(f"[case] rope {dtype} {interleaved} {rows} rows {hq}/{hkv} of {d}, {rot} rotate", flush=True)
+    q, k, pos = inputs(rows, hq, hkv, d, dtype, dev)
+    keep = q.clone(), k.clone()
+    p = rope.plan(rot_dim=rot, interleaved=interleaved, device=dev)
+    for transpose in (False, True):
+        for got, x in zip(rope.rotate(p, q, k, pos, transpose=transpose), keep):
+            check(got, x, pos, rot, interleaved, transpose=transpose)
+    assert torch.equal(q, keep[0]) and torch.equal(k, keep[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", SCALES)
+def test_scalings_at_far_positions(dev, scale):
+    q, k, _ = inputs(12, 4, 2, 128, torch.float32, dev)
+    pos = torch.tensor([0, 1, 2, 31, -1, -77, 4095, 131071, 1 << 20, (1 << 24) + 1, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device=dev)
+    p = rope.plan(rot_dim=128, device=dev, **scale)
+    # the oracle's own angle, p f in float64, is off by 2^-53 of itself, more than the bar from 2^28 rad on: compared below it
+    near = pos.cpu().numpy() < 2 ** 28
+    near &= pos.cpu().numpy() > -2 ** 28
+    for got, x in zip(rope.rotate(p, q, k, pos), (q, k)):
+        check(got[torch.from_numpy(near).to(dev)], x[torch.from_numpy(near).to(dev)], pos[torch.from_numpy(near).to(dev)], 128, False, **scale)
+        assert torch.isfinite(got).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot", [(128, 128), (64, 32), (64, 30)])
+def test_views_in_place(dev, dtype, interleaved, d, rot):
+    """q and k inside a fused projection's output, rotated in place: its other
+    columns and the rows behind keep their bits."""
+    rows, hq, hkv = 70, 6, 2
+    g = torch.Generator(device=dev).manual_seed(3)
+    x = torch.randn(rows + 9, hq + 2 * hkv, d, generator=g, device=dev).to(dtype)
+    pos = torch.randint(0, 5000, (rows,), generator=g, device=dev, dtype=torch.int32)
+    keep = x.clone()
+    p = rope.plan(rot_dim=rot, interleaved=interleaved, device=dev)
+    q, k = x[:rows, :hq], x[:rows, hq:hq + hkv]
+    got = rope.rotate(p, q, k, pos, q_out=q, k_out=x[:rows, hq:hq + hkv])
+    assert got[0] is q
+    check(q, keep[:rows, :hq], pos, rot, interleaved)
+    check(k, keep[:rows, hq:hq + hkv], pos, rot, interleaved)
+    assert torch.equal(x[:, hq + hkv:], keep[:, hq + hkv:]) and torch.equal(x[rows:], keep[rows:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_strides(dev, interleaved):
+    """Head-major inputs and outputs, broadcast inputs, addresses off 16 bytes."""
+    rows, h, d = 37, 5, 64
+    q, k, pos = inputs(rows, h, 2, d, torch.bfloat16, dev)
+    p = rope.plan(rot_dim=d, interleaved=interleaved, device=dev)
+    want = rope.rotate(p, q, k, pos)
+    major = q.transpose(0, 1).contiguous().transpose(0, 1)
+    out = torch.empty_like(major.transpose(0, 1).contiguous()).transpose(0, 1)
+    assert torch.equal(rope.rotate(p, major, None, pos, q_out=out)[0], want[0])
+    buf = torch.zeros(rows * h * d + 1, dtype=torch.bfloat16, device=dev)
+    odd = buf[1:].view(rows, h, d)
+    odd.copy_(q)
+    for got, w in zip(rope.rotate(p, odd, k, pos, q_out=odd), want):
+        assert torch.equal(got, w)
+    assert buf[0] == 0
+    one = q[:, :1].expand(rows, 4, d)
+    got, none = rope.rotate(p, one, None, pos)
+    assert none is None and torch.equal(got, want[0][:, :1].expand(rows, 4, d))
+    same_row = q[:1].expand(rows, h, d)
+    check(rope.rotate(p, same_row, None, pos)[0], same_row, pos, d, interleaved)
+
+
+@pytest.mark.gpu
+def test_gradient(dev):
+    """The transpose against the formula (<g, R x> = <R' g, x>) and against
+    differences of the rotation, a YaRN magnitude included. In fp32 an element
+    errs by 2^-21 m (|x0| + |x1|) + 2^-24 |y|."""
+    scale = dict(scaling="yarn", factor=8.0, original_len=256.0)
+    q, k, pos = inputs(9, 3, 2, 64, torch.float32, dev, far=4096)
+    gq, gk, _ = inputs(9, 3, 2, 64, torch.float32, dev, seed=50)
+    for interleaved in (False, True):
+        p = rope.plan(rot_dim=48, interleaved=interleaved, device=dev, **scale)
+        y, dx = rope.rotate(p, q, k, pos), rope.rotate(p, gq, gk, pos, transpose=True)
+        for x, g, a, b in zip((q, k), (gq, gk), y, dx):
+            check(b, g, pos, 48, interleaved, transpose=True, **scale)
+            left, right = (g.double() * a.double()).sum(), (b.double() * x.double()).sum()
+            m = 0.1 * math.log(8.0) + 1
+            assert abs(left - right) <= 4 * 2.0 ** -21 * m * (g.double().abs().sum() * x.double().abs().max())
+            for at in ((0, 0, 0), (3, 1, 20), (8, 0, 47), (5, 1, 60)):
+                step = torch.zeros_like(x)
+                step[at] = 0.5
+                ends = [rope.rotate(p, x + s * step, None, pos)[0].double() for s in (1, -1)]
+                slope = ((ends[0] - ends[1]) * g.double()).sum()  # the ends are 1 apart, and the rotation is linear
+                row = at[0]
+                bar = 2 * 2.0 ** -21 * m * 2 * (x[row].abs().max() + 0.5).double() * g[row].double().abs().sum() * 2
+                assert abs(slope - b[at].double()) <= bar
+
+
+@pytest.mark.gpu
+def test_streams_and_graphs(dev):
+    q, k, pos = inputs(100, 8, 2, 128, torch.bfloat16, dev)
+    p = rope.plan(rot_dim=128, device=dev)
+    want = rope.rotate(p, q, k, pos)
+    s = torch.cuda.Stream(dev)
+    torch.cuda.synchronize()
+    got = rope.rotate(p, q, k, pos, stream=s)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    out = [torch.empty_like(x) for x in (q, k)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        rope.rotate(p, q, k, pos, q_out=out[0], k_out=out[1])
+    for n in range(4):
+        pos.add_(17)
+        for o in out:
+            o.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        want = rope.rotate(p, q, k, pos)
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.gpu
+def test_python_refusals(dev):
+    q, k, pos = inputs(10, 4, 2, 64, torch.bfloat16, dev)
+    p = rope.plan(rot_dim=64, device=dev)
+    fused = torch.zeros(10, 8, 64, dtype=torch.bfloat16, device=dev)
+    for err, a, kw in ((TypeError, (q.double(), k, pos), {}), (TypeError, (q, k.float(), pos), {}), (TypeError, (q, k, pos.long()), {}),
+                       (ValueError, (q, k, pos[:9]), {}), (ValueError, (q[:9], k, pos), {}), (ValueError, (q, k, pos.cpu()), {}),
+                       (ValueError, (q, k[..., :32], pos), {}), (ValueError, (q.transpose(1, 2).contiguous().transpose(1, 2), k, pos), {}),
+                       (ValueError, (q, k, pos), dict(q_out=k)), (ValueError, (q, k, pos), dict(q_out=q[:9])), (ValueError, (q, None, pos), dict(k_out=k)),
+                       (ValueError, (fused[:, :4], fused[:, 4:6], pos), dict(q_out=fused[:, 2:6])),
+                       (ValueError, (q, k, pos), dict(q_out=fused[:, :4], k_out=fused[:, 3:5])), (TypeError, (None, k, pos), {}),
+                       (ValueError, (q.cpu(), k.cpu(), pos.cpu()), {})):
+        with pytest.raises(err):
+            rope.rotate(p, *a, **kw)
+    with pytest.raises(_lib.SangamError):
+        rope.rotate(rope.plan(rot_dim=128, device=dev), q, k, pos)
+    with pytest.raises(_lib.SangamError):
+        rope.rotate(p, q, k, pos, q_out=torch.empty(1, 1, 64, dtype=q.dtype, device=dev).expand(10, 4, 64))
+    empty = rope.rotate(p, q[:0], k[:0], pos[:0])
+    assert empty[0].shape == (0, 4, 64)
