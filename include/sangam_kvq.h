@@ -19,8 +19,8 @@
  * again gives the same values) but for magnitudes within 2^125 of 2^128, which
  * may round to 2^128 and read back as infinity. A block with an infinity or a
  * NaN has b = 255 and codes 0, and reads back as NaN. Blocks that other writers
- * made read as the formats define them, scale bytes below 10 excepted (their
- * values may be lost to 0).
+ * made read as the formats define them; values below 2^-126, under scale bytes
+ * below 10, count as 0 in the attention.
  *
  * Layouts (row-major, contiguous, 16-byte aligned):
  *   k, v              [pool_pages, Hkv, 16, D] (e4m3) or [pool_pages, Hkv, 16, D / 2] bytes

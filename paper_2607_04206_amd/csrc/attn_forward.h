@@ -27,11 +27,14 @@ struct LaunchEvents {
 
 // A launch with events carries them in its dispatch (hipExtLaunchKernel), so
 // their timestamps bracket the kernel itself, as a kernel trace does.
+inline hipError_t launch_args(const void* fn, dim3 grid, unsigned threads, void** kargs, hipStream_t stream, LaunchEvents ev) {
+    if (!ev.start && !ev.stop) return hipLaunchKernel(fn, grid, dim3(threads), kargs, 0, stream);
+    return hipExtLaunchKernel(fn, grid, dim3(threads), kargs, 0, stream, ev.start, ev.stop, 0);
+}
 template <typename Args>
 hipError_t launch(const void* fn, dim3 grid, unsigned threads, Args args, hipStream_t stream, LaunchEvents ev) {
     void* kargs[] = {&args};
-    if (!ev.start && !ev.stop) return hipLaunchKernel(fn, grid, dim3(threads), kargs, 0, stream);
-    return hipExtLaunchKernel(fn, grid, dim3(threads), kargs, 0, stream, ev.start, ev.stop, 0);
+    return launch_args(fn, grid, threads, kargs, stream, ev);
 }
 
 // The split merge of a call whose tiles do not merge (attn_fwd.hip).

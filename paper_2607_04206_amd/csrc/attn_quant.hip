@@ -22,15 +22,35 @@ using namespace sangam;
 
 namespace {
 
+// LDS of a tile: its stage buffers, or V tiles and page ids where waves are on
+// their own, and, later, the sums of those that share a context
+constexpr int tile_bytes(int d, int qw, int kw, int nb, int nstage, bool across) {
+    const bool solo = qw == 1 && across;
+    const int stages = solo ? kw * 32 * d * 2 + kMaxCachedRange / 16 * 8 : 2 * nstage * 32 * nb * kw * d * 2;
+    const int sums = kw > 1 ? qw * kw * (d / 2 + 2) * 64 * 4 : 0;
+    return stages > sums ? stages : sums;
+}
+
+// deal: 0, or the number of CUs, where all of a launch's tiles, longest first,
+// are on the chip at once, several to a CU: every other round of one per CU is
+// dealt out backwards, so that the CUs with the longest tiles of one get the
+// shortest of the next (32 MHA decodes of up to 1151 keys 51.2 -> 49.1 us).
 template <typename Fmt, int D, int QW, int KW, int QB, int NB, int NSTAGE, bool HEADS_ACROSS>
-__global__ __launch_bounds__(64 * QW * KW, waves_per_simd(QB, false)) void attn_quant_kernel(QuantArgs a) {
-    __shared__ TileShared<2 * NSTAGE * 32 * NB * KW * D * 2> shared;
-    const TileRec t = a.tiles[blockIdx.x];
+__global__ __launch_bounds__(64 * QW * KW, waves_per_simd(QB, false)) void attn_quant_kernel(QuantArgs a, uint32_t deal) {
+    __shared__ TileShared<tile_bytes(D, QW, KW, NB, NSTAGE, HEADS_ACROSS)> shared;
+    uint32_t b = blockIdx.x;
+    if (QW == 1 && deal > 0) {
+        const uint32_t round = b / deal;
+        if ((round & 1) && (round + 1) * deal <= gridDim.x) b = (2 * round + 1) * deal - 1 - b;
+    }
+    const TileRec t = a.tiles[b];
     attn_tile<D, QW, KW, QB, NB, NSTAGE, HEADS_ACROSS, 0, QuantCache<Fmt>>(a, t, a.items[t.item], shared);
 }
 
 // Prefill-shaped tiles and MHA block decodes in one launch, as
-// attn_mixed_kernel; tiles of 256 rows are taken as two of 128.
+// attn_mixed_kernel; tiles of 256 rows are taken as two of 128. At head dim 128
+// all four waves take a decode's keys (16 decodes beside 1819 and 1201 rows 169
+// us, with two of them 174), a block ahead (two do not fit the registers).
 struct MixedQuantArgs {
     QuantArgs a;  // tiles: the prefill-shaped ones
     const TileRec* decode_tiles;
@@ -40,12 +60,14 @@ struct MixedQuantArgs {
 
 template <typename Fmt, int D>
 __global__ __launch_bounds__(256, 2) void attn_quant_mixed_kernel(MixedQuantArgs m) {
-    __shared__ TileShared<2 * 2 * 64 * D * 2> shared;
+    constexpr int KW = D == 128 ? 4 : 2;
+    constexpr int PREFILL = tile_bytes(D, 4, 1, 2, 2, false), DECODE = tile_bytes(D, 1, KW, 1, 1, true);
+    __shared__ TileShared<(PREFILL > DECODE ? PREFILL : DECODE)> shared;
     const MixedBlock b = mixed_block(m.order, blockIdx.x);
     if (b.index < 0) return;
     if (b.decode) {
         const TileRec t = m.decode_tiles[b.index];
-        attn_tile<D, 1, 2, 1, 1, 2, true, 2, QuantCache<Fmt>>(m.a, t, m.a.items[t.item], shared);
+        attn_tile<D, 1, KW, 1, 1, 1, true, 4 - KW, QuantCache<Fmt>>(m.a, t, m.a.items[t.item], shared);
         return;
     }
     TileRec t = m.a.tiles[b.index >> m.wide];
@@ -68,9 +90,10 @@ struct QuantKernels {
     }
 
     template <int D, int QW, int KW, int QB, int NB, bool HA, int NSTAGE = 2>
-    static hipError_t tiles(const Args& args, int n_tiles, hipStream_t stream, LaunchEvents ev) {
-        return launch(reinterpret_cast<const void*>(&attn_quant_kernel<Fmt, D, QW, KW, QB, NB, NSTAGE, HA>),
-                      dim3(unsigned(n_tiles)), unsigned(64 * QW * KW), args, stream, ev);
+    static hipError_t tiles(const Args& args, int n_tiles, hipStream_t stream, LaunchEvents ev, uint32_t deal = 0) {
+        void* kargs[] = {const_cast<Args*>(&args), &deal};
+        return launch_args(reinterpret_cast<const void*>(&attn_quant_kernel<Fmt, D, QW, KW, QB, NB, NSTAGE, HA>),
+                           dim3(unsigned(n_tiles)), unsigned(64 * QW * KW), kargs, stream, ev);
     }
 
     hipError_t mixed(const PlanHeader& h, const Args& args, const TileRec* decodes, const MixedOrder& order,
@@ -96,8 +119,10 @@ struct QuantKernels {
     static hipError_t decode_tiles(const PlanHeader& h, const Args& args, hipStream_t stream, LaunchEvents ev, bool* supported) {
         *supported = true;
         const int n = h.n_decode_tiles, kw = h.decode_kw, nb = h.decode_nb;
-        if (h.decode_qw == 1 && kw == 2 && nb == 1) return tiles<D, 1, 2, 1, 1, true>(args, n, stream, ev);
-        if (h.decode_qw == 2 && kw == 2 && nb == 2) return tiles<D, 2, 2, 1, 2, true>(args, n, stream, ev);
+        const int cus = h.cus > 0 ? h.cus : 256;
+        // one query head: four work-groups to a CU at least
+        if (h.decode_qw == 1 && kw == 2 && nb == 1) return tiles<D, 1, 2, 1, 1, true>(args, n, stream, ev, n <= 4 * cus ? cus : 0);
+        if (h.decode_qw == 2 && kw == 2 && nb == 2) return tiles<D, 2, 2, 1, 2, true, 1>(args, n, stream, ev);
         if (kw == 1 && nb == 2) {
             switch (h.decode_qw) {
                 case 3: return tiles<D, 3, 1, 1, 2, true>(args, n, stream, ev);

@@ -211,13 +211,14 @@ struct TileShared {
 //   NSTAGE K/V stage buffers in LDS (NSTAGE - 1 stages in flight). 1: K and V
 //          have one buffer each, and K of the next stage arrives while V of
 //          this one is used, V while its K is
-//          (bf16; a quantised cache has no turns: its next stage waits in
-//          registers, and one buffer leaves LDS to more work-groups)
+//          (bf16; over a quantised cache the next stage waits in registers;
+//          where every wave is for itself, this many blocks do)
 //   HELP   more waves, which only stage and write back
 //   Cache  what the cached rows are
 template <int D, int QW, int KW, int QB, int NB, int NSTAGE, bool HEADS_ACROSS, int HELP, typename Cache, typename Shared>
 __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const TileRec t, const ItemRec it, Shared& shared) {
     constexpr bool QUANT = Cache::QUANT;
+    constexpr bool SOLO = QUANT && QW == 1 && HEADS_ACROSS;  // every wave for itself (below)
     constexpr int NT = 64 * (QW * KW + HELP);  // threads
     constexpr int KT = 32 * NB;          // keys per wave per stage
     constexpr int STEP = KT * KW;        // keys per stage
@@ -257,7 +258,7 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
     static_assert(NSTAGE <= 2 || SP % NW == 0, "deeper pipelines need whole staging rounds");
     static_assert(64 % SP == 0 && (NSTAGE - 1) * SP < 64, "a stage's page ids sit in one register of 64 lanes");
 
-    static_assert(sizeof(shared.stages) >= 2 * NSTAGE * TILE, "the stage buffers");
+    static_assert(SOLO || sizeof(shared.stages) >= 2 * NSTAGE * TILE, "the stage buffers");
     uint8_t* const smem = shared.stages;
     int32_t* const fpos = shared.fpos;
     int32_t* const wpages = shared.wpages;
@@ -313,7 +314,7 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
         const int row = row_base + 32 * qb + qn;
         const uint16_t* qp = a.q + ((size_t)(it.q_start + (row < it.n ? row : 0)) * a.hq + head) * D;
 #pragma unroll
-        for (int s = 0; s < DS; ++s) qf[qb][s] = *(const bf16x8*)(qp + 16 * s + 8 * hh);
+        for (int s = 0; s < DS; ++s) qf[qb][s] = *(const bf16x8*)(qp + (SOLO ? 8 * s + D / 2 * hh : 16 * s + 8 * hh));
     }
 
     // ---- staging. A stage is SP pages of 16 key rows; wave w copies pages
@@ -780,7 +781,9 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
     if (tid < nwp) wpage = a.page_ids[it.page_start + (plist ? lpos >> 4 : wpg0 + tid)];
     constexpr auto yes = std::true_type{};
     constexpr auto no = std::false_type{};
-    if constexpr (QUANT) {
+    if constexpr (SOLO) {
+        // begins below
+    } else if constexpr (QUANT) {
         if (NB != 4) {
             fetch(0);
             next_pages(0);
@@ -795,7 +798,203 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
         if (plist) fpos[tid] = lpos;
     }
     int st = 0;
-    if constexpr (QUANT) {
+    if constexpr (SOLO) {
+        // One query head: no other wave of the work-group reads the keys of this
+        // one, so nothing is shared and nothing waits at a barrier. A wave takes
+        // every KW-th block of 32 keys, loads it NSTAGE blocks ahead into
+        // registers and converts it there. K goes from them into QK^T directly:
+        // the order of the dims in that product is free as long as Q has the
+        // same one, and with dims D / 2 hh + 8 n at step n a lane's operands are
+        // one half of its key's row, whole blocks that it can load. V, whose
+        // operands run along the keys, is turned through a tile of LDS of the
+        // wave's own. The page ids of the tile's range stand in LDS.
+        // Bound by HBM where there are tiles enough: 64 contexts of 206,649
+        // positions in all, 32 heads, e4m3, 355 us (5.3 TB/s are fetched) against
+        // 543 for tiles of bf16 values that two waves share, with a barrier per
+        // stage. (K loaded in the order of memory and passed to its lanes
+        // through LDS takes half the lines per instruction, and 363 us.)
+        static_assert(QB == 1 && NB == 1 && NSTAGE <= 2, "a block of 32 keys at a time");
+        constexpr int BL = D / 64;                    // blocks of K, and of V, per lane
+        constexpr int PAGES = kMaxCachedRange / 16;   // of a tile (an item without cached rows has two at most)
+        static_assert(KW * 32 * ROWB + PAGES * 8 <= sizeof(shared.stages), "V tiles, page ids and page_info");
+        struct Keys {
+            typename Cache::Block k[BL], v[BL];
+            uint32_t k_scales;  // of k, a byte each
+        };
+        int32_t* const ids = reinterpret_cast<int32_t*>(smem + KW * 32 * ROWB);
+        uint32_t* const infos = reinterpret_cast<uint32_t*>(ids + PAGES);
+        for (int k = tid; k < npg; k += NT) {
+            ids[k] = a.page_ids[it.page_start + pg0 + k];
+            if (plist) infos[k] = a.page_info[it.page_start + pg0 + k];
+        }
+        __syncthreads();
+        const int nblocks = (kv_end - kv_begin + 31) / 32;
+        const int first_fresh = plist ? __builtin_amdgcn_readfirstlane(lpos) : it.o;
+        auto place_of = [&](int b, int r) {  // row of the pool that holds key r of block b
+            return (size_t(uint32_t(ids[2 * b + (r >> 4)])) * a.hkv + t.kv_head) * 16 + (r & 15);
+        };
+        auto fresh_row = [&](int b, int r) -> int64_t {  // row of k_new / v_new of key r of block b, or -1
+            if (plist) {
+                const uint32_t inf = infos[2 * b + (r >> 4)], s = r & 15;
+                return (inf >> s) & 1u ? int64_t(it.q_start) + (inf >> kPageInfoRowShift) + __builtin_popcount(inf & ((1u << s) - 1u)) : -1;
+            }
+            const int n = kv_begin + 32 * b + r - it.o;
+            return unsigned(n) < unsigned(it.n) ? int64_t(it.q_start) + n : -1;
+        };
+        const uint8_t* const kc = reinterpret_cast<const uint8_t*>(a.k_cache);
+        const uint8_t* const vc = reinterpret_cast<const uint8_t*>(a.v_cache);
+        auto load = [&](int b, Keys& x) __attribute__((always_inline)) {
+            const int last = kv_end - kv_begin - 32 * b - 1;  // keys past the range: its last one, masked later
+            const size_t kr = place_of(b, min(qn, last)) * BPR + hh * BL;
+#pragma unroll
+            for (int i = 0; i < BL; ++i) x.k[i].load(kc, kr + i);
+            x.k_scales = BL == 2 ? uint32_t(*(const uint16_t*)(a.k_scale + kr)) : a.k_scale[kr];
+#pragma unroll
+            for (int i = 0; i < BL; ++i) {
+                const int u = i * 64 + lane;
+                x.v[i].load(vc, a.v_scale, place_of(b, min(u / BPR, last)) * BPR + u % BPR);
+            }
+            asm volatile("" ::: "memory");  // the loads stay up here
+        };
+        // what was loaded, from here on (the compiler would split the scales,
+        // and wait for them, right behind the load)
+        auto arrive = [&](Keys& x) __attribute__((always_inline)) {
+            asm volatile("" : "+v"(x.k_scales));
+#pragma unroll
+            for (int i = 0; i < BL; ++i) {
+                x.k[i].scale = x.k_scales >> (8 * i) & 255u;
+                asm volatile("" : "+v"(x.v[i].scale));
+            }
+        };
+        uint8_t* const vtile = smem + ks * 32 * ROWB;
+        const uint32_t va = lds0 + ks * 32 * ROWB + voff;
+        // One block, whose K operands and pieces of V `k_piece` and `v_piece`
+        // give; `next` is called when both have been taken.
+        auto block = [&](int b, auto k_piece, auto v_piece, auto next) __attribute__((always_inline)) {
+            const int last = kv_end - kv_begin - 32 * b - 1;
+            f32x16 s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+            for (int n = 0; n < DS; ++n)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k_piece(n)), qf[0][n], s, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < BL; ++i) {
+                const int u = i * 64 + lane, r = u / BPR, c = 4 * (u % BPR);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *(LDS u32x4*)(vtile + r * ROWB + (((c + e) ^ swz_v<D>(r)) << 4)) = v_piece(i, e);
+            }
+            asm volatile("" ::: "memory");
+            next();
+            if (last < 31)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + 4 * hh + (i & 3) > last) s[i] = -INFINITY;
+            float mx = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+            mx = half_max(mx) * c;
+            const bool need = mx > m_used[0] + kRescaleThreshold;
+            if (__builtin_amdgcn_ballot_w64(need)) {
+                const float alpha = need ? __builtin_amdgcn_exp2f(m_used[0] - mx) : 1.0f;
+                m_used[0] = need ? mx : m_used[0];
+                l_run[0] *= alpha;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[0][mb][i] *= alpha;
+            }
+            const float mneg = m_used[0] == -INFINITY ? 0.0f : -m_used[0];
+            bf16x8 pf[2];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, mneg));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], c, mneg));
+                l_run[0] += p0 + p1;
+                pf[i >> 3][i & 7] = (__bf16)p0;
+                pf[i >> 3][(i & 7) + 1] = (__bf16)p1;
+            }
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) {
+                    const uint32_t vp = (va ^ uint32_t(mb << 6)) + kk * 16 * ROWB;
+                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS bf16x4*)(uintptr_t)vp);
+                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LDS bf16x4*)(uintptr_t)(vp + 8 * ROWB));
+                    o[0][mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, pf[kk],
+                                                                      o[0][mb], 0, 0, 0);
+                }
+            asm volatile("" ::: "memory");
+        };
+        // blocks [m0, m1) may hold fresh rows; the others are taken first
+        const int m0 = min(nblocks, max(0, first_fresh - kv_begin) / 32);
+        const int m1 = last_pos < kv_begin ? m0 : min(nblocks, (last_pos - kv_begin) / 32 + 1);
+        const int cached = m0 + nblocks - m1;
+        if (computes) {
+            Keys x[NSTAGE];
+            auto at = [&](int k) { return k < m0 ? k : k + m1 - m0; };
+            auto take = [&](int k, Keys& y, auto next) __attribute__((always_inline)) {
+                arrive(y);
+                block(at(k), [&](int n) { return y.k[n / 4].piece(n % 4); }, [&](int i, int e) { return y.v[i].piece(e); },
+                      [&]() { if constexpr (decltype(next)::value) load(at(k + NSTAGE * KW < cached ? k + NSTAGE * KW : k), y); });
+            };
+            // Every pass loads, past the end a block that it has, and a pair of
+            // passes has no way out between: with loads that may not be there
+            // the compiler waits for all of them.
+            if (ks < cached) {
+                int k = ks;
+                load(at(k), x[0]);
+                if constexpr (NSTAGE == 2) {
+                    load(at(k + KW < cached ? k + KW : k), x[1]);
+                    for (; k + KW < cached; k += 2 * KW) {
+                        take(k, x[0], yes);
+                        take(k + KW, x[1], yes);
+                    }
+                    if (k < cached) take(k, x[0], no);
+                } else {
+                    for (; k < cached; k += KW) take(k, x[0], yes);
+                }
+            }
+            for (int b = m0 + ks; b < m1; b += KW) {
+                const int last = kv_end - kv_begin - 32 * b - 1;
+                load(b, x[0]);
+                arrive(x[0]);
+                const int64_t krow = fresh_row(b, min(qn, last));
+                const uint16_t* const kf = a.k_new + ((size_t)(krow < 0 ? 0 : krow) * a.hkv + t.kv_head) * D + D / 2 * hh;
+                block(b,
+                      [&](int n) {
+                          const u32x4 f = *(const u32x4*)(kf + 8 * n);
+                          return krow < 0 ? x[0].k[n / 4].piece(n % 4) : f;
+                      },
+                      [&](int i, int e) {
+                          const int u = i * 64 + lane;
+                          const int64_t row = fresh_row(b, min(u / BPR, last));
+                          const u32x4 f = *(const u32x4*)(a.v_new + ((size_t)(row < 0 ? 0 : row) * a.hkv + t.kv_head) * D + u % BPR * kMxBlock + 8 * e);
+                          return row < 0 ? x[0].v[i].piece(e) : f;
+                      },
+                      []() {});
+            }
+        }
+        if (writer) {  // the fresh rows of the range into their pages, a block per thread
+            for (int u = tid; u < it.n * BPR; u += NT) {
+                const int row = u / BPR, b = u % BPR;
+                const int p = plist ? a.positions[it.pos_start + row] : it.o + row;
+                if (p < wb_lo || p >= wb_hi) continue;
+                const size_t at = ((size_t(uint32_t(ids[(p >> 4) - pg0])) * a.hkv + t.kv_head) * 16 + (p & 15)) * BPR + b;
+                const size_t from = ((size_t)(it.q_start + row) * a.hkv + t.kv_head) * D + b * kMxBlock;
+                typename Cache::Block q;
+                u32x4 x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = *(const u32x4*)(a.k_new + from + 8 * e);
+                q.quantise(x);
+                q.store(reinterpret_cast<uint8_t*>(a.k_cache), a.k_scale, at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = *(const u32x4*)(a.v_new + from + 8 * e);
+                q.quantise(x);
+                q.store(reinterpret_cast<uint8_t*>(a.v_cache), a.v_scale, at);
+            }
+        }
+    } else if constexpr (QUANT) {
         // Stage st + 1 is on its way into registers while stage st is
         // computed; with two buffers it is placed before the barrier that ends
         // stage st, with one behind it. A whole prefill's stages are copied
@@ -895,13 +1094,16 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
             mine[(MB * 16 + 1) * 64 + lane] = l_run[0];
         }
         __syncthreads();
-        static_assert(KW == 2, "sums of two");
-        const float* src[2] = {mbuf, mbuf + MERGE_REGS * 64};
-        const float m_tot = fmaxf(src[0][(MB * 16) * 64 + lane], src[1][(MB * 16) * 64 + lane]);
-        // wave ks = 0 always holds a valid key, so m_tot is finite
-        float sc[2], l[2];
+        const float* src[KW];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < KW; ++k) src[k] = mbuf + k * MERGE_REGS * 64;
+        float m_tot = fmaxf(src[0][(MB * 16) * 64 + lane], src[1][(MB * 16) * 64 + lane]);
+#pragma unroll
+        for (int k = 2; k < KW; ++k) m_tot = fmaxf(m_tot, src[k][(MB * 16) * 64 + lane]);
+        // wave ks = 0 always holds a valid key, so m_tot is finite
+        float sc[KW], l[KW];
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
             sc[k] = __builtin_amdgcn_exp2f(src[k][(MB * 16) * 64 + lane] - m_tot);
             l[k] = src[k][(MB * 16 + 1) * 64 + lane];
         }
@@ -910,12 +1112,16 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
         const float l1 = sc[1] * l[1];
         l_run[0] = __builtin_fmaf(sc[0], l[0], l1);
 #pragma unroll
+        for (int k = 2; k < KW; ++k) l_run[0] = __builtin_fmaf(sc[k], l[k], l_run[0]);
+#pragma unroll
         for (int mb = 0; mb < MBW; ++mb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int at = ((mb0 + mb) * 16 + i) * 64 + lane;
                 const float o0 = sc[0] * src[0][at];
                 o[0][mb][i] = __builtin_fmaf(sc[1], src[1][at], o0);
+#pragma unroll
+                for (int k = 2; k < KW; ++k) o[0][mb][i] = __builtin_fmaf(sc[k], src[k][at], o[0][mb][i]);
             }
         m_used[0] = m_tot;
     }
@@ -1049,8 +1255,9 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
     // row in 16-byte pieces (stored directly, one instruction would leave
     // 16-byte fragments of 32 rows).
     constexpr int EROW = D * 2 + 16;  // bytes per staged row: 16-byte aligned, shifted by four banks
-    constexpr int EBASE = KW > 1 ? QW * KW * MERGE_REGS * 64 * 4 : 0;  // past the waves' partials
+    constexpr int EBASE = KW > 1 && !SOLO ? QW * KW * MERGE_REGS * 64 * 4 : 0;  // past the waves' partials, or in their place
     constexpr bool ESTAGE = EBASE + QW * QB * 32 * EROW <= sizeof(shared.stages);
+    if constexpr (SOLO) __syncthreads();  // every wave has read the partials
     if constexpr (ESTAGE && KW == 1) {
         if (!split_out) __syncthreads();  // every wave is past its last stage's reads
     }

@@ -101,8 +101,7 @@ __device__ __forceinline__ float mx_power(uint32_t scale) { return __uint_as_flo
 // 8 values of a block, or their codes
 template <typename Fmt>
 __device__ __forceinline__ mx_u32x4 mx_read(const uint32_t (&c)[Fmt::kWords], uint32_t scale) {
-    const mx_u32x4 x = Fmt::read(c, mx_power(scale));
-    return scale == kMxNaN ? mx_u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u} : x;
+    return Fmt::read(c, mx_power(scale));  // (NaN for any code under 255: an exponent of all ones is a NaN scale)
 }
 template <typename Fmt>
 __device__ __forceinline__ void mx_write(uint32_t (&c)[Fmt::kWords], mx_u32x4 x, uint32_t scale) {
@@ -120,9 +119,12 @@ struct MxBlock {
     uint32_t scale;
 
     // block `at` of a tensor's codes and scales
-    __device__ __forceinline__ void load(const uint8_t* code, const uint8_t* scales, size_t at) {
+    __device__ __forceinline__ void load(const uint8_t* code, size_t at) {
 #pragma unroll
         for (int w = 0; w < Fmt::kWords; ++w) codes[w] = *(const mx_u32x4*)(code + at * kBytes + 16 * w);
+    }
+    __device__ __forceinline__ void load(const uint8_t* code, const uint8_t* scales, size_t at) {
+        load(code, at);
         scale = scales[at];
     }
     __device__ __forceinline__ void store(uint8_t* code, uint8_t* scales, size_t at) const {
