@@ -7,7 +7,10 @@
 // and 8 (e4m3) or 4 (e2m1) on the pool side; four neighbouring lanes hold a
 // block, so that both sides' accesses are whole rows and whole chunks of a
 // page, and the import finds the block's largest magnitude with two exchanges
-// inside the quad. Bound by HBM.
+// inside the quad. Bound by HBM: a hand-off of 304 MB (packed) through e4m3 pages
+// 163 us, 5.7 TB/s of a streaming read's 5.83, one of 91 MB through e2m1 pages 48
+// (4.8 TB/s); large exports, four fifths of whose bytes are written, by its
+// write rate (3.8 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -38,13 +41,28 @@ struct KvqCopyArgs {
 
 constexpr int64_t kMaxBlocks = (int64_t(1) << 32) / 256 - 1;  // a grid's threads are counted in 32 bits
 
+// Packed bytes (K and V) from which the stores are nontemporal. Measured, import
+// and export by themselves with plain -> with nontemporal stores: e4m3 65 MB
+// 19.8 -> 18.0 and 20.6 -> 15.5 us, 304 MB 87.1 -> 83.9 and 87.4 -> 79.9, 1408 MB
+// 397 -> 372 and 417 -> 378; e2m1 65 MB 15.3 -> 15.1 and 17.1 -> 13.1, 1408 MB 344
+// -> 338 and 438 -> 366. An export right behind its import, which finds less of
+// the pages in the cache: e4m3 65 MB together 41.7 -> 38.8, 91 MB 51.7 -> 53.2, 304
+// MB 174 -> 163. Smaller ones are left to whoever reads them next.
+constexpr int64_t kStreamBytes = int64_t(32) << 20;
+
 // the largest of a quad's values, in all four lanes
 __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
     x = max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0xB1, 0xF, 0xF, true)));  // lanes 1 0 3 2
     return max(x, uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x4E, 0xF, 0xF, true)));  // lanes 2 3 0 1
 }
 
-template <typename Fmt, int D, bool EXPORT>
+template <bool STREAM, typename T>
+__device__ __forceinline__ void put(T* p, T v) {
+    if (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
+template <typename Fmt, int D, bool EXPORT, bool STREAM>
 __global__ __launch_bounds__(256) void kvq_copy_kernel(KvqCopyArgs a) {
     constexpr int NC = D / 8;             // pieces of a row
     constexpr int HPG = 256 / (16 * NC);  // heads of a work-group
@@ -65,25 +83,29 @@ __global__ __launch_bounds__(256) void kvq_copy_kernel(KvqCopyArgs a) {
     if (EXPORT) {
 #pragma unroll
         for (int w = 0; w < Fmt::kWords; ++w) c[w] = code[w];
-        *packed = mx_read<Fmt>(c, a.scales[t][block]);
+        put<STREAM>(packed, mx_read<Fmt>(c, a.scales[t][block]));
     } else {
         const mx_u32x4 x = *packed;
         const mx_u16x2 m = mx_largest(mx_u16x2{0, 0}, x);
         const uint32_t scale = mx_scale<Fmt>(quad_max(m[0] > m[1] ? m[0] : m[1]));
         mx_write<Fmt>(c, x, scale);
 #pragma unroll
-        for (int w = 0; w < Fmt::kWords; ++w) code[w] = c[w];
+        for (int w = 0; w < Fmt::kWords; ++w) put<STREAM>(code + w, c[w]);
         if (pos % 4 == 0) a.scales[t][block] = uint8_t(scale);
     }
 }
 
+template <typename Fmt, int D>
+const void* copy_fn(bool is_export, bool stream) {
+    if (is_export)
+        return stream ? reinterpret_cast<const void*>(&kvq_copy_kernel<Fmt, D, true, true>)
+                      : reinterpret_cast<const void*>(&kvq_copy_kernel<Fmt, D, true, false>);
+    return stream ? reinterpret_cast<const void*>(&kvq_copy_kernel<Fmt, D, false, true>)
+                  : reinterpret_cast<const void*>(&kvq_copy_kernel<Fmt, D, false, false>);
+}
 template <typename Fmt>
-const void* copy_fn(int d, bool is_export) {
-    if (d == 128)
-        return is_export ? reinterpret_cast<const void*>(&kvq_copy_kernel<Fmt, 128, true>)
-                         : reinterpret_cast<const void*>(&kvq_copy_kernel<Fmt, 128, false>);
-    return is_export ? reinterpret_cast<const void*>(&kvq_copy_kernel<Fmt, 64, true>)
-                     : reinterpret_cast<const void*>(&kvq_copy_kernel<Fmt, 64, false>);
+const void* copy_fn(int d, bool is_export, bool stream) {
+    return d == 128 ? copy_fn<Fmt, 128>(is_export, stream) : copy_fn<Fmt, 64>(is_export, stream);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -119,7 +141,8 @@ sangam_status run_copy(bool is_export, const void* plan_host, const void* plan_d
     args.hkv = h->hkv;
     const int heads = 256 / (2 * h->d);  // of a work-group
     args.groups = uint32_t((h->hkv + heads - 1) / heads);
-    const void* fn = cache->format == SANGAM_KV_E4M3 ? copy_fn<MxE4m3>(h->d, is_export) : copy_fn<MxE2m1>(h->d, is_export);
+    const bool nt = h->total_rows * h->hkv * h->d * 4 > kStreamBytes;
+    const void* fn = cache->format == SANGAM_KV_E4M3 ? copy_fn<MxE4m3>(h->d, is_export, nt) : copy_fn<MxE2m1>(h->d, is_export, nt);
     void* kargs[] = {&args};
     const int64_t step = std::max<int64_t>(kMaxBlocks / args.groups, 1);  // pages of a launch
     for (int64_t first = 0; first < h->total_pages; first += step) {
