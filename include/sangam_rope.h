@@ -88,7 +88,10 @@ typedef struct sangam_rope_tensor {
  * transpose 0 or 1.
  * Errors: SANGAM_ERR_PLAN, SANGAM_ERR_INVALID_ARG (a NULL pointer, a size or
  * stride out of range), SANGAM_ERR_UNSUPPORTED (dtype), SANGAM_ERR_ALIGN (a
- * pointer not aligned to its elements), SANGAM_ERR_HIP.
+ * pointer not aligned to its elements), SANGAM_ERR_HIP. An output that may
+ * share an element with an input (but for itself in place) or with the other
+ * output is SANGAM_ERR_INVALID_ARG: where the spans of the two overlap, unless
+ * both step from row to row alike and lie side by side in the rows.
  */
 sangam_status sangam_rope_rotate(const void *plan_host, const void *plan_dev, const sangam_rope_tensor *q,
                                  const sangam_rope_tensor *k, int32_t head_dim, int32_t dtype,

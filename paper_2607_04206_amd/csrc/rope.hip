@@ -53,6 +53,12 @@ struct RopeArgs {
 
 constexpr int kThreads = 256;
 
+// Output bytes from which the stores are nontemporal. Measured with plain ->
+// nontemporal stores, 64 heads of 128 dims: 33 MB 11.5 -> 12.1 us, 66 MB 28.5 ->
+// 21.6, 131 MB 51.8 -> 50.3, 256 MB 98.3 -> 95.1, 983 MB 365 -> 360. (What is
+// smaller stays in the cache for the attention that reads it next.)
+constexpr int64_t kStreamBytes = int64_t(48) << 20;
+
 // cos and sin of a number of turns given in 64 bits
 __device__ __forceinline__ float2 cos_sin(double turns) {
     const double quarter = __builtin_rint(4.0 * turns);
@@ -65,9 +71,15 @@ __device__ __forceinline__ float2 cos_sin(double turns) {
     return float2{(q == 1 || q == 2) ? -a : a, q >= 2 ? -b : b};
 }
 
+template <bool STREAM, typename V>
+__device__ __forceinline__ void put(void* p, V v) {
+    if (STREAM) __builtin_nontemporal_store(v, static_cast<V*>(p));
+    else *static_cast<V*>(p) = v;
+}
+
 // T: element; V: elements of a vector access (1 where a stride, an address or
 // the number of pairs does not allow whole ones)
-template <typename T, int V, bool INTERLEAVED>
+template <typename T, int V, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     typedef T Vec __attribute__((ext_vector_type(V)));
     extern __shared__ float2 angles[];  // [rows_each][rot / 2]
@@ -94,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
         T* out = static_cast<T*>(t.out) + (row0 + r) * t.out_row + h * t.out_head;
         if (c >= rotating) {  // past the rotating dims
             const int d = a.rot + (c - rotating) * V;
-            *(Vec*)(out + d) = *(const Vec*)(in + d);
+            put<STREAM>(out + d, *(const Vec*)(in + d));
             continue;
         }
         const float2* cs = angles + r * half;
@@ -108,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                 y[e] = T(x0 * w.x - x1 * w.y);
                 y[e + 1] = T(x1 * w.x + x0 * w.y);
             }
-            *(Vec*)(out + c * V) = y;
+            put<STREAM>(out + c * V, y);
         } else {
             const int lo = INTERLEAVED ? 2 * c : c * V, hi = INTERLEAVED ? lo + 1 : lo + half;
             const Vec x = *(const Vec*)(in + lo), z = *(const Vec*)(in + hi);
@@ -120,19 +132,21 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                 y[e] = T(x0 * k.x - x1 * k.y);
                 w[e] = T(x1 * k.x + x0 * k.y);
             }
-            *(Vec*)(out + lo) = y;
-            *(Vec*)(out + hi) = w;
+            put<STREAM>(out + lo, y);
+            put<STREAM>(out + hi, w);
         }
     }
 }
 
+template <typename T, int V, bool INTERLEAVED>
+const void* kernel_of(bool vectors, bool stream) {
+    if (!vectors) return reinterpret_cast<const void*>(&rope_kernel<T, 1, INTERLEAVED, false>);
+    return stream ? reinterpret_cast<const void*>(&rope_kernel<T, V, INTERLEAVED, true>)
+                  : reinterpret_cast<const void*>(&rope_kernel<T, V, INTERLEAVED, false>);
+}
 template <typename T, int V>
-const void* kernel_of(bool vectors, bool interleaved) {
-    if (vectors)
-        return interleaved ? reinterpret_cast<const void*>(&rope_kernel<T, V, true>)
-                           : reinterpret_cast<const void*>(&rope_kernel<T, V, false>);
-    return interleaved ? reinterpret_cast<const void*>(&rope_kernel<T, 1, true>)
-                       : reinterpret_cast<const void*>(&rope_kernel<T, 1, false>);
+const void* kernel_of(bool vectors, bool interleaved, bool stream) {
+    return interleaved ? kernel_of<T, V, true>(vectors, stream) : kernel_of<T, V, false>(vectors, stream);
 }
 
 sangam_status fail(sangam_status code, const std::string& msg) {
@@ -151,6 +165,24 @@ bool apart(int64_t rows, int64_t row_stride, int64_t heads, int64_t head_stride,
         return one_outer || outer >= span;
     };
     return nested(heads, head_stride, one_head, row_stride, one_row) || nested(rows, row_stride, one_row, head_stride, one_head);
+}
+
+// A view [rows, heads, d] of elements.
+struct View {
+    uintptr_t at;
+    int64_t row, head, heads;
+};
+
+// Whether two views may share an element: not where their spans, or, with the
+// same step from row to row, their columns of a row are apart (views of one
+// fused buffer).
+bool may_overlap(const View& a, const View& b, int64_t rows, int64_t d, int64_t size) {
+    const int64_t wa = (a.heads - 1) * a.head + d, wb = (b.heads - 1) * b.head + d;  // of a row
+    const int64_t gap = (int64_t(b.at) - int64_t(a.at)) / size;
+    if (gap >= (rows - 1) * a.row + wa || -gap >= (rows - 1) * b.row + wb) return false;
+    if (a.row != b.row || a.row <= 0 || wa > a.row || wb > a.row) return true;
+    const int64_t at = ((gap % a.row) + a.row) % a.row;  // b's first column, from a's
+    return at < wa || at + wb > a.row;
 }
 
 constexpr int64_t kMaxStride = int64_t(1) << 40;
@@ -198,6 +230,17 @@ extern "C" sangam_status sangam_rope_rotate(const void* plan_host, const void* p
         args.t[i] = RopeTensor{t->in, t->out, t->in_row_stride, t->in_head_stride, t->out_row_stride, t->out_head_stride};
     }
     if (rows == 0) return SANGAM_OK;
+    View views[4];  // inputs, outputs
+    for (int i = 0; i < 2; ++i) {
+        const RopeTensor& t = args.t[i];
+        views[i] = View{reinterpret_cast<uintptr_t>(t.in), t.in_row, t.in_head, heads[i]};
+        views[2 + i] = View{reinterpret_cast<uintptr_t>(t.out), t.out_row, t.out_head, heads[i]};
+    }
+    for (int o = 0; o < (k ? 2 : 1); ++o)
+        for (int i = 0; i < (k ? 2 : 1); ++i)
+            if (!(o == i && args.t[o].in == args.t[o].out) && may_overlap(views[i], views[2 + o], rows, head_dim, size))
+                return fail(SANGAM_ERR_INVALID_ARG, std::string(o ? "k's" : "q's") + " output overlaps " + (i ? "k" : "q") + " without being it");
+    if (k && may_overlap(views[2], views[3], rows, head_dim, size)) return fail(SANGAM_ERR_INVALID_ARG, "the outputs overlap");
     if (!plan_dev || !positions_dev) return fail(SANGAM_ERR_INVALID_ARG, "plan_dev and positions_dev must not be NULL");
     if (reinterpret_cast<uintptr_t>(plan_dev) & 15u || reinterpret_cast<uintptr_t>(positions_dev) & 3u)
         return fail(SANGAM_ERR_ALIGN, "plan_dev must be 16-byte and positions_dev 4-byte aligned");
@@ -220,9 +263,10 @@ extern "C" sangam_status sangam_rope_rotate(const void* plan_host, const void* p
     while (groups() < 512 && args.rows_each > 1) args.rows_each /= 2;
     while (groups() < 512 && int64_t(args.rows_each) * args.heads_each * args.units > kThreads && args.heads_each > 1)
         args.heads_each = (args.heads_each + 1) / 2;
-    const void* fn = dtype == SANGAM_DTYPE_FP32   ? kernel_of<float, 4>(vectors, h->interleaved)
-                     : dtype == SANGAM_DTYPE_FP16 ? kernel_of<_Float16, 8>(vectors, h->interleaved)
-                                                  : kernel_of<__bf16, 8>(vectors, h->interleaved);
+    const bool nt = rows * args.heads * head_dim * size > kStreamBytes;
+    const void* fn = dtype == SANGAM_DTYPE_FP32   ? kernel_of<float, 4>(vectors, h->interleaved, nt)
+                     : dtype == SANGAM_DTYPE_FP16 ? kernel_of<_Float16, 8>(vectors, h->interleaved, nt)
+                                                  : kernel_of<__bf16, 8>(vectors, h->interleaved, nt);
     void* kargs[] = {&args};
     const unsigned lds = unsigned(args.rows_each) * unsigned(h->rot_dim / 2) * unsigned(sizeof(float2));
     const unsigned splits = unsigned((args.heads + args.heads_each - 1) / args.heads_each);

@@ -65,20 +65,38 @@ def empty_cache(num_pool_pages: int, num_kv_heads: int, head_dim: int, *, format
     return QuantCache(*codes, *scales)
 
 
-def _stream(dev: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.cuda.Stream:
+def _expect(t: torch.Tensor, name: str, dtype, shape, dev) -> None:
+    """attn._need's checks; its words where one fails."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous()):
+        attn._need(t, name, dtype, shape, dev)
+
+
+def _launch(dev: torch.device, fn, *args) -> None:
+    """The C call with dev as the current device."""
+    if torch.cuda.current_device() == dev.index:
+        check(fn(*args))
+        return
+    with torch.cuda.device(dev):
+        check(fn(*args))
+
+
+def _stream(dev: torch.device, stream: Optional[torch.cuda.Stream]) -> int:
+    """The hipStream_t of the given or current stream (without a Stream object
+    for the current one, which takes longer than the call's checks)."""
     if dev.type != "cuda":
-        raise ValueError("the quantised cache needs device tensors (a ROCm GPU)")
+        raise ValueError("the call needs device tensors (a ROCm GPU)")
     if stream is None:
-        return torch.cuda.current_stream(dev)
+        return torch._C._cuda_getCurrentRawStream(dev.index)
     if stream.device != dev:
         raise ValueError(f"stream belongs to {stream.device}, the tensors are on {dev}")
-    return stream
+    return stream.cuda_stream
 
 
-def _new(shape, dtype, dev, stream: torch.cuda.Stream) -> torch.Tensor:
-    """A tensor that `stream` writes (its memory is not reused before that)."""
+def _new(shape, dtype, dev, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A tensor that `stream`, if not the current one, writes (its memory is
+    not reused before that)."""
     t = torch.empty(shape, dtype=dtype, device=dev)
-    if stream != torch.cuda.current_stream(dev):
+    if stream is not None:
         t.record_stream(stream)
     return t
 
@@ -94,39 +112,38 @@ def forward(p: attn.Plan, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Ten
     dev = q.device
     s = _stream(dev, stream)
     T, Hq, Hkv, D = p.total_q, p.num_q_heads, p.num_kv_heads, p.head_dim
-    attn._need(q, "q", torch.bfloat16, (T, Hq, D), dev)
-    attn._need(k_new, "k_new", torch.bfloat16, (T, Hkv, D), dev)
-    attn._need(v_new, "v_new", torch.bfloat16, (T, Hkv, D), dev)
+    _expect(q, "q", torch.bfloat16, (T, Hq, D), dev)
+    _expect(k_new, "k_new", torch.bfloat16, (T, Hkv, D), dev)
+    _expect(v_new, "v_new", torch.bfloat16, (T, Hkv, D), dev)
     _check_cache(cache, Hkv, D, p.num_pool_pages, dev)
     attn._need(page_ids, "page_ids", torch.int32, None, dev)
-    if page_ids.dim() != 1 or page_ids.numel() < p.total_pages:
+    num_page_ids = page_ids.numel()
+    if page_ids.dim() != 1 or num_page_ids < p.total_pages:
         raise ValueError(f"page_ids must be a 1-D tensor of at least {p.total_pages} entries "
                          "(the plan's page table, on the device)")
     if out is not None:
-        attn._need(out, "out", torch.bfloat16, (T, Hq, D), dev)
+        _expect(out, "out", torch.bfloat16, (T, Hq, D), dev)
     if lse is not None:
-        attn._need(lse, "lse", torch.float32, (T, Hq), dev)
+        _expect(lse, "lse", torch.float32, (T, Hq), dev)
     if workspace is not None and (not workspace.is_contiguous() or workspace.device != dev):
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
     if launch_events is not None and len(launch_events) != 6:
         raise ValueError("launch_events needs 6 events (start and stop of 3 launches)")
-    with torch.cuda.device(dev):
-        if p.dev is None or p.dev.device != dev:
-            p.to(dev)
-        if out is None:
-            out = _new((T, Hq, D), torch.bfloat16, dev, s)
-        if lse is None and want_lse:
-            lse = _new((T, Hq), torch.float32, dev, s)
-        if workspace is None and p.workspace_bytes > 0:
-            workspace = _new((p.workspace_bytes,), torch.uint8, dev, s)
-        p.order_after_upload(s)
-        evs = None if launch_events is None else (ctypes.c_void_p * 6)(*[e.cuda_event for e in launch_events])
-        check(lib.sangam_kvq_forward(p.host_ptr(), p.dev.data_ptr(), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
-                                     ctypes.byref(cache.c_cache()), page_ids.data_ptr(), int(page_ids.numel()), out.data_ptr(),
-                                     lse.data_ptr() if lse is not None else None,
-                                     workspace.data_ptr() if workspace is not None else None,
-                                     workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                     s.cuda_stream, evs))
+    if p.dev is None or p.dev.device != dev:
+        p.to(dev)
+    if out is None:
+        out = _new((T, Hq, D), torch.bfloat16, dev, stream)
+    if lse is None and want_lse:
+        lse = _new((T, Hq), torch.float32, dev, stream)
+    if workspace is None and p.workspace_bytes > 0:
+        workspace = _new((p.workspace_bytes,), torch.uint8, dev, stream)
+    if p.upload_done is not None and p.upload_stream.cuda_stream != s:
+        p.order_after_upload(stream if stream is not None else torch.cuda.current_stream(dev))
+    evs = None if launch_events is None else (ctypes.c_void_p * 6)(*[e.cuda_event for e in launch_events])
+    _launch(dev, lib.sangam_kvq_forward, p.host_ptr(), p.dev.data_ptr(), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+            ctypes.byref(cache.c_cache()), page_ids.data_ptr(), num_page_ids, out.data_ptr(),
+            lse.data_ptr() if lse is not None else None, workspace.data_ptr() if workspace is not None else None,
+            workspace.numel() * workspace.element_size() if workspace is not None else 0, s, evs)
     return out, lse
 
 
@@ -141,12 +158,11 @@ def _check_cache(cache: QuantCache, hkv: int, d: int, pages: int, dev) -> None:
         raise ValueError(f"the plan addresses {pages} pool pages, the cache holds {cache.num_pool_pages}")
 
 
-def _copy(fn, p: kv.KvPlan, cache: QuantCache, stream, args) -> None:
-    dev = cache.k.device
-    with torch.cuda.device(dev):
-        if p.dev is None or p.dev.device != dev:
-            p.to(dev)
-        check(fn(p.host_ptr(), p.dev.data_ptr(), *args, stream.cuda_stream))
+def _packed(p: kv.KvPlan, t: torch.Tensor, name: str, dev) -> None:
+    """kv._check_packed's check; its words where it fails."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.device == dev and t.is_contiguous() and
+            t.shape == (p.rows, p.num_kv_heads, p.head_dim)):
+        kv._check_packed(p, t, name, dev)
 
 
 def kv_export(p: kv.KvPlan, cache: QuantCache, k_packed: Optional[torch.Tensor] = None,
@@ -159,10 +175,16 @@ def kv_export(p: kv.KvPlan, cache: QuantCache, k_packed: Optional[torch.Tensor] 
     s = _stream(dev, stream)
     _check_cache(cache, p.num_kv_heads, p.head_dim, p.num_pool_pages, dev)
     shape = (p.rows, p.num_kv_heads, p.head_dim)
-    k_packed, v_packed = (_new(shape, torch.bfloat16, dev, s) if t is None else t for t in (k_packed, v_packed))
-    kv._check_packed(p, k_packed, "k_packed", dev)
-    kv._check_packed(p, v_packed, "v_packed", dev)
-    _copy(lib.sangam_kvq_export, p, cache, s, (ctypes.byref(cache.c_cache()), k_packed.data_ptr(), v_packed.data_ptr()))
+    if k_packed is None:
+        k_packed = _new(shape, torch.bfloat16, dev, stream)
+    if v_packed is None:
+        v_packed = _new(shape, torch.bfloat16, dev, stream)
+    _packed(p, k_packed, "k_packed", dev)
+    _packed(p, v_packed, "v_packed", dev)
+    if p.dev is None or p.dev.device != dev:
+        p.to(dev)
+    _launch(dev, lib.sangam_kvq_export, p.host_ptr(), p.dev.data_ptr(), ctypes.byref(cache.c_cache()), k_packed.data_ptr(),
+            v_packed.data_ptr(), s)
     return k_packed, v_packed
 
 
@@ -173,6 +195,9 @@ def kv_import(p: kv.KvPlan, k_packed: torch.Tensor, v_packed: torch.Tensor, cach
     dev = cache.k.device
     s = _stream(dev, stream)
     _check_cache(cache, p.num_kv_heads, p.head_dim, p.num_pool_pages, dev)
-    kv._check_packed(p, k_packed, "k_packed", dev)
-    kv._check_packed(p, v_packed, "v_packed", dev)
-    _copy(lib.sangam_kvq_import, p, cache, s, (k_packed.data_ptr(), v_packed.data_ptr(), ctypes.byref(cache.c_cache())))
+    _packed(p, k_packed, "k_packed", dev)
+    _packed(p, v_packed, "v_packed", dev)
+    if p.dev is None or p.dev.device != dev:
+        p.to(dev)
+    _launch(dev, lib.sangam_kvq_import, p.host_ptr(), p.dev.data_ptr(), k_packed.data_ptr(), v_packed.data_ptr(),
+            ctypes.byref(cache.c_cache()), s)

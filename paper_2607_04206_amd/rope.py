@@ -12,7 +12,7 @@ import torch
 
 from . import _lib
 from ._lib import RopeDesc, RopeTensor, check, lib
-from .kvq import _new, _stream
+from .kvq import _launch, _new, _stream
 
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
@@ -25,8 +25,11 @@ class RopePlan:
     rot_dim: int
     interleaved: bool
 
+    def __post_init__(self):
+        self._ptr = self.host.ctypes.data
+
     def host_ptr(self) -> int:
-        return self.host.ctypes.data
+        return self._ptr
 
     def to(self, device) -> "RopePlan":
         self.dev = torch.from_numpy(self.host).to(device)
@@ -58,34 +61,22 @@ def plan(*, rot_dim: int, interleaved: bool = False, base: float = 10000.0, scal
     return p
 
 
-def _check(t: torch.Tensor, name: str, rows: int, dtype, head_dim, device) -> None:
+def _expect(t: torch.Tensor, name: str, shape, dtype, dev) -> None:
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype != dtype or t.dtype not in DTYPES:
-        raise TypeError(f"q and k must both be bfloat16, float16 or float32, got {t.dtype} for {name}")
-    if t.dim() != 3 or t.shape[0] != rows or t.shape[1] < 1 or t.shape[2] != head_dim:
-        raise ValueError(f"{name} must be [{rows}, heads, {head_dim}], got {tuple(t.shape)}")
-    if t.stride(2) != 1:
-        raise ValueError(f"the dims of a head of {name} must be consecutive")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype} as q is, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.device != dev:
+        raise ValueError(f"{name} must be on {dev}, got {t.device}")
 
 
-def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
-    """Whether two tensors [rows, heads, D] may share an element (exactly so for
-    views that lie side by side in rows of one buffer)."""
-    size = a.element_size()
-    span = lambda t: sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1  # noqa: E731
-    gap = (b.data_ptr() - a.data_ptr()) // size
-    if gap >= span(a) or -gap >= span(b):
-        return False
-    row = a.stride(0)
-    if a.shape[0] > 1 and row == b.stride(0) and row > 0:
-        wa, wb = span(a[0]), span(b[0])
-        at = gap % row
-        if wa <= row and wb <= row and at >= wa and at + wb <= row:
-            return False
-    return True
+def _tensor(t: torch.Tensor, out: torch.Tensor, name: str, heads: int) -> RopeTensor:
+    (row, head, dim), (out_row, out_head, out_dim) = t.stride(), out.stride()
+    if (dim != 1 or out_dim != 1) and t.shape[2] > 1:
+        raise ValueError(f"the dims of a head of {name} and of its output must be consecutive")
+    return RopeTensor(t.data_ptr(), out.data_ptr(), row, head, out_row, out_head, heads, 0)
 
 
 def rotate(p: RopePlan, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor,
@@ -97,39 +88,34 @@ def rotate(p: RopePlan, q: torch.Tensor, k: Optional[torch.Tensor], positions: t
     int32 [rows] on the device. Allocates the outputs with torch when they are
     not passed; q_out=q and k_out=k rotate in place. transpose gives the
     gradient with respect to q and k from that of the outputs."""
-    if not isinstance(q, torch.Tensor) or q.dim() != 3:
-        raise TypeError("q must be a torch.Tensor of three dimensions")
-    if k is None and k_out is not None:
-        raise ValueError("k_out without k")
-    dev = q.device
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in DTYPES:
+        raise TypeError("q must be a torch.Tensor [rows, heads, D] of bfloat16, float16 or float32")
+    dev, dtype = q.device, q.dtype
     s = _stream(dev, stream)
-    rows, d = int(q.shape[0]), int(q.shape[2])
-    if not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32:
+    rows, heads, d = q.shape
+    if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32:
         raise TypeError("positions must be an int32 tensor")
-    if tuple(positions.shape) != (rows,) or not positions.is_contiguous() or positions.device != dev:
+    if positions.shape != (rows,) or not positions.is_contiguous() or positions.device != dev:
         raise ValueError(f"positions must be a contiguous [{rows}] tensor on {dev}")
-    pairs = [(q, q_out, "q")] + ([(k, k_out, "k")] if k is not None else [])
-    for t, o, name in pairs:
-        _check(t, name, rows, q.dtype, d, dev)
-        if o is not None:
-            _check(o, name + "_out", rows, q.dtype, d, dev)
-            if o.shape[1] != t.shape[1]:
-                raise ValueError(f"{name}_out must have {t.shape[1]} heads, got {o.shape[1]}")
-    if rows:
-        outs = [o for _, o, _ in pairs if o is not None]
-        for o in outs:
-            for t, own, name in pairs:
-                same = o is own and o.data_ptr() == t.data_ptr() and o.stride() == t.stride()
-                if not same and _overlap(o, t):
-                    raise ValueError(f"an output overlaps {name} without being it")
-        if len(outs) == 2 and _overlap(*outs):
-            raise ValueError("q_out and k_out overlap")
-    with torch.cuda.device(dev):
-        if p.dev is None or p.dev.device != dev:
-            p.to(dev)
-        done = [o if o is not None else _new(tuple(t.shape), t.dtype, dev, s) for t, o, _ in pairs]
-        c = [RopeTensor(t.data_ptr(), o.data_ptr(), t.stride(0), t.stride(1), o.stride(0), o.stride(1), int(t.shape[1]), 0)
-             for (t, _, _), o in zip(pairs, done)]
-        check(lib.sangam_rope_rotate(p.host_ptr(), p.dev.data_ptr(), ctypes.byref(c[0]), ctypes.byref(c[1]) if k is not None else None,
-                                     d, DTYPES[q.dtype], positions.data_ptr(), rows, int(bool(transpose)), s.cuda_stream))
-    return done[0], done[1] if k is not None else None
+    if p.dev is None or p.dev.device != dev:
+        p.to(dev)
+    if q_out is None:
+        q_out = _new(q.shape, dtype, dev, stream)
+    else:
+        _expect(q_out, "q_out", q.shape, dtype, dev)
+    c_q, c_k = _tensor(q, q_out, "q", heads), None
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 3:
+            raise TypeError("k must be a torch.Tensor [rows, heads, D]")
+        kv_heads = k.shape[1]
+        _expect(k, "k", (rows, kv_heads, d), dtype, dev)
+        if k_out is None:
+            k_out = _new(k.shape, dtype, dev, stream)
+        else:
+            _expect(k_out, "k_out", k.shape, dtype, dev)
+        c_k = ctypes.byref(_tensor(k, k_out, "k", kv_heads))
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    _launch(dev, lib.sangam_rope_rotate, p.host_ptr(), p.dev.data_ptr(), ctypes.byref(c_q), c_k, d, DTYPES[dtype],
+            positions.data_ptr(), rows, 1 if transpose else 0, s)
+    return q_out, k_out

@@ -124,12 +124,26 @@ def test_no_rows_is_no_launch():
     assert _lib.lib.sangam_rope_rotate(p.host_ptr(), None, ctypes.byref(q), ctypes.byref(q), 64, 0, None, 0, 0, None) == 0
 
 
-def test_overlaps_are_seen():
-    x = torch.zeros(10, 6, 8)
-    assert not rope._overlap(x[:, :2], x[:, 2:4]) and not rope._overlap(x[:, 2:4], x[:, :2]) and not rope._overlap(x[:5], x[5:])
-    assert rope._overlap(x[:, :2], x[:, 1:3]) and rope._overlap(x, x) and rope._overlap(x[:5], x[4:])
-    assert rope._overlap(x[:, 4:6], x[1:, 4:6]) and not rope._overlap(x[:, 4:6], x[1:, :2])
-    assert rope._overlap(x, x.transpose(0, 1)) and not rope._overlap(x, torch.zeros(10, 6, 8))
+def _refused(q_in, q_out, k_in=None, k_out=None):
+    """Whether the C entry refuses tensors for their overlaps (of host tensors:
+    what passes the checks fails for the missing plan_dev, in another way)."""
+    p = rope.plan(rot_dim=8)
+    c = [_lib.RopeTensor(i.data_ptr(), o.data_ptr(), i.stride(0), i.stride(1), o.stride(0), o.stride(1), i.shape[1], 0)
+         for i, o in ((q_in, q_out), (k_in, k_out)) if i is not None]
+    st = _lib.lib.sangam_rope_rotate(p.host_ptr(), None, ctypes.byref(c[0]), ctypes.byref(c[1]) if len(c) > 1 else None, 8, 2, 4096,
+                                     q_in.shape[0], 0, None)
+    assert st == -1
+    return b"overlap" in _lib.lib.sangam_last_error()
+
+
+def test_overlaps_are_refused():
+    x, y = torch.zeros(10, 6, 8), torch.zeros(10, 6, 8)
+    assert not _refused(x, x) and not _refused(x, y) and not _refused(x[:, :2], x[:, 2:4]) and not _refused(x[:, 2:4], x[:, :2])
+    assert not _refused(x[:5], x[5:]) and not _refused(x[:, :3], x[:, :3], x[:, 3:], x[:, 3:])
+    assert _refused(x[:, :2], x[:, 1:3]) and _refused(x[:5], x[4:9]) and _refused(x[:9], x[1:]) and _refused(x[1:], x[:9])
+    assert _refused(x[:9, 4:6], x[1:, 4:6]) and not _refused(x[:9, 4:6], x[1:, :2])
+    assert _refused(x[:, :2], y[:, :2], x[:, 2:3], y[:, 1:2]) and _refused(x[:, :2], y[:, :2], x[:, 2:3], x[:, :1])
+    assert _refused(x.transpose(0, 1).contiguous().transpose(0, 1), x[:, :6], x, x) and not _refused(x[:1], y[:1], x[1:2], y[1:2])
 
 
 # ------------------------------------------------------------------------ GPU
@@ -291,8 +305,8 @@ def test_python_refusals(dev):
                        (ValueError, (q, k, pos[:9]), {}), (ValueError, (q[:9], k, pos), {}), (ValueError, (q, k, pos.cpu()), {}),
                        (ValueError, (q, k[..., :32], pos), {}), (ValueError, (q.transpose(1, 2).contiguous().transpose(1, 2), k, pos), {}),
                        (ValueError, (q, k, pos), dict(q_out=k)), (ValueError, (q, k, pos), dict(q_out=q[:9])), (ValueError, (q, None, pos), dict(k_out=k)),
-                       (ValueError, (fused[:, :4], fused[:, 4:6], pos), dict(q_out=fused[:, 2:6])),
-                       (ValueError, (q, k, pos), dict(q_out=fused[:, :4], k_out=fused[:, 3:5])), (TypeError, (None, k, pos), {}),
+                       (_lib.SangamError, (fused[:, :4], fused[:, 4:6], pos), dict(q_out=fused[:, 2:6])), (TypeError, (q, k[0], pos), {}),
+                       (_lib.SangamError, (q, k, pos), dict(q_out=fused[:, :4], k_out=fused[:, 3:5])), (TypeError, (None, k, pos), {}),
                        (ValueError, (q.cpu(), k.cpu(), pos.cpu()), {})):
         with pytest.raises(err):
             rope.rotate(p, *a, **kw)
