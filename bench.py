@@ -181,7 +181,7 @@ def cpu_baseline(wl, budget_s, single_thread=True):
 def kernel_source_hash():
     import hashlib
     h = hashlib.sha256()
-    for f in ("attn_fwd.hip", "mixed_order.h", "plan.cpp", "plan_format.h"):
+    for f in ("attn_fwd.hip", "attn_tile.h", "attn_forward.h", "mixed_order.h", "plan.cpp", "plan_format.h"):
         with open(os.path.join(ROOT, "paper_2607_04206_amd", "csrc", f), "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()[:16]
@@ -284,7 +284,8 @@ def serve_trace(args):
 
     dev = torch.device("cuda:0")
     reqs = workloads.serving_trace(args.seed, args.trace_iters, args.trace_rate)
-    loop = ServingLoop(reqs, hq=28, hkv=4, d=128, tau=args.tau, device=dev, seed=args.seed)
+    loop = ServingLoop(reqs, hq=28, hkv=4, d=128, tau=args.tau, device=dev, seed=args.seed,
+                       kv_format=args.kv_format, rotary={} if args.rotary else None)
     log = loop.run(args.trace_iters * 8)
     torch.cuda.synchronize()
     ms = np.asarray([r.events[0].elapsed_time(r.events[1]) for r in log])
@@ -314,6 +315,10 @@ def serve_trace(args):
         "prefill_wait_iterations_p99": pct(waits, 99),
         "plan_ms_mean": float(np.mean([r.plan_ms for r in log])),
     }
+    if args.kv_format:
+        res["kv_format"] = args.kv_format
+    if args.rotary:
+        res["rotary"] = True
     print(json.dumps(res), flush=True)
 
 
@@ -442,6 +447,10 @@ def main():
                     help="instead of one workload: a serving loop over a synthetic request trace, each "
                          "iteration's microbatch composed by the deficit token-budget rule (Dream 28/4 heads)")
     ap.add_argument("--tau", type=int, default=4096, help="token budget per iteration (--serve-trace)")
+    ap.add_argument("--kv-format", choices=("e4m3", "e2m1"), default=None,
+                    help="quantised KV cache instead of bf16 (--serve-trace)")
+    ap.add_argument("--rotary", action="store_true",
+                    help="rotate q and k at their positions before each call (--serve-trace)")
     ap.add_argument("--trace-iters", type=int, default=600, help="iterations (--serve-trace)")
     ap.add_argument("--trace-rate", type=float, default=0.3, help="requests per iteration (--serve-trace)")
     ap.add_argument("--kv-transfer", action="store_true",

@@ -31,12 +31,17 @@ constexpr int tile_bytes(int d, int qw, int kw, int nb, int nstage, bool across)
     return stages > sums ? stages : sums;
 }
 
+// Waves per SIMD that the registers leave room for: three at head dim 64, where
+// tiles of two and three heads would spill. 24 decodes beside three prefills of
+// 32/8 heads of 64, with two -> three: e4m3 77.5 -> 70.6 us, e2m1 74.5 -> 67.1.
+constexpr int waves(int d, int qw) { return d == 64 && qw != 2 && qw != 3 ? 3 : 2; }
+
 // deal: 0, or the number of CUs, where all of a launch's tiles, longest first,
 // are on the chip at once, several to a CU: every other round of one per CU is
 // dealt out backwards, so that the CUs with the longest tiles of one get the
 // shortest of the next (32 MHA decodes of up to 1151 keys 51.2 -> 49.1 us).
 template <typename Fmt, int D, int QW, int KW, int QB, int NB, int NSTAGE, bool HEADS_ACROSS>
-__global__ __launch_bounds__(64 * QW * KW, waves_per_simd(QB, false)) void attn_quant_kernel(QuantArgs a, uint32_t deal) {
+__global__ __launch_bounds__(64 * QW * KW, waves(D, QW)) void attn_quant_kernel(QuantArgs a, uint32_t deal) {
     __shared__ TileShared<tile_bytes(D, QW, KW, NB, NSTAGE, HEADS_ACROSS)> shared;
     uint32_t b = blockIdx.x;
     if (QW == 1 && deal > 0) {
@@ -59,7 +64,7 @@ struct MixedQuantArgs {
 };
 
 template <typename Fmt, int D>
-__global__ __launch_bounds__(256, 2) void attn_quant_mixed_kernel(MixedQuantArgs m) {
+__global__ __launch_bounds__(256, waves(D, 4)) void attn_quant_mixed_kernel(MixedQuantArgs m) {
     constexpr int KW = D == 128 ? 4 : 2;
     constexpr int PREFILL = tile_bytes(D, 4, 1, 2, 2, false), DECODE = tile_bytes(D, 1, KW, 1, 1, true);
     __shared__ TileShared<(PREFILL > DECODE ? PREFILL : DECODE)> shared;

@@ -1050,8 +1050,9 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
             // The next stage's values are converted beside the last steps of
             // QK^T, where a CU holds two work-groups and a wave has one page:
             // 64 decodes of 32/8 heads of 128 e4m3 93.0 -> 89.9 us, e2m1 84.8 ->
-            // 80.5. (Seven and eight waves, one work-group to a CU, lose 1 %.)
-            if constexpr (!decltype(tail)::value && NSTAGE == 2 && PW == 1 && QW == 4) {
+            // 80.5. (Seven and eight waves, one work-group to a CU, lose 1 %; head
+            // dim 64 has no registers for it.)
+            if constexpr (!decltype(tail)::value && NSTAGE == 2 && PW == 1 && QW == 4 && D == 128) {
                 if (head_ok && more && (st + 1 < mixed0 || (st + 1 >= mixed1 && st + 1 < full_stages))) {
                     attend(st, tail, go_on, [&](int n) __attribute__((always_inline)) {
                         constexpr int NK = NB * DS, PER = (PIECES + NK - 1) / NK, FIRST = NK - (PIECES + PER - 1) / PER;

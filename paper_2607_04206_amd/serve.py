@@ -4,7 +4,8 @@ decodes of one 32-token block until it is resolved, then a re-prefill that
 refreshes the cache at the block boundary; Sec. 2.2, Sec. 4.3), each
 iteration's microbatch is composed by the deficit token-budget rule
 (Sec. 4.1, Alg. 1) and served by one sangam_attn_forward call over a paged KV
-pool (Sec. 5).
+pool (Sec. 5), or by one sangam_kvq_forward call over a quantised pool. With
+rotary positions, q and k are rotated at their rows' positions before it.
 
 Only one attention layer is run per iteration (the model around it is out of
 scope), with synthetic Q / K / V values: the loop exercises batch composition,
@@ -18,7 +19,7 @@ from typing import List, Optional
 import numpy as np
 import torch
 
-from . import attn, sched
+from . import attn, kv, kvq, rope, sched
 
 BLOCK = 32
 PAGE = 16
@@ -77,16 +78,25 @@ class Iteration:
 
 
 class ServingLoop:
-    """Drive a list of trace requests through iterations of one GPU."""
+    """Drive a list of trace requests through iterations of one GPU.
+
+    kv_format: None for a bf16 cache, or a format of kvq.FORMATS.
+    rotary: None, or the arguments of rope.plan (rot_dim is the head dim unless
+    they say otherwise)."""
 
     def __init__(self, requests, *, hq: int, hkv: int, d: int, tau: int, device,
-                 num_pool_pages: Optional[int] = None, max_rows: int = 1 << 15, seed: int = 0):
+                 num_pool_pages: Optional[int] = None, max_rows: int = 1 << 15, seed: int = 0,
+                 kv_format: Optional[str] = None, rotary: Optional[dict] = None):
+        if kv_format is not None and kv_format not in kvq.FORMATS:
+            raise ValueError(f"kv_format must be None or one of {sorted(kvq.FORMATS)}, got {kv_format!r}")
         self.reqs = [_State(r) for r in sorted(requests, key=lambda r: (r.arrival, r.rid))]
         self.hq, self.hkv, self.d, self.tau = hq, hkv, d, tau
         self.dev = device
         need = sum(-(-(s.L) // PAGE) for s in self.reqs)
         self.pool = PagePool(num_pool_pages if num_pool_pages is not None else max(need, 1))
         self.max_rows = max_rows
+        self.rope = None if rotary is None else rope.plan(**{"rot_dim": d, **rotary}, device=device)
+        self.cache = None  # the quantised pool
         if device is not None:  # device None: plan every batch but run nothing (host checks)
             g = torch.Generator(device="cpu").manual_seed(seed)
             shape = (self.pool.num_pages, hkv, PAGE, d)
@@ -95,12 +105,36 @@ class ServingLoop:
             self.q = torch.randn((max_rows, hq, d), generator=g).to(torch.bfloat16).to(device)
             self.k_new = torch.randn((max_rows, hkv, d), generator=g).to(torch.bfloat16).to(device)
             self.v_new = torch.randn((max_rows, hkv, d), generator=g).to(torch.bfloat16).to(device)
+            if kv_format is not None:
+                self._quantise_pool(kv_format)
+            if self.rope is not None:
+                self.q_rot, self.k_rot = torch.empty_like(self.q), torch.empty_like(self.k_new)
             self.out = torch.empty((max_rows, hq, d), dtype=torch.bfloat16, device=device)
             self.lse = torch.empty((max_rows, hq), dtype=torch.float32, device=device)
         self.deficit = 0
         self.next_arrival = 0
         self.waiting: List[_State] = []  # arrival order of the requests (re-prefills keep their place)
         self.sm_scale = float(np.float32(1.0 / np.sqrt(d)))
+
+    def _page_rows(self, page_ids: np.ndarray) -> kv.KvPlan:
+        """A plan of all rows of some pages."""
+        n = len(page_ids)
+        return kv.plan(kv_len=[PAGE * n], page_indptr=[0, n], page_ids=page_ids, num_kv_heads=self.hkv, head_dim=self.d,
+                       num_pool_pages=self.pool.num_pages, device=self.dev)
+
+    def _quantise_pool(self, kv_format: str) -> None:
+        """The bf16 pool's content in quantised pages, in its place."""
+        p = self._page_rows(np.arange(self.pool.num_pages, dtype=np.int32))
+        self.cache = kvq.empty_cache(self.pool.num_pages, self.hkv, self.d, format=kv_format, device=self.dev)
+        kvq.kv_import(p, *kv.kv_export(p, self.k_cache, self.v_cache), self.cache)
+        self.k_cache = self.v_cache = None
+
+    def _pages(self, page_ids: np.ndarray, pid: torch.Tensor):
+        """Copies of some pages' K and V, bf16 [pages, Hkv, 16, D]."""
+        if self.cache is None:
+            return self.k_cache[pid.long()].clone(), self.v_cache[pid.long()].clone()
+        rows = kvq.kv_export(self._page_rows(page_ids), self.cache)
+        return tuple(x.view(-1, PAGE, self.hkv, self.d).transpose(1, 2).contiguous() for x in rows)
 
     def _arrive(self, t: int) -> None:
         while self.next_arrival < len(self.reqs) and self.reqs[self.next_arrival].req.arrival <= t:
@@ -151,6 +185,7 @@ class ServingLoop:
             timed = capture = False
         else:
             self._nd = nd
+            self._positions = np.concatenate([np.arange(a, a + b, dtype=np.int32) for a, b in zip(o, n)]) if self.rope else None
             self._desc = (q_indptr, np.asarray(o, np.int32), kv_len, page_indptr)
             self._run(p, page_ids, rows, timed, capture)
         rec = Iteration(t=t, decodes=len(decodes), prefills=len(admitted),
@@ -168,14 +203,16 @@ class ServingLoop:
         stream = torch.cuda.current_stream(self.dev)
         snap = None
         nd = self._nd
+        q, k_new, v_new = self.q[:rows], self.k_new[:rows], self.v_new[:rows]
+        if self.rope is not None:
+            positions = torch.from_numpy(self._positions).to(self.dev, non_blocking=True)
+            q, k_new = rope.rotate(self.rope, q, k_new, positions, q_out=self.q_rot[:rows], k_out=self.k_rot[:rows])
         if capture:
             q_indptr, q_offset, kv_len, page_indptr = self._desc
             snap = dict(q_indptr=q_indptr, q_offset=q_offset, kv_len=kv_len,
                         page_indptr=page_indptr, page_ids=page_ids, sm_scale=self.sm_scale,
-                        q=self.q[:rows].clone(), k_new=self.k_new[:rows].clone(),
-                        v_new=self.v_new[:rows].clone(),
-                        k_pages=self.k_cache[pid.long()].clone(), v_pages=self.v_cache[pid.long()].clone(),
-                        decodes=nd)
+                        q=q.clone(), k_new=k_new.clone(), v_new=v_new.clone(), decodes=nd)
+            snap["k_pages"], snap["v_pages"] = self._pages(page_ids, pid)
         ev = lev = used = None
         if timed:
             ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True))
@@ -184,8 +221,12 @@ class ServingLoop:
                 e.record(stream)
             used = p.launches()
             ev[0].record(stream)
-        attn.forward(p, self.q[:rows], self.k_new[:rows], self.v_new[:rows], self.k_cache, self.v_cache,
-                     pid, out=self.out[:rows], lse=self.lse[:rows], launch_events=lev)
+        if self.cache is None:
+            attn.forward(p, q, k_new, v_new, self.k_cache, self.v_cache, pid, out=self.out[:rows],
+                         lse=self.lse[:rows], launch_events=lev)
+        else:
+            kvq.forward(p, q, k_new, v_new, self.cache, pid, out=self.out[:rows], lse=self.lse[:rows],
+                        launch_events=lev)
         if timed:
             ev[1].record(stream)
             lev = [(lev[2 * k], lev[2 * k + 1]) for k in range(3) if used[k]]
