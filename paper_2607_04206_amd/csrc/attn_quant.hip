@@ -40,8 +40,8 @@ constexpr int waves(int d, int qw) { return d == 64 && qw != 2 && qw != 3 ? 3 : 
 // are on the chip at once, several to a CU: every other round of one per CU is
 // dealt out backwards, so that the CUs with the longest tiles of one get the
 // shortest of the next (32 MHA decodes of up to 1151 keys 51.2 -> 49.1 us).
-template <typename Fmt, int D, int QW, int KW, int QB, int NB, int NSTAGE, bool HEADS_ACROSS>
-__global__ __launch_bounds__(64 * QW * KW, waves(D, QW)) void attn_quant_kernel(QuantArgs a, uint32_t deal) {
+template <typename Fmt, int D, int QW, int KW, int QB, int NB, int NSTAGE, bool HEADS_ACROSS, int HELP>
+__global__ __launch_bounds__(64 * (QW * KW + HELP), waves(D, QW)) void attn_quant_kernel(QuantArgs a, uint32_t deal) {
     __shared__ TileShared<tile_bytes(D, QW, KW, NB, NSTAGE, HEADS_ACROSS)> shared;
     uint32_t b = blockIdx.x;
     if (QW == 1 && deal > 0) {
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * QW * KW, waves(D, QW)) void attn_quant_kernel(
         if ((round & 1) && (round + 1) * deal <= gridDim.x) b = (2 * round + 1) * deal - 1 - b;
     }
     const TileRec t = a.tiles[b];
-    attn_tile<D, QW, KW, QB, NB, NSTAGE, HEADS_ACROSS, 0, QuantCache<Fmt>>(a, t, a.items[t.item], shared);
+    attn_tile<D, QW, KW, QB, NB, NSTAGE, HEADS_ACROSS, HELP, QuantCache<Fmt>>(a, t, a.items[t.item], shared);
 }
 
 // Prefill-shaped tiles and MHA block decodes in one launch, as
@@ -94,11 +94,11 @@ struct QuantKernels {
         return a;
     }
 
-    template <int D, int QW, int KW, int QB, int NB, bool HA, int NSTAGE = 2>
+    template <int D, int QW, int KW, int QB, int NB, bool HA, int NSTAGE = 2, int HELP = 0>
     static hipError_t tiles(const Args& args, int n_tiles, hipStream_t stream, LaunchEvents ev, uint32_t deal = 0) {
         void* kargs[] = {const_cast<Args*>(&args), &deal};
-        return launch_args(reinterpret_cast<const void*>(&attn_quant_kernel<Fmt, D, QW, KW, QB, NB, NSTAGE, HA>),
-                           dim3(unsigned(n_tiles)), unsigned(64 * QW * KW), kargs, stream, ev);
+        return launch_args(reinterpret_cast<const void*>(&attn_quant_kernel<Fmt, D, QW, KW, QB, NB, NSTAGE, HA, HELP>),
+                           dim3(unsigned(n_tiles)), unsigned(64 * (QW * KW + HELP)), kargs, stream, ev);
     }
 
     hipError_t mixed(const PlanHeader& h, const Args& args, const TileRec* decodes, const MixedOrder& order,
@@ -129,11 +129,18 @@ struct QuantKernels {
         if (h.decode_qw == 1 && kw == 2 && nb == 1) return tiles<D, 1, 2, 1, 1, true>(args, n, stream, ev, n <= 4 * cus ? cus : 0);
         if (h.decode_qw == 2 && kw == 2 && nb == 2) return tiles<D, 2, 2, 1, 2, true, 1>(args, n, stream, ev);
         if (kw == 1 && nb == 2) {
+            // Two or three waves more, which only stage, where five or six heads
+            // leave that many places of a CU's eight: 64 decodes of 20/4 heads
+            // e4m3 67.5 -> 61.0 us, e2m1 67.4 -> 59.7, of 24/4 68.5 -> 67.3 and 68.7
+            // -> 63.5. One more cannot keep up with seven heads (48 decodes of
+            // 28/4 44.8 -> 49.8 us) or three (73.4 -> 83.3). At head dim 64 a CU
+            // holds more work-groups instead.
+            constexpr bool H = D == 128;
             switch (h.decode_qw) {
                 case 3: return tiles<D, 3, 1, 1, 2, true>(args, n, stream, ev);
                 case 4: return tiles<D, 4, 1, 1, 2, true>(args, n, stream, ev);
-                case 5: return tiles<D, 5, 1, 1, 2, true>(args, n, stream, ev);
-                case 6: return tiles<D, 6, 1, 1, 2, true>(args, n, stream, ev);
+                case 5: return tiles<D, 5, 1, 1, 2, true, 2, H ? 3 : 0>(args, n, stream, ev);
+                case 6: return tiles<D, 6, 1, 1, 2, true, 2, H ? 2 : 0>(args, n, stream, ev);
                 case 7: return tiles<D, 7, 1, 1, 2, true>(args, n, stream, ev);
                 case 8: return tiles<D, 8, 1, 1, 2, true>(args, n, stream, ev);
                 default: break;

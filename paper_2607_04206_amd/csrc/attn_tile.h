@@ -430,21 +430,25 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
     // page, or at head dim 64, where a page has half as many, of K's in the
     // lower half-wave and of V's in the upper one. A lane of a page with fresh
     // rows takes those from k_new / v_new in place(), as they are.
+    // Where there are HELP waves, they do all of it.
+    constexpr int SW = HELP > 0 ? HELP : NW;           // staging waves
+    constexpr int PWQ = (SP + SW - 1) / SW;            // pages of one per stage
+    const int swave = HELP > 0 ? wave - QW * KW : wave;
     constexpr int BPR = D / kMxBlock;
     constexpr int TPL = BPR / 2;  // tensors of a page that a lane has a block of
     const int ublock = lane % (16 * BPR);
     const int urow = ublock / BPR;
-    typename Cache::Block raw[PW][TPL];
-    uint32_t fresh_info[PW];  // page_info of the pages
+    typename Cache::Block raw[PWQ][TPL];
+    uint32_t fresh_info[PWQ];  // page_info of the pages
     auto fetch = [&](int st) __attribute__((always_inline)) {
         if constexpr (QUANT) {
             if (all_fresh) return;
             const bool whole = st < mixed0 || (st >= mixed1 && st < full_stages);
             const int pl0 = st * SP & 63;
 #pragma unroll
-            for (int i = 0; i < PW; ++i) {
-                const int k = wave + i * NW;  // page of the stage
-                if (SP % NW != 0 && k >= SP) break;
+            for (int i = 0; i < PWQ; ++i) {
+                const int k = swave + i * SW;  // page of the stage
+                if (SP % SW != 0 && k >= SP) break;
                 int pl = pl0 + k, row = urow;
                 if (!whole) {  // a page past the range: the stage's first page again, rows past its end: its last row
                     int key0 = kv_begin + st * STEP;
@@ -467,9 +471,9 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
         if constexpr (QUANT) {
             const bool whole = st < mixed0 || (st >= mixed1 && st < full_stages);
 #pragma unroll
-            for (int i = 0; i < PW; ++i) {
-                const int k = wave + i * NW;
-                if (SP % NW != 0 && k >= SP) break;
+            for (int i = 0; i < PWQ; ++i) {
+                const int k = swave + i * SW;
+                if (SP % SW != 0 && k >= SP) break;
                 uint8_t* const tile = smem + buf * 2 * TILE + (k * 16 + urow) * ROWB;
                 int64_t fresh_row = -1;  // row of k_new / v_new, -1: a cached row
                 if (!whole) {
@@ -505,12 +509,12 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
 
     // place() of a stage without fresh rows, in PIECES of 8 dims of a lane's
     // blocks each, for the steps of the stage before
-    constexpr int PIECES = PW * TPL * 4;
+    constexpr int PIECES = PWQ * TPL * 4;
     auto place_piece = [&](int buf, int n) __attribute__((always_inline)) {
         if constexpr (QUANT) {
             const int i = n / (TPL * 4), j = n / 4 % TPL, e = n % 4;
-            const int k = wave + i * NW;
-            if (SP % NW != 0 && k >= SP) return;
+            const int k = swave + i * SW;
+            if (SP % SW != 0 && k >= SP) return;
             const bool v = TPL == 2 ? j != 0 : hh != 0;
             *(LDS u32x4*)(smem + buf * 2 * TILE + (v ? TILE : 0) + (k * 16 + urow) * ROWB +
                           ((((ublock % BPR) * 4 + e) ^ (v ? swz_v<D>(urow) : swz_k<D>(urow))) << 4)) = raw[i][j].piece(e);
@@ -801,7 +805,7 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
     if constexpr (SOLO) {
         // begins below
     } else if constexpr (QUANT) {
-        if (NB != 4) {
+        if (NB != 4 && HELP == 0) {
             fetch(0);
             next_pages(0);
         }
@@ -1019,6 +1023,7 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
         // (The wide tiles have no registers for that: long prefills, which
         // read no cached rows. A long block over a cached context waits.)
         static_assert(NSTAGE <= 2, "the next stage waits in registers");
+        static_assert(HELP == 0 || NSTAGE == 2, "helpers place the next stage beside the others' work");
         constexpr bool LATE = NB == 4;
         auto go_on = []() {};
         auto bring = [&](int s) {  // into LDS
@@ -1052,7 +1057,7 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
             // 64 decodes of 32/8 heads of 128 e4m3 93.0 -> 89.9 us, e2m1 84.8 ->
             // 80.5. (Seven and eight waves, one work-group to a CU, lose 1 %; head
             // dim 64 has no registers for it.)
-            if constexpr (!decltype(tail)::value && NSTAGE == 2 && PW == 1 && QW == 4 && D == 128) {
+            if constexpr (!decltype(tail)::value && NSTAGE == 2 && PWQ == 1 && QW == 4 && D == 128) {
                 if (head_ok && more && (st + 1 < mixed0 || (st + 1 >= mixed1 && st + 1 < full_stages))) {
                     attend(st, tail, go_on, [&](int n) __attribute__((always_inline)) {
                         constexpr int NK = NB * DS, PER = (PIECES + NK - 1) / NK, FIRST = NK - (PIECES + PER - 1) / PER;
@@ -1069,12 +1074,49 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
                 ahead(st + 2);
             }
         };
-        if (NSTAGE == 2) {
-            bring(0);
-            if (!all_fresh) ahead(1);
+        if constexpr (HELP > 0) {
+            // The helpers take the waves' places on the SIMDs that have one
+            // fewer, and the others no time off for the staging. (Two loops:
+            // neither's registers are the other's.)
+            auto begin = [&]() __attribute__((always_inline)) {  // a stage, after the barrier
+                if (all_fresh) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                if (all_fresh && st + 1 < nstages) issue_stage(st + 1, (st + 1) % NSTAGE, yes, yes);
+                if (st >= wst0 && st < wst1) write_back(st, yes, yes);
+            };
+            if (all_fresh) issue_stage(0, 0, yes, yes);
+            if (computes) {
+                for (; st < full_stages; ++st) {
+                    begin();
+                    if (head_ok) attend(st, std::false_type{}, go_on, nothing);
+                }
+                if (st < nstages) {
+                    begin();
+                    if (head_ok) attend(st, std::true_type{}, go_on, nothing);
+                }
+            } else {
+                if (!all_fresh) {
+                    fetch(0);
+                    next_pages(0);
+                    place(0, 0);
+                    ahead(1);
+                }
+                for (; st < nstages; ++st) {
+                    begin();
+                    if (!all_fresh && st + 1 < nstages) {
+                        place(st + 1, (st + 1) % NSTAGE);
+                        ahead(st + 2);
+                    }
+                }
+            }
+        } else {
+            if (NSTAGE == 2) {
+                bring(0);
+                if (!all_fresh) ahead(1);
+            }
+            for (; st < full_stages; ++st) stage(std::false_type{});
+            if (st < nstages) stage(std::true_type{});
         }
-        for (; st < full_stages; ++st) stage(std::false_type{});
-        if (st < nstages) stage(std::true_type{});
     } else if constexpr (TURNS) {
         // a stage: its K is there, V on its way under QK^T, the next K under PV
         auto stage = [&](auto tail) __attribute__((always_inline)) {
