@@ -76,7 +76,7 @@ typedef struct sangam_rope_tensor {
     int64_t in_head_stride;  /* >= 0 */
     int64_t out_row_stride;  /* no two (row, head) of out may overlap */
     int64_t out_head_stride;
-    int32_t heads;           /* >= 1 */
+    int32_t heads;           /* 1 to 65536 */
     int32_t reserved;        /* 0 */
 } sangam_rope_tensor;
 

@@ -15,6 +15,7 @@
 #include "../../include/sangam_kvq.h"
 #include "attn_forward.h"
 #include "attn_tile.h"
+#include "entry.h"
 #include "mixed_order.h"
 #include "plan_format.h"
 
@@ -180,19 +181,21 @@ extern "C" sangam_status sangam_kvq_forward(const void* plan_host, const void* p
                                             const void* v_new, const sangam_kvq_cache* cache, const int32_t* page_ids_dev,
                                             int64_t num_page_ids, void* out, float* lse, void* workspace,
                                             size_t workspace_bytes, void* stream, void* const* events) {
-    clear_error();
-    if (!cache || !cache->k_scale || !cache->v_scale) {
-        set_error("the cache and its scales must not be NULL");
-        return SANGAM_ERR_INVALID_ARG;
-    }
-    if (!aligned16(cache->k_scale) || !aligned16(cache->v_scale)) {
-        set_error("the cache's scales must be 16-byte aligned");
-        return SANGAM_ERR_ALIGN;
-    }
-    const ForwardTensors c{plan_host, plan_dev, q, k_new, v_new, cache->k, cache->v, cache->pool_pages, page_ids_dev,
-                           num_page_ids, out, lse, workspace, workspace_bytes, stream, events};
-    if (cache->format == SANGAM_KV_E4M3) return run_quant<MxE4m3>(*cache, c);
-    if (cache->format == SANGAM_KV_E2M1) return run_quant<MxE2m1>(*cache, c);
-    set_error("cache format must be SANGAM_KV_E4M3 or SANGAM_KV_E2M1");
-    return SANGAM_ERR_UNSUPPORTED;
+    return entry([&]() -> sangam_status {
+        clear_error();
+        if (!cache || !cache->k_scale || !cache->v_scale) {
+            set_error("the cache and its scales must not be NULL");
+            return SANGAM_ERR_INVALID_ARG;
+        }
+        if (!aligned16(cache->k_scale) || !aligned16(cache->v_scale)) {
+            set_error("the cache's scales must be 16-byte aligned");
+            return SANGAM_ERR_ALIGN;
+        }
+        const ForwardTensors c{plan_host, plan_dev, q, k_new, v_new, cache->k, cache->v, cache->pool_pages, page_ids_dev,
+                               num_page_ids, out, lse, workspace, workspace_bytes, stream, events};
+        if (cache->format == SANGAM_KV_E4M3) return run_quant<MxE4m3>(*cache, c);
+        if (cache->format == SANGAM_KV_E2M1) return run_quant<MxE2m1>(*cache, c);
+        set_error("cache format must be SANGAM_KV_E4M3 or SANGAM_KV_E2M1");
+        return SANGAM_ERR_UNSUPPORTED;
+    });
 }

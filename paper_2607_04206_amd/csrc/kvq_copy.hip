@@ -17,6 +17,7 @@
 #include <string>
 
 #include "../../include/sangam_kvq.h"
+#include "entry.h"
 #include "kv_format.h"
 #include "mx_format.h"
 
@@ -160,10 +161,10 @@ sangam_status run_copy(bool is_export, const void* plan_host, const void* plan_d
 
 extern "C" sangam_status sangam_kvq_export(const void* plan_host, const void* plan_dev, const sangam_kvq_cache* cache,
                                            void* k_packed, void* v_packed, void* stream) {
-    return run_copy(true, plan_host, plan_dev, cache, k_packed, v_packed, stream);
+    return entry([&] { return run_copy(true, plan_host, plan_dev, cache, k_packed, v_packed, stream); });
 }
 
 extern "C" sangam_status sangam_kvq_import(const void* plan_host, const void* plan_dev, const void* k_packed,
                                            const void* v_packed, const sangam_kvq_cache* cache, void* stream) {
-    return run_copy(false, plan_host, plan_dev, cache, k_packed, v_packed, stream);
+    return entry([&] { return run_copy(false, plan_host, plan_dev, cache, k_packed, v_packed, stream); });
 }

@@ -3,20 +3,19 @@
 //
 // Every element is read once and written once, and a pair needs one sine and
 // one cosine, the same for all heads of a row: the kernel is bound by HBM as
-// long as those are computed once per row and not per head (computed by each
-// thread for its own 8 pairs they would take as long as the memory does). A
+// long as those are computed once per row and not per head (some 40 instructions
+// each, for a thread's own 8 pairs as many as the memory leaves time for). A
 // work-group holds some rows and some heads: it computes the rows' angles into
 // LDS (64-bit product, turns reduced to an eighth there, then fp32), and its
 // threads rotate units of 16 bytes on either side of a pair (halves) or of
 // 16 bytes of pairs (interleaved).
-#include <hip/hip_bf16.h>
-#include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <string>
 
 #include "../../include/sangam_rope.h"
+#include "entry.h"
 #include "rope_format.h"
 
 namespace sangam {
@@ -216,11 +215,8 @@ bool may_overlap(const View& a, const View& b, int64_t rows, int64_t d, int64_t 
 
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
-}  // namespace
-
-extern "C" sangam_status sangam_rope_rotate(const void* plan_host, const void* plan_dev, const sangam_rope_tensor* q,
-                                            const sangam_rope_tensor* k, int32_t head_dim, int32_t dtype,
-                                            const int32_t* positions_dev, int64_t rows, int32_t transpose, void* stream) {
+sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_rope_tensor* q, const sangam_rope_tensor* k,
+                     int32_t head_dim, int32_t dtype, const int32_t* positions_dev, int64_t rows, int32_t transpose, void* stream) {
     clear_error();
     const RopePlanHeader* h = check_rope_plan(plan_host);
     if (!h) return fail(SANGAM_ERR_PLAN, "plan_host is not a rotary plan of this library version");
@@ -240,7 +236,7 @@ extern "C" sangam_status sangam_rope_rotate(const void* plan_host, const void* p
     for (int i = 0; i < 2; ++i) {
         const sangam_rope_tensor* t = i ? k : q;
         if (!t) continue;
-        if (t->heads < 1 || t->heads > (1 << 20)) return fail(SANGAM_ERR_INVALID_ARG, "heads must be 1 to 2^20");
+        if (t->heads < 1 || t->heads > (1 << 16)) return fail(SANGAM_ERR_INVALID_ARG, "heads must be 1 to 2^16");
         heads[i] = t->heads;
         if (rows == 0) continue;
         if (!t->in || !t->out) return fail(SANGAM_ERR_INVALID_ARG, "the tensors must not be NULL");
@@ -314,4 +310,12 @@ extern "C" sangam_status sangam_rope_rotate(const void* plan_host, const void* p
         if (e != hipSuccess) return fail(SANGAM_ERR_HIP, std::string("rotary launch: ") + hipGetErrorString(e));
     }
     return SANGAM_OK;
+}
+
+}  // namespace
+
+extern "C" sangam_status sangam_rope_rotate(const void* plan_host, const void* plan_dev, const sangam_rope_tensor* q,
+                                            const sangam_rope_tensor* k, int32_t head_dim, int32_t dtype,
+                                            const int32_t* positions_dev, int64_t rows, int32_t transpose, void* stream) {
+    return entry([&] { return rotate(plan_host, plan_dev, q, k, head_dim, dtype, positions_dev, rows, transpose, stream); });
 }

@@ -5,6 +5,7 @@
 #include <string>
 
 #include "../../include/sangam_rope.h"
+#include "entry.h"
 #include "rope_format.h"
 
 namespace sangam {
@@ -21,12 +22,14 @@ const RopePlanHeader* check_rope_plan(const void* plan) {
 
 using namespace sangam;
 
-static sangam_status rope_fail(sangam_status code, const char* msg) {
+namespace {
+
+sangam_status rope_fail(sangam_status code, const char* msg) {
     set_error(msg);
     return code;
 }
 
-extern "C" sangam_status sangam_rope_plan(const sangam_rope_desc* d, void* plan_buf, size_t cap, size_t* used) {
+sangam_status rope_plan(const sangam_rope_desc* d, void* plan_buf, size_t cap, size_t* used) {
     clear_error();
     if (!d || !used) return rope_fail(SANGAM_ERR_INVALID_ARG, "desc and used must not be NULL");
     *used = 0;
@@ -74,4 +77,10 @@ extern "C" sangam_status sangam_rope_plan(const sangam_rope_desc* d, void* plan_
         turns[j] = f / two_pi;
     }
     return SANGAM_OK;
+}
+
+}  // namespace
+
+extern "C" sangam_status sangam_rope_plan(const sangam_rope_desc* d, void* plan_buf, size_t cap, size_t* used) {
+    return entry([&] { return rope_plan(d, plan_buf, cap, used); });
 }

@@ -18,7 +18,7 @@ FORMATS = {"e4m3": (1, torch.float8_e4m3fn, 1), "e2m1": (2, torch.uint8, 2)}
 BLOCK = 32  # consecutive dims of a row that share a scale
 
 
-@dataclass
+@dataclass(eq=False)
 class QuantCache:
     """A pool of quantised pages. k, v: codes, torch.float8_e4m3fn [pages, Hkv,
     16, D] or, two e2m1 codes to a byte (the even dim in the low half),
@@ -93,12 +93,21 @@ def _stream(dev: torch.device, stream: Optional[torch.cuda.Stream]) -> int:
 
 
 def _new(shape, dtype, dev, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """A tensor that `stream`, if not the current one, writes (its memory is
-    not reused before that)."""
+    """A tensor that `stream`, if one was given, writes (its memory is not
+    reused before that)."""
     t = torch.empty(shape, dtype=dtype, device=dev)
     if stream is not None:
         t.record_stream(stream)
     return t
+
+
+def _on_device(p, dev: torch.device, stream: Optional[torch.cuda.Stream]) -> int:
+    """Address of the plan's copy on dev, made there if there is none."""
+    if p.dev is None or p.dev.device != dev:
+        p.to(dev)
+    if stream is not None:
+        p.dev.record_stream(stream)
+    return p.dev.data_ptr()
 
 
 def forward(p: attn.Plan, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cache: QuantCache,
@@ -129,8 +138,7 @@ def forward(p: attn.Plan, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Ten
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
     if launch_events is not None and len(launch_events) != 6:
         raise ValueError("launch_events needs 6 events (start and stop of 3 launches)")
-    if p.dev is None or p.dev.device != dev:
-        p.to(dev)
+    plan_dev = _on_device(p, dev, stream)
     if out is None:
         out = _new((T, Hq, D), torch.bfloat16, dev, stream)
     if lse is None and want_lse:
@@ -140,7 +148,7 @@ def forward(p: attn.Plan, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Ten
     if p.upload_done is not None and p.upload_stream.cuda_stream != s:
         p.order_after_upload(stream if stream is not None else torch.cuda.current_stream(dev))
     evs = None if launch_events is None else (ctypes.c_void_p * 6)(*[e.cuda_event for e in launch_events])
-    _launch(dev, lib.sangam_kvq_forward, p.host_ptr(), p.dev.data_ptr(), q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+    _launch(dev, lib.sangam_kvq_forward, p.host_ptr(), plan_dev, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
             ctypes.byref(cache.c_cache()), page_ids.data_ptr(), num_page_ids, out.data_ptr(),
             lse.data_ptr() if lse is not None else None, workspace.data_ptr() if workspace is not None else None,
             workspace.numel() * workspace.element_size() if workspace is not None else 0, s, evs)
@@ -181,9 +189,7 @@ def kv_export(p: kv.KvPlan, cache: QuantCache, k_packed: Optional[torch.Tensor] 
         v_packed = _new(shape, torch.bfloat16, dev, stream)
     _packed(p, k_packed, "k_packed", dev)
     _packed(p, v_packed, "v_packed", dev)
-    if p.dev is None or p.dev.device != dev:
-        p.to(dev)
-    _launch(dev, lib.sangam_kvq_export, p.host_ptr(), p.dev.data_ptr(), ctypes.byref(cache.c_cache()), k_packed.data_ptr(),
+    _launch(dev, lib.sangam_kvq_export, p.host_ptr(), _on_device(p, dev, stream), ctypes.byref(cache.c_cache()), k_packed.data_ptr(),
             v_packed.data_ptr(), s)
     return k_packed, v_packed
 
@@ -197,7 +203,5 @@ def kv_import(p: kv.KvPlan, k_packed: torch.Tensor, v_packed: torch.Tensor, cach
     _check_cache(cache, p.num_kv_heads, p.head_dim, p.num_pool_pages, dev)
     _packed(p, k_packed, "k_packed", dev)
     _packed(p, v_packed, "v_packed", dev)
-    if p.dev is None or p.dev.device != dev:
-        p.to(dev)
-    _launch(dev, lib.sangam_kvq_import, p.host_ptr(), p.dev.data_ptr(), k_packed.data_ptr(), v_packed.data_ptr(),
+    _launch(dev, lib.sangam_kvq_import, p.host_ptr(), _on_device(p, dev, stream), k_packed.data_ptr(), v_packed.data_ptr(),
             ctypes.byref(cache.c_cache()), s)

@@ -12,7 +12,7 @@ import torch
 
 from . import _lib
 from ._lib import RopeDesc, RopeTensor, check, lib
-from .kvq import _launch, _new, _stream
+from .kvq import _launch, _new, _on_device, _stream
 
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
@@ -97,8 +97,6 @@ def rotate(p: RopePlan, q: torch.Tensor, k: Optional[torch.Tensor], positions: t
         raise TypeError("positions must be an int32 tensor")
     if positions.shape != (rows,) or not positions.is_contiguous() or positions.device != dev:
         raise ValueError(f"positions must be a contiguous [{rows}] tensor on {dev}")
-    if p.dev is None or p.dev.device != dev:
-        p.to(dev)
     if q_out is None:
         q_out = _new(q.shape, dtype, dev, stream)
     else:
@@ -116,6 +114,6 @@ def rotate(p: RopePlan, q: torch.Tensor, k: Optional[torch.Tensor], positions: t
         c_k = ctypes.byref(_tensor(k, k_out, "k", kv_heads))
     elif k_out is not None:
         raise ValueError("k_out without k")
-    _launch(dev, lib.sangam_rope_rotate, p.host_ptr(), p.dev.data_ptr(), ctypes.byref(c_q), c_k, d, DTYPES[dtype],
+    _launch(dev, lib.sangam_rope_rotate, p.host_ptr(), _on_device(p, dev, stream), ctypes.byref(c_q), c_k, d, DTYPES[dtype],
             positions.data_ptr(), rows, 1 if transpose else 0, s)
     return q_out, k_out

@@ -420,6 +420,59 @@ def test_streams_graphs_and_events(dev, fmt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FMTS)
+def test_values_that_are_no_numbers(dev, fmt):
+    """A NaN block of one KV head's cached row makes that head's query heads
+    NaN and no others; infinite fresh rows are written as NaN blocks."""
+    wl = workloads.make_workload("nan", 6, hq=6, hkv=3, d=128, decodes=[(64, 300)], prefills=[40])
+    wl = quantised(wl, fmt)
+    t, cache, codes, scales = quant_inputs(wl, dev, fmt)
+    p = plan_of(wl, dev)
+    clean, _ = kvq.forward(p, t["q"], t["k_new"], t["v_new"], cache, t["page_ids"])
+    page = int(wl.item_pages(0)[200 // 16])
+    for which in ("k_scale", "v_scale"):
+        bad = kvq.QuantCache(cache.k, cache.v, cache.k_scale.clone(), cache.v_scale.clone())
+        getattr(bad, which)[page, 1, 200 % 16, 2] = 255
+        out, _ = kvq.forward(p, t["q"], t["k_new"], t["v_new"], bad, t["page_ids"])
+        nan = torch.isnan(out[:32].float())
+        dims = nan[:, 2:4] if which == "k_scale" else nan[:, 2:4, 64:96]  # a block of V is 32 of its dims
+        assert dims.all() and nan.sum() == dims.numel()
+        rest = ~nan
+        assert torch.equal(out[:32][rest], clean[:32][rest]) and torch.equal(out[32:], clean[32:])
+    k_new = t["k_new"].clone()
+    k_new[3, 2, 5], k_new[4, 0, 100] = float("inf"), float("-inf")  # rows 67 and 68 of the block decode
+    kvq.forward(p, t["q"], k_new, t["v_new"], cache, t["page_ids"])
+    at = int(wl.item_pages(0)[67 // 16])
+    assert cache.k_scale[at, 2, 67 % 16].tolist()[0] == 255 and cache.k_scale[at, 0, 68 % 16].tolist()[3] == 255
+    assert int((cache.k_scale[at] == 255).sum()) == 2
+    assert not cache.k.view(torch.uint8)[at, 2, 67 % 16, :32 if fmt == "e4m3" else 16].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FMTS)
+def test_pages_far_apart(dev, fmt):
+    """Pages past 2^32 bytes of the pool: the bits of the same call on a small one."""
+    hkv, d = 8, 128
+    wl = workloads.make_workload("far", 7, hq=8, hkv=hkv, d=d, decodes=[(64, 500), (0, 40)], prefills=[100])
+    wl = quantised(wl, fmt)
+    t, small, codes, scales = quant_inputs(wl, dev, fmt)
+    pages = 2 ** 32 // (hkv * 16 * small.k.shape[3]) + wl.num_pool_pages + 100
+    far = dataclasses.replace(wl, page_ids=(pages - 1 - wl.page_ids).astype(np.int32), num_pool_pages=pages)
+    big = kvq.empty_cache(pages, hkv, d, format=fmt, device=dev)
+    for a, b in ((big.k, small.k), (big.v, small.v), (big.k_scale, small.k_scale), (big.v_scale, small.v_scale)):
+        a.view(torch.uint8)[pages - wl.num_pool_pages:] = b.view(torch.uint8).flip(0)
+    res = [kvq.forward(plan_of(w, dev), t["q"], t["k_new"], t["v_new"], c, torch.from_numpy(w.page_ids).to(dev)) for w, c in ((wl, small), (far, big))]
+    assert torch.equal(res[0][0].view(torch.int16), res[1][0].view(torch.int16)) and torch.equal(res[0][1], res[1][1])
+    table = lambda w: kv.plan(kv_len=w.kv_len, page_indptr=w.page_indptr, page_ids=w.page_ids, num_kv_heads=hkv, head_dim=d,  # noqa: E731
+                              num_pool_pages=w.num_pool_pages, device=dev)
+    rows = [kvq.kv_export(table(w), c) for w, c in ((wl, small), (far, big))]
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(*rows))
+    kvq.kv_import(table(far), rows[0][1], rows[0][0], big)
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(kvq.kv_export(table(far), big), rows[0][::-1]))
+    assert not big.k.view(torch.uint8)[:pages - wl.num_pool_pages].any()
+
+
+@pytest.mark.gpu
 def test_python_refusals(dev):
     wl = workloads.ragged_small(0, hq=4, hkv=2, d=64)
     t = workloads.device_inputs(wl, dev)

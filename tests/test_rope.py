@@ -12,6 +12,9 @@ below 1), the reduced angle's rounding (2^-28 turns, 2^-25 rad), the factor m
 """
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -122,6 +125,20 @@ def test_no_rows_is_no_launch():
     p = rope.plan(rot_dim=64)
     q = _tensor(in_=None, out=None)
     assert _lib.lib.sangam_rope_rotate(p.host_ptr(), None, ctypes.byref(q), ctypes.byref(q), 64, 0, None, 0, 0, None) == 0
+
+
+@pytest.mark.parametrize("seed", [1, 2])
+def test_plan_under_asan_ubsan(tmp_path, seed):
+    if not shutil.which("g++"):
+        pytest.skip("needs g++")
+    here = os.path.dirname(os.path.abspath(__file__))
+    exe = str(tmp_path / "driver")
+    csrc = os.path.join(os.path.dirname(here), "paper_2607_04206_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-g", "-O1", "-Wall",
+                    os.path.join(here, "sanitize", "rope_driver.cpp"), os.path.join(csrc, "rope_plan.cpp"), "-o", exe], check=True)
+    r = subprocess.run([exe, str(seed)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and " 0 failed checks" in r.stdout, r.stdout[-500:] + r.stderr[-2000:]
+    assert int(r.stdout.split()[0]) > 2000 and int(r.stdout.split()[2]) > 2000
 
 
 def _refused(q_in, q_out, k_in=None, k_out=None):
@@ -244,6 +261,20 @@ def test_strides(dev, interleaved):
     assert none is None and torch.equal(got, want[0][:, :1].expand(rows, 4, d))
     same_row = q[:1].expand(rows, h, d)
     check(rope.rotate(p, same_row, None, pos)[0], same_row, pos, d, interleaved)
+
+
+@pytest.mark.gpu
+def test_rows_far_apart(dev):
+    """Offsets past 2^31 elements and 2^32 bytes."""
+    d, step = 64, 2 ** 31 + 64
+    buf = torch.empty(step + 4 * d, dtype=torch.bfloat16, device=dev)
+    q, k, pos = inputs(2, 2, 1, d, torch.bfloat16, dev)
+    far = buf.as_strided((2, 2, d), (step, d, 1))
+    far.copy_(q)
+    p = rope.plan(rot_dim=d, device=dev)
+    want = rope.rotate(p, q, k, pos)
+    got = rope.rotate(p, far, k, pos, q_out=far)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 @pytest.mark.gpu
