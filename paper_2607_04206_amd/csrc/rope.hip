@@ -55,6 +55,7 @@ constexpr int kThreads = 256;
 // 15.4 us, with two 14.9, with four 14.4 (5.8 TB/s); 15,627 of 64 heads of 128 97.1,
 // 95.9, 95.1.
 constexpr int kUnits = 4;
+constexpr int kGroups = 8 * 256;  // work-groups that a launch has if it can
 
 // Output bytes from which the stores are nontemporal. Measured with plain ->
 // nontemporal stores, 64 heads of 128 dims: 33 MB 11.5 -> 12.1 us, 66 MB 28.5 ->
@@ -279,14 +280,15 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
     args.units = rotating + (in_place ? 0 : (head_dim - h->rot_dim) / v);
     args.size_cos = h->magnitude;
     args.size_sin = transpose ? -h->magnitude : h->magnitude;
-    // A work-group: up to four rows of all heads, fewer rows and then fewer
-    // heads while the launch has under two work-groups per CU and each thread
-    // more than one unit.
+    // A work-group: up to four rows of all heads; fewer rows, and then fewer
+    // heads while each thread has more than one unit, where the launch has
+    // under eight work-groups per CU (1536 rows of 32 heads, 768 -> 1536
+    // work-groups, 8.2 -> 7.6 us; more rows each take the same time).
     args.rows_each = 4;
     args.heads_each = args.heads;
     auto groups = [&] { return (rows + args.rows_each - 1) / args.rows_each * ((args.heads + args.heads_each - 1) / args.heads_each); };
-    while (groups() < 512 && args.rows_each > 1) args.rows_each /= 2;
-    while (groups() < 512 && int64_t(args.rows_each) * args.heads_each * args.units > kThreads && args.heads_each > 1)
+    while (groups() < kGroups && args.rows_each > 1) args.rows_each /= 2;
+    while (groups() < kGroups && int64_t(args.rows_each) * args.heads_each * args.units > kThreads && args.heads_each > 1)
         args.heads_each = (args.heads_each + 1) / 2;
     const bool nt = rows * args.heads * head_dim * size > kStreamBytes;
     const void* fn = dtype == SANGAM_DTYPE_FP32   ? kernel_of<float, 4>(vectors, h->interleaved, nt)
