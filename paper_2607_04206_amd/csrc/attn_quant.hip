@@ -2,14 +2,14 @@
 // ABI entry point (include/sangam_kvq.h).
 //
 // The call, its plans and its tiles are those of attn_fwd.hip (attn_tile in
-// attn_tile.h); what differs is how a cached page gets into a tile. Codes
-// cannot go to LDS as they are: QK^T and PV take bf16 operands, and a code that
-// each wave converted for itself would be converted once per query head of the
-// group. A lane loads whole blocks (32 codes and their scale) of the next stage
-// into registers while the present stage is computed, converts them and writes
-// the bf16 values, which are exact, into the tile that all waves read. The
-// fresh rows of a block pass unquantised, and the tiles that write them back
-// quantise them from LDS.
+// attn_tile.h); what differs is how a cached page gets into a product. With
+// several query heads on a KV head, a code that each wave converted for itself
+// would be converted once per head: a lane loads whole blocks (32 codes and
+// their scale) of the next stage into registers while the present stage is
+// computed, converts them and writes the bf16 values, which are exact, into the
+// tile in LDS that all waves read. With one query head each wave streams keys of
+// its own through its registers, without barriers. Fresh rows pass unquantised,
+// and the tiles that write them back quantise them on the way.
 #include <hip/hip_runtime.h>
 
 #include "../../include/sangam_kvq.h"

@@ -215,6 +215,7 @@ bool may_overlap(const View& a, const View& b, int64_t rows, int64_t d, int64_t 
 }
 
 constexpr int64_t kMaxStride = int64_t(1) << 40;
+constexpr int64_t kMaxSpan = int64_t(1) << 48;  // of all rows, or of all heads, so that offsets fit 64 bits
 
 sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_rope_tensor* q, const sangam_rope_tensor* k,
                      int32_t head_dim, int32_t dtype, const int32_t* positions_dev, int64_t rows, int32_t transpose, void* stream) {
@@ -246,6 +247,8 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
         if (t->in_row_stride < 0 || t->in_head_stride < 0 || t->in_row_stride > kMaxStride || t->in_head_stride > kMaxStride ||
             t->out_row_stride > kMaxStride || t->out_head_stride > kMaxStride)
             return fail(SANGAM_ERR_INVALID_ARG, "strides must be 0 to 2^40");
+        if (std::max(t->in_row_stride, t->out_row_stride) > kMaxSpan / rows || std::max(t->in_head_stride, t->out_head_stride) > kMaxSpan / t->heads)
+            return fail(SANGAM_ERR_INVALID_ARG, "rows times their stride and heads times theirs must be 0 to 2^48");
         if (!apart(rows, t->out_row_stride, t->heads, t->out_head_stride, head_dim))
             return fail(SANGAM_ERR_INVALID_ARG, "rows and heads of the output overlap");
         if (t->in == t->out && (t->in_row_stride != t->out_row_stride || t->in_head_stride != t->out_head_stride))

@@ -26,12 +26,14 @@ class KvPlan:
     num_kv_heads: int
     head_dim: int
     num_pool_pages: int
+    upload_stream: Optional[torch.cuda.Stream] = None  # the stream the device copy was made on
 
     def host_ptr(self) -> int:
         return self.host.ctypes.data
 
     def to(self, device) -> "KvPlan":
         self.dev = torch.from_numpy(self.host).to(device)
+        self.upload_stream = torch.cuda.current_stream(self.dev.device) if self.dev.is_cuda else None
         return self
 
 

@@ -93,20 +93,24 @@ def _stream(dev: torch.device, stream: Optional[torch.cuda.Stream]) -> int:
 
 
 def _new(shape, dtype, dev, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """A tensor that `stream`, if one was given, writes (its memory is not
-    reused before that)."""
-    t = torch.empty(shape, dtype=dtype, device=dev)
-    if stream is not None:
-        t.record_stream(stream)
+    """A tensor that `stream`, if one was given, writes: of that stream's memory
+    (the current stream may still work on what it has freed), not reused before
+    what the current stream does with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    t.record_stream(torch.cuda.current_stream(dev))
     return t
 
 
-def _on_device(p, dev: torch.device, stream: Optional[torch.cuda.Stream]) -> int:
-    """Address of the plan's copy on dev, made there if there is none."""
+def _on_device(p, dev: torch.device, s: int, stream: Optional[torch.cuda.Stream]) -> int:
+    """Address of the plan's copy on dev, made there if there is none; not
+    reused before the call on stream `s` (the given or current one) has read it."""
     if p.dev is None or p.dev.device != dev:
         p.to(dev)
-    if stream is not None:
-        p.dev.record_stream(stream)
+    if p.upload_stream is None or p.upload_stream.cuda_stream != s:
+        p.dev.record_stream(stream if stream is not None else torch.cuda.current_stream(dev))
     return p.dev.data_ptr()
 
 
@@ -138,7 +142,7 @@ def forward(p: attn.Plan, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Ten
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
     if launch_events is not None and len(launch_events) != 6:
         raise ValueError("launch_events needs 6 events (start and stop of 3 launches)")
-    plan_dev = _on_device(p, dev, stream)
+    plan_dev = _on_device(p, dev, s, stream)
     if out is None:
         out = _new((T, Hq, D), torch.bfloat16, dev, stream)
     if lse is None and want_lse:
@@ -189,7 +193,7 @@ def kv_export(p: kv.KvPlan, cache: QuantCache, k_packed: Optional[torch.Tensor] 
         v_packed = _new(shape, torch.bfloat16, dev, stream)
     _packed(p, k_packed, "k_packed", dev)
     _packed(p, v_packed, "v_packed", dev)
-    _launch(dev, lib.sangam_kvq_export, p.host_ptr(), _on_device(p, dev, stream), ctypes.byref(cache.c_cache()), k_packed.data_ptr(),
+    _launch(dev, lib.sangam_kvq_export, p.host_ptr(), _on_device(p, dev, s, stream), ctypes.byref(cache.c_cache()), k_packed.data_ptr(),
             v_packed.data_ptr(), s)
     return k_packed, v_packed
 
@@ -203,5 +207,5 @@ def kv_import(p: kv.KvPlan, k_packed: torch.Tensor, v_packed: torch.Tensor, cach
     _check_cache(cache, p.num_kv_heads, p.head_dim, p.num_pool_pages, dev)
     _packed(p, k_packed, "k_packed", dev)
     _packed(p, v_packed, "v_packed", dev)
-    _launch(dev, lib.sangam_kvq_import, p.host_ptr(), _on_device(p, dev, stream), k_packed.data_ptr(), v_packed.data_ptr(),
+    _launch(dev, lib.sangam_kvq_import, p.host_ptr(), _on_device(p, dev, s, stream), k_packed.data_ptr(), v_packed.data_ptr(),
             ctypes.byref(cache.c_cache()), s)

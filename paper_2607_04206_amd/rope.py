@@ -24,6 +24,7 @@ class RopePlan:
     dev: Optional[torch.Tensor]  # the same bytes on the device
     rot_dim: int
     interleaved: bool
+    upload_stream: Optional[torch.cuda.Stream] = None  # the stream the device copy was made on
 
     def __post_init__(self):
         self._ptr = self.host.ctypes.data
@@ -33,6 +34,7 @@ class RopePlan:
 
     def to(self, device) -> "RopePlan":
         self.dev = torch.from_numpy(self.host).to(device)
+        self.upload_stream = torch.cuda.current_stream(self.dev.device) if self.dev.is_cuda else None
         return self
 
 
@@ -114,6 +116,6 @@ def rotate(p: RopePlan, q: torch.Tensor, k: Optional[torch.Tensor], positions: t
         c_k = ctypes.byref(_tensor(k, k_out, "k", kv_heads))
     elif k_out is not None:
         raise ValueError("k_out without k")
-    _launch(dev, lib.sangam_rope_rotate, p.host_ptr(), _on_device(p, dev, stream), ctypes.byref(c_q), c_k, d, DTYPES[dtype],
+    _launch(dev, lib.sangam_rope_rotate, p.host_ptr(), _on_device(p, dev, s, stream), ctypes.byref(c_q), c_k, d, DTYPES[dtype],
             positions.data_ptr(), rows, 1 if transpose else 0, s)
     return q_out, k_out

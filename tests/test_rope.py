@@ -111,6 +111,7 @@ def _tensor(**over):
     (dict(in_=None), {}, -1), (dict(out=None), {}, -1), (dict(in_=4097, out=1 << 20), {}, -6), (dict(heads=0), {}, -1),
     (dict(in_row_stride=-256, out=1 << 20), {}, -1), (dict(out_row_stride=-256, in_row_stride=-256), {}, -1),
     (dict(out=1 << 20, out_head_stride=63), {}, -1), (dict(out=1 << 20, out_row_stride=255), {}, -1), (dict(out=1 << 20, out_row_stride=0), {}, -1),
+    (dict(in_row_stride=1 << 40, out_row_stride=1 << 40), dict(rows=(1 << 31) - 1), -1),  # more than 64 bits hold
     (dict(out_row_stride=512), {}, -1)])  # in place with other strides
 def test_rotate_refuses(over, call, status):
     # fake device addresses: every check fails before any HIP call
@@ -325,6 +326,32 @@ def test_streams_and_graphs(dev):
         torch.cuda.synchronize()
         want = rope.rotate(p, q, k, pos)
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.gpu
+def test_memory_between_streams(dev):
+    """Outputs of a call on a given stream do not take memory that the current
+    stream still reads, and a plan's memory outlives the call that reads it."""
+    q, _, pos = inputs(300, 16, 2, 64, torch.bfloat16, dev)
+    p = rope.plan(rot_dim=64, device=dev)
+    want, _ = rope.rotate(p, q, None, pos)
+    s = torch.cuda.Stream(dev)
+    torch.cuda.synchronize()
+    held = torch.full_like(want, 3.0)
+    torch.cuda._sleep(20_000_000)  # the copy of `held` is still to come when its memory is free
+    copy = held.clone()
+    del held
+    got, _ = rope.rotate(p, q, None, pos, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(copy, torch.full_like(want, 3.0))
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        got, _ = rope.rotate(p, q, None, pos)
+    size = p.dev.numel()
+    del p
+    others = [torch.zeros(size, dtype=torch.uint8, device=dev) for _ in range(8)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(others) == 8
 
 
 @pytest.mark.gpu
