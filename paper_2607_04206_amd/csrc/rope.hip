@@ -44,6 +44,7 @@ struct RopeArgs {
     int32_t rot;
     int32_t head_dim;
     int32_t units;      // of a head: rotating ones, then ones to copy
+    int32_t copy;       // dims of a head to copy
     int32_t rows_each;  // rows of a work-group
     int32_t heads_each; // heads of a work-group
     float size_cos;     // factors on cos and sin
@@ -75,17 +76,36 @@ __device__ __forceinline__ float2 cos_sin(double turns) {
     return float2{(q == 1 || q == 2) ? -a : a, q >= 2 ? -b : b};
 }
 
-template <bool STREAM, typename V>
-__device__ __forceinline__ void put(void* p, V v) {
-    if (STREAM) __builtin_nontemporal_store(v, static_cast<V*>(p));
-    else *static_cast<V*>(p) = v;
+// A pair turned by (cos, sin). Which product is fused is written out: every
+// variant of the kernel gives the same bits.
+__device__ __forceinline__ float turned0(float x0, float x1, float2 k) { return __builtin_fmaf(x0, k.x, -(x1 * k.y)); }
+__device__ __forceinline__ float turned1(float x0, float x1, float2 k) { return __builtin_fmaf(x1, k.x, x0 * k.y); }
+// (fp16: as a number of 32 bits first; a product and sum that end in 16 at once
+// round once, and the compiler takes them in some places)
+template <typename T>
+__device__ __forceinline__ T rounded(float y) {
+    if constexpr (sizeof(T) == 2 && !__is_same(T, __bf16)) asm("" : "+v"(y));
+    return T(y);
 }
 
-// T: element; V: elements of a vector access (1 where a stride, an address or
-// the number of pairs does not allow whole ones)
-template <typename T, int V, bool INTERLEAVED, bool STREAM>
+template <bool STREAM, typename Access, typename V>
+__device__ __forceinline__ void put(void* p, V v) {
+    if (STREAM) __builtin_nontemporal_store(v, static_cast<V*>(p));
+    else *static_cast<Access*>(p) = v;
+}
+
+// T: element; V: elements of a vector access
+// EDGES: where a stride, an address or a number of pairs or of dims to copy does
+// not allow whole, aligned vectors. Accesses are aligned to elements, and the last
+// vector of the pairs, or of the dims to copy, moves back to end where they do:
+// some outputs are computed and written twice, to the same bits. (In place that
+// would rotate twice: V is 1.) 4748 rows of 28 + 4 heads of 128 dims, 126 of them
+// rotated, fp16: one element at a time 48.5 us, so 22.9;
+// 15,000 of 32 + 8 heads of 64, 18 rotated, bf16: 118.6 and 47.0.
+template <typename T, int V, bool INTERLEAVED, bool STREAM, bool EDGES>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     typedef T Vec __attribute__((ext_vector_type(V)));
+    typedef Vec Access __attribute__((aligned(EDGES ? sizeof(T) : sizeof(Vec))));
     constexpr bool ONE = INTERLEAVED && V > 1;  // a unit is one vector of whole pairs, else the two sides of V pairs
     extern __shared__ float2 angles[];          // [rows_each][rot / 2]
     const int half = a.rot / 2;
@@ -93,7 +113,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     const int nrows = int(a.rows - row0 < a.rows_each ? a.rows - row0 : a.rows_each);
     const int head0 = int(blockIdx.y) * a.heads_each;
     const int nheads = min(a.heads_each, a.heads - head0);
-    const int rotating = INTERLEAVED ? a.rot / (V > 1 ? V : 2) : half / V;
+    const int side = INTERLEAVED ? a.rot / (ONE ? 1 : 2) : half;  // elements that units of V cover
+    const int rotating = EDGES ? (side + V - 1) / V : side / V;
     const int total = nrows * nheads * a.units;
 
     // A thread's next units, loaded together; those of the first round are on
@@ -102,7 +123,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
         Vec x, z;
         T* out;     // of its head; nullptr: no unit
         int first;  // dim of x
-        int pairs;  // its first pair's entry in angles, -1: to copy
+        int pairs;  // its first pair's entry in angles, -1: to copy, -2: to copy less than a vector
     } w[kUnits];
     auto load = [&](int u0) {
 #pragma unroll
@@ -118,10 +139,21 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
             const T* in = static_cast<const T*>(t.in) + (row0 + r) * t.in_row + h * t.in_head;
             w[j].out = static_cast<T*>(t.out) + (row0 + r) * t.out_row + h * t.out_head;
             const bool copy = c >= rotating;
-            w[j].first = copy ? a.rot + (c - rotating) * V : ONE || !INTERLEAVED ? c * V : 2 * c;
-            w[j].pairs = copy ? -1 : r * half + (ONE ? c * V / 2 : c * V);
-            w[j].x = *(const Vec*)(in + w[j].first);
-            if (!ONE && !copy) w[j].z = *(const Vec*)(in + w[j].first + (INTERLEAVED ? 1 : half));
+            int at = copy ? (c - rotating) * V : c * V;
+            if (EDGES) at = min(at, (copy ? a.copy : side) - V);
+            w[j].first = copy ? a.rot + at : ONE || !INTERLEAVED ? at : 2 * at;
+            w[j].pairs = copy ? -1 : r * half + (ONE ? at / 2 : at);
+            if (EDGES && copy && a.copy < V) {
+                w[j].out += a.rot;
+                w[j].pairs = -2;
+                w[j].first = 0;
+#pragma unroll
+                for (int e = 0; e < V - 1; ++e)
+                    if (e < a.copy) w[j].x[e] = in[a.rot + e];
+                continue;
+            }
+            w[j].x = *(const Access*)(in + w[j].first);
+            if (!ONE && !copy) w[j].z = *(const Access*)(in + w[j].first + (INTERLEAVED ? 1 : half));
         }
     };
     load(threadIdx.x);
@@ -137,8 +169,14 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
         for (int j = 0; j < kUnits; ++j) {
             T* const out = w[j].out + w[j].first;
             if (!w[j].out) continue;
+            if (EDGES && w[j].pairs == -2) {
+#pragma unroll
+                for (int e = 0; e < V - 1; ++e)
+                    if (e < a.copy) out[e] = w[j].x[e];
+                continue;
+            }
             if (w[j].pairs < 0) {
-                put<STREAM>(out, w[j].x);
+                put<STREAM, Access>(out, w[j].x);
                 continue;
             }
             const float2* cs = angles + w[j].pairs;
@@ -148,34 +186,37 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                 for (int e = 0; e < V; e += 2) {
                     const float2 k = cs[e / 2];
                     const float x0 = float(w[j].x[e]), x1 = float(w[j].x[e + 1]);
-                    y[e] = T(x0 * k.x - x1 * k.y);
-                    y[e + 1] = T(x1 * k.x + x0 * k.y);
+                    y[e] = rounded<T>(turned0(x0, x1, k));
+                    y[e + 1] = rounded<T>(turned1(x0, x1, k));
                 }
-                put<STREAM>(out, y);
+                put<STREAM, Access>(out, y);
             } else {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const float2 k = cs[e];
                     const float x0 = float(w[j].x[e]), x1 = float(w[j].z[e]);
-                    y[e] = T(x0 * k.x - x1 * k.y);
-                    z[e] = T(x1 * k.x + x0 * k.y);
+                    y[e] = rounded<T>(turned0(x0, x1, k));
+                    z[e] = rounded<T>(turned1(x0, x1, k));
                 }
-                put<STREAM>(out, y);
-                put<STREAM>(out + (INTERLEAVED ? 1 : half), z);
+                put<STREAM, Access>(out, y);
+                put<STREAM, Access>(out + (INTERLEAVED ? 1 : half), z);
             }
         }
     }
 }
 
+enum class Access { kElements, kEdges, kVectors };
+
 template <typename T, int V, bool INTERLEAVED>
-const void* kernel_of(bool vectors, bool stream) {
-    if (!vectors) return reinterpret_cast<const void*>(&rope_kernel<T, 1, INTERLEAVED, false>);
-    return stream ? reinterpret_cast<const void*>(&rope_kernel<T, V, INTERLEAVED, true>)
-                  : reinterpret_cast<const void*>(&rope_kernel<T, V, INTERLEAVED, false>);
+const void* kernel_of(Access access, bool stream) {
+    if (access == Access::kElements) return reinterpret_cast<const void*>(&rope_kernel<T, 1, INTERLEAVED, false, false>);
+    if (access == Access::kEdges) return reinterpret_cast<const void*>(&rope_kernel<T, V, INTERLEAVED, false, true>);
+    return stream ? reinterpret_cast<const void*>(&rope_kernel<T, V, INTERLEAVED, true, false>)
+                  : reinterpret_cast<const void*>(&rope_kernel<T, V, INTERLEAVED, false, false>);
 }
 template <typename T, int V>
-const void* kernel_of(bool vectors, bool interleaved, bool stream) {
-    return interleaved ? kernel_of<T, V, true>(vectors, stream) : kernel_of<T, V, false>(vectors, stream);
+const void* kernel_of(Access access, bool interleaved, bool stream) {
+    return interleaved ? kernel_of<T, V, true>(access, stream) : kernel_of<T, V, false>(access, stream);
 }
 
 sangam_status fail(sangam_status code, const std::string& msg) {
@@ -232,7 +273,7 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
     const int V = int(16 / size);
     // vectors: whole ones on each side of the pairs, and every access aligned
     bool vectors = h->rot_dim % (h->interleaved ? V : 2 * V) == 0 && head_dim % V == 0;
-    bool in_place = true;
+    bool in_place = true, any_in_place = false;
     RopeArgs args{};
     int heads[2] = {0, 0};
     for (int i = 0; i < 2; ++i) {
@@ -256,6 +297,7 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
         for (int64_t stride : {t->in_row_stride, t->in_head_stride, t->out_row_stride, t->out_head_stride}) vectors = vectors && stride % V == 0;
         vectors = vectors && reinterpret_cast<uintptr_t>(t->in) % 16 == 0 && reinterpret_cast<uintptr_t>(t->out) % 16 == 0;
         in_place = in_place && t->in == t->out;
+        any_in_place = any_in_place || t->in == t->out;
         args.t[i] = RopeTensor{t->in, t->out, t->in_row_stride, t->in_head_stride, t->out_row_stride, t->out_head_stride};
     }
     if (rows == 0) return SANGAM_OK;
@@ -273,14 +315,18 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
     if (!plan_dev || !positions_dev) return fail(SANGAM_ERR_INVALID_ARG, "plan_dev and positions_dev must not be NULL");
     if (reinterpret_cast<uintptr_t>(plan_dev) & 15u || reinterpret_cast<uintptr_t>(positions_dev) & 3u)
         return fail(SANGAM_ERR_ALIGN, "plan_dev must be 16-byte and positions_dev 4-byte aligned");
-    const int v = vectors ? V : 1;
+    // edges: a vector of pairs at least
+    const bool short_side = h->rot_dim < (h->interleaved ? V : 2 * V);
+    const Access access = vectors ? Access::kVectors : any_in_place || short_side ? Access::kElements : Access::kEdges;
+    const int v = access == Access::kElements ? 1 : V;
     args.turns = reinterpret_cast<const double*>(static_cast<const uint8_t*>(plan_dev) + h->off_turns);
     args.heads_q = heads[0];
     args.heads = heads[0] + heads[1];
     args.rot = h->rot_dim;
     args.head_dim = head_dim;
-    const int rotating = h->interleaved ? h->rot_dim / std::max(v, 2) : h->rot_dim / 2 / v;
-    args.units = rotating + (in_place ? 0 : (head_dim - h->rot_dim) / v);
+    args.copy = in_place ? 0 : head_dim - h->rot_dim;
+    const int side = h->interleaved && v > 1 ? h->rot_dim : h->rot_dim / 2;
+    args.units = (side + v - 1) / v + (args.copy + v - 1) / v;
     args.size_cos = h->magnitude;
     args.size_sin = transpose ? -h->magnitude : h->magnitude;
     // A work-group: up to four rows of all heads; fewer rows, and then fewer
@@ -294,9 +340,9 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
     while (groups() < kGroups && int64_t(args.rows_each) * args.heads_each * args.units > kThreads && args.heads_each > 1)
         args.heads_each = (args.heads_each + 1) / 2;
     const bool nt = rows * args.heads * head_dim * size > kStreamBytes;
-    const void* fn = dtype == SANGAM_DTYPE_FP32   ? kernel_of<float, 4>(vectors, h->interleaved, nt)
-                     : dtype == SANGAM_DTYPE_FP16 ? kernel_of<_Float16, 8>(vectors, h->interleaved, nt)
-                                                  : kernel_of<__bf16, 8>(vectors, h->interleaved, nt);
+    const void* fn = dtype == SANGAM_DTYPE_FP32   ? kernel_of<float, 4>(access, h->interleaved, nt)
+                     : dtype == SANGAM_DTYPE_FP16 ? kernel_of<_Float16, 8>(access, h->interleaved, nt)
+                                                  : kernel_of<__bf16, 8>(access, h->interleaved, nt);
     void* kargs[] = {&args};
     const unsigned lds = unsigned(args.rows_each) * unsigned(h->rot_dim / 2) * unsigned(sizeof(float2));
     const unsigned splits = unsigned((args.heads + args.heads_each - 1) / args.heads_each);

@@ -265,6 +265,29 @@ def test_strides(dev, interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot", [(128, 126), (128, 110), (128, 122), (64, 46), (37, 24), (20, 18), (64, 62), (21, 16), (130, 128), (24, 8), (9, 8), (7, 4)])
+def test_numbers_of_pairs_that_no_vector_divides(dev, dtype, interleaved, d, rot):
+    """Outputs beside guards, head strides and addresses of odd numbers of
+    elements, and the same in place, which gives the same bits."""
+    rows, h, pad = 53, 5, 3
+    q, k, pos = inputs(rows, h, 2, d, dtype, dev)
+    p = rope.plan(rot_dim=rot, interleaved=interleaved, device=dev)
+    buf = torch.full((1 + rows * h * (d + pad),), 7.0, dtype=dtype, device=dev)
+    out = buf[1:].view(rows, h, d + pad)[:, :, :d]
+    got = rope.rotate(p, q, k, pos, q_out=out)
+    check(out, q, pos, rot, interleaved)
+    check(got[1], k, pos, rot, interleaved)
+    guards = buf.clone()
+    guards[1:].view(rows, h, d + pad)[:, :, :d] = 7.0
+    assert (guards == 7.0).all()
+    here = q.clone()
+    rope.rotate(p, here, None, pos, q_out=here)
+    assert torch.equal(here, out)
+
+
+@pytest.mark.gpu
 def test_rows_far_apart(dev):
     """Offsets past 2^31 elements and 2^32 bytes."""
     d, step = 64, 2 ** 31 + 64
