@@ -45,6 +45,7 @@ struct RopeArgs {
     int32_t head_dim;
     int32_t units;      // of a head: rotating ones, then ones to copy
     int32_t copy;       // dims of a head to copy
+    int32_t in_place;   // whether q or k is rotated in place
     int32_t rows_each;  // rows of a work-group
     int32_t heads_each; // heads of a work-group
     float size_cos;     // factors on cos and sin
@@ -98,10 +99,11 @@ __device__ __forceinline__ void put(void* p, V v) {
 // EDGES: where a stride, an address or a number of pairs or of dims to copy does
 // not allow whole, aligned vectors. Accesses are aligned to elements, and the last
 // vector of the pairs, or of the dims to copy, moves back to end where they do:
-// some outputs are computed and written twice, to the same bits. (In place that
-// would rotate twice: V is 1.) 4748 rows of 28 + 4 heads of 128 dims, 126 of them
-// rotated, fp16: one element at a time 48.5 us, so 22.9;
-// 15,000 of 32 + 8 heads of 64, 18 rotated, bf16: 118.6 and 47.0.
+// some outputs are computed and written twice, to the same bits. In place, where
+// what it reads of its neighbour may be rotated already, it writes its own
+// elements only. 4748 rows of 28 + 4 heads of 128 dims, 126 of them rotated, fp16:
+// one element at a time 48.5 us, so 22.9, in place 38.9 and 22.8; 15,000 of 32 + 8 heads
+// of 64, 18 rotated, bf16: 118.6 and 47.0, in place 34.0 and 29.8.
 template <typename T, int V, bool INTERLEAVED, bool STREAM, bool EDGES>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     typedef T Vec __attribute__((ext_vector_type(V)));
@@ -124,6 +126,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
         T* out;     // of its head; nullptr: no unit
         int first;  // dim of x
         int pairs;  // its first pair's entry in angles, -1: to copy, -2: to copy less than a vector
+        int skip;   // elements of x that another unit writes
     } w[kUnits];
     auto load = [&](int u0) {
 #pragma unroll
@@ -140,7 +143,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
             w[j].out = static_cast<T*>(t.out) + (row0 + r) * t.out_row + h * t.out_head;
             const bool copy = c >= rotating;
             int at = copy ? (c - rotating) * V : c * V;
-            if (EDGES) at = min(at, (copy ? a.copy : side) - V);
+            w[j].skip = 0;
+            if (EDGES) {
+                const int whole = at;
+                at = min(at, (copy ? a.copy : side) - V);
+                if (a.in_place && !copy) w[j].skip = whole - at;
+            }
             w[j].first = copy ? a.rot + at : ONE || !INTERLEAVED ? at : 2 * at;
             w[j].pairs = copy ? -1 : r * half + (ONE ? at / 2 : at);
             if (EDGES && copy && a.copy < V) {
@@ -189,6 +197,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     y[e] = rounded<T>(turned0(x0, x1, k));
                     y[e + 1] = rounded<T>(turned1(x0, x1, k));
                 }
+                if (EDGES && w[j].skip > 0) {
+#pragma unroll
+                    for (int e = 1; e < V; ++e)
+                        if (e >= w[j].skip) out[e] = y[e];
+                    continue;
+                }
                 put<STREAM, Access>(out, y);
             } else {
 #pragma unroll
@@ -197,6 +211,15 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     const float x0 = float(w[j].x[e]), x1 = float(w[j].z[e]);
                     y[e] = rounded<T>(turned0(x0, x1, k));
                     z[e] = rounded<T>(turned1(x0, x1, k));
+                }
+                if (EDGES && w[j].skip > 0) {
+#pragma unroll
+                    for (int e = 1; e < V; ++e)
+                        if (e >= w[j].skip) {
+                            out[e] = y[e];
+                            out[e + half] = z[e];
+                        }
+                    continue;
                 }
                 put<STREAM, Access>(out, y);
                 put<STREAM, Access>(out + (INTERLEAVED ? 1 : half), z);
@@ -317,7 +340,7 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
         return fail(SANGAM_ERR_ALIGN, "plan_dev must be 16-byte and positions_dev 4-byte aligned");
     // edges: a vector of pairs at least
     const bool short_side = h->rot_dim < (h->interleaved ? V : 2 * V);
-    const Access access = vectors ? Access::kVectors : any_in_place || short_side ? Access::kElements : Access::kEdges;
+    const Access access = vectors ? Access::kVectors : short_side ? Access::kElements : Access::kEdges;
     const int v = access == Access::kElements ? 1 : V;
     args.turns = reinterpret_cast<const double*>(static_cast<const uint8_t*>(plan_dev) + h->off_turns);
     args.heads_q = heads[0];
@@ -325,6 +348,7 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
     args.rot = h->rot_dim;
     args.head_dim = head_dim;
     args.copy = in_place ? 0 : head_dim - h->rot_dim;
+    args.in_place = any_in_place;
     const int side = h->interleaved && v > 1 ? h->rot_dim : h->rot_dim / 2;
     args.units = (side + v - 1) / v + (args.copy + v - 1) / v;
     args.size_cos = h->magnitude;

@@ -282,9 +282,15 @@ def test_numbers_of_pairs_that_no_vector_divides(dev, dtype, interleaved, d, rot
     guards = buf.clone()
     guards[1:].view(rows, h, d + pad)[:, :, :d] = 7.0
     assert (guards == 7.0).all()
-    here = q.clone()
-    rope.rotate(p, here, None, pos, q_out=here)
-    assert torch.equal(here, out)
+    here = buf.clone()
+    x = here[1:].view(rows, h, d + pad)[:, :, :d]
+    x.copy_(q)
+    apart = rope.rotate(p, x, k, pos, q_out=x)[1]  # q in place, k not
+    assert torch.equal(here, buf) and torch.equal(apart, got[1])
+    both = k.clone()
+    x.copy_(q)
+    rope.rotate(p, x, both, pos, q_out=x, k_out=both)
+    assert torch.equal(here, buf) and torch.equal(both, got[1])
 
 
 @pytest.mark.gpu
