@@ -157,6 +157,17 @@ __device__ __forceinline__ float half_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// x of both halves summed in the lower one, y of both halves in the upper one,
+// and such a pair's two sums in every lane.
+__device__ __forceinline__ float half_sums(float x, float y) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float2 both_sums(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return float2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+
 // The running max moves only when a score exceeds it by more than this (log2
 // units), so P <= 2^8 and O is rescaled rarely; the result is unchanged
 // because O and l always share the same reference.
@@ -358,6 +369,9 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
     const size_t stage_stride = STEP * row_stride;  // elements
 
     // do_k, do_v: whether to copy the stage's K rows and its V rows
+    // (Over a quantised cache only whole prefills are copied: what cached and
+    // listed rows need takes no registers there.)
+    const bool copies_fresh = QUANT || all_fresh, copies_listed = !QUANT && plist;
     auto issue_stage = [&](int st, int buf, auto do_k, auto do_v) __attribute__((always_inline)) {
         uint8_t* kb = smem + buf * 2 * TILE;
         uint8_t* vb = kb + TILE;
@@ -372,7 +386,7 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
                 if (SP % NW != 0 && k >= SP) break;
                 LDS void* kd = (LDS void*)(kb + k * 16 * ROWB);
                 LDS void* vd = (LDS void*)(vb + k * 16 * ROWB);
-                if (all_fresh) {
+                if (copies_fresh) {
                     if (do_k) copy_page(kf + i * NW * 16 * row_stride, foff_k, kd);
                     if (do_v) copy_page(vf + i * NW * 16 * row_stride, foff_v, vd);
                 } else {
@@ -391,10 +405,10 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
             const bool past = skey0 + k * 16 >= kv_end;
             const int key0 = past ? skey0 : skey0 + k * 16;
             const int pl = past ? pl0 : pl0 + k;
-            const uint32_t inf = plist ? uint32_t(__builtin_amdgcn_readlane(int(iv), pl)) : 0u;
-            const size_t off = all_fresh ? 0 : (size_t)__builtin_amdgcn_readlane(pv, pl) * page_stride;
-            if (key0 + 16 <= kv_end && !all_fresh &&
-                (plist ? (inf & 0xFFFFu) == 0 : key0 + 16 <= it.o || key0 >= it.o + it.n)) {
+            const uint32_t inf = copies_listed ? uint32_t(__builtin_amdgcn_readlane(int(iv), pl)) : 0u;
+            const size_t off = copies_fresh ? 0 : (size_t)__builtin_amdgcn_readlane(pv, pl) * page_stride;
+            if (key0 + 16 <= kv_end && !copies_fresh &&
+                (copies_listed ? (inf & 0xFFFFu) == 0 : key0 + 16 <= it.o || key0 >= it.o + it.n)) {
                 if (do_k) copy_page(kcache + off, coff_k, kd);
                 if (do_v) copy_page(vcache + off, coff_v, vd);
                 continue;
@@ -403,7 +417,7 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
             // last page (rows past its end repeat its last row)
             const int lim = min(16, kv_end - key0);
             // fresh rows of the page: row `first` onwards, in order
-            const int64_t first = plist ? int64_t(it.q_start) + (inf >> kPageInfoRowShift)
+            const int64_t first = copies_listed ? int64_t(it.q_start) + (inf >> kPageInfoRowShift)
                                         : int64_t(it.q_start) + key0 - it.o;
             const uint64_t fk = (uint64_t)(a.k_new + (size_t)t.kv_head * D) + uint64_t(first * int64_t(row_bytes));
             const uint64_t fv = (uint64_t)(a.v_new + (size_t)t.kv_head * D) + uint64_t(first * int64_t(row_bytes));
@@ -412,8 +426,8 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
             for (int j = 0; j < IPP; ++j) {
                 const int r = RPI * j + lane / NC, pos = lane % NC;
                 const int rc = min(r, lim - 1);
-                const bool fresh = plist ? (inf >> rc) & 1u : unsigned(key0 + rc - it.o) < unsigned(it.n);
-                const uint32_t frow = plist ? __builtin_popcount(inf & ((1u << rc) - 1u)) : rc;
+                const bool fresh = copies_listed ? (inf >> rc) & 1u : unsigned(key0 + rc - it.o) < unsigned(it.n);
+                const uint32_t frow = copies_listed ? __builtin_popcount(inf & ((1u << rc) - 1u)) : rc;
                 const uint32_t ro = fresh ? frow * row_bytes : uint32_t(rc * ROWB);
                 const int64_t lo = int64_t(ro) - 1024 * j;
                 ak[j] = (fresh ? fk : (uint64_t)(kcache + off)) + uint64_t(lo + ((pos ^ swz_k<D>(r)) << 4));
@@ -613,12 +627,13 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
 
     f32x16 o[QB][MB];
     float m_used[QB];  // reference max (log2 domain) of this lane's query, per block
-    float l_run[QB];   // sum of P over this lane's half of the keys: of the rounded P, or, over
-                       // a quantised cache, of P as it is, which the LSE is then exact in
+    float l_run[QB];   // sum of the rounded P over this lane's half of the keys
+    float l_full[QB];  // over a quantised cache: of P as it is, which the LSE is then exact in
+                       // (SOLO has no register for it: l_run is both, as below)
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         m_used[qb] = -INFINITY;
-        l_run[qb] = 0.0f;
+        l_run[qb] = l_full[qb] = 0.0f;
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -715,6 +730,7 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
                 const float alpha = need ? __builtin_amdgcn_exp2f(m_used[qb] - mx[qb]) : 1.0f;
                 m_used[qb] = need ? mx[qb] : m_used[qb];
                 l_run[qb] *= alpha;
+                if constexpr (QUANT) l_full[qb] *= alpha;
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -746,8 +762,8 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
                     const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sb[i], c, mneg[qb]));
                     const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sb[i + 1], c, mneg[qb]));
                     const bf16x2 pp = {(__bf16)p0, (__bf16)p1};
-                    if constexpr (QUANT) l_run[qb] += p0 + p1;
-                    else l_run[qb] = __builtin_amdgcn_fdot2_f32_bf16(pp, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l_run[qb], false);
+                    if constexpr (QUANT) l_full[qb] += p0 + p1;
+                    l_run[qb] = __builtin_amdgcn_fdot2_f32_bf16(pp, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l_run[qb], false);
                     pf[qb][kk][j] = pp[0];
                     pf[qb][kk][j + 1] = pp[1];
                 }
@@ -927,14 +943,18 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
             }
             const float mneg = m_used[0] == -INFINITY ? 0.0f : -m_used[0];
             bf16x8 pf[2];
+            float full = 0.0f, rounded = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, mneg));
                 const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], c, mneg));
-                l_run[0] += p0 + p1;
-                pf[i >> 3][i & 7] = (__bf16)p0;
-                pf[i >> 3][(i & 7) + 1] = (__bf16)p1;
+                const bf16x2 pp = {(__bf16)p0, (__bf16)p1};
+                full += p0 + p1;
+                rounded = __builtin_amdgcn_fdot2_f32_bf16(pp, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, rounded, false);
+                pf[i >> 3][i & 7] = pp[0];
+                pf[i >> 3][(i & 7) + 1] = pp[1];
             }
+            l_run[0] += half_sums(rounded, full);
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -1154,6 +1174,14 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
         }
     }
 
+    // Over a quantised cache both sums go on as one value, the rounded weights'
+    // in the lower half-wave and the full one in the upper one. O is divided by
+    // the former, so that it is an average of V's rows (equal rows give
+    // themselves); the LSE, by which splits are weighed, is that of the latter.
+    if constexpr (QUANT && !SOLO)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) l_run[qb] = half_sums(l_run[qb], l_full[qb]);
+
     // ---- combine the context sub-ranges of the waves that share query rows:
     // each of the KW waves then holds MBW of the MB 32-dim blocks of O
     constexpr int MBW = MB / KW;
@@ -1207,9 +1235,9 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
     float lse_val[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const float l_tot = half_sum(l_run[qb]);
-        const float inv = 1.0f / l_tot;
-        lse_val[qb] = m_used[qb] * 0.69314718055994530942f + logf(l_tot);
+        const float2 l = QUANT ? both_sums(l_run[qb]) : float2{half_sum(l_run[qb]), 0.0f};
+        const float inv = 1.0f / l.x;
+        lse_val[qb] = m_used[qb] * 0.69314718055994530942f + logf(QUANT ? l.y : l.x);
 #pragma unroll
         for (int mb = 0; mb < MBW; ++mb)
 #pragma unroll

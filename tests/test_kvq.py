@@ -421,6 +421,33 @@ def test_streams_graphs_and_events(dev, fmt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("hq,hkv,d,prefills,kw", [
+    *((2 * g, 2, d, [], dict(num_cus=8)) for g in range(1, 9) for d in (64, 128)),  # decode tiles of every group
+    (4, 4, 128, [], dict(force_kv_splits=3)), (14, 2, 128, [], dict(force_kv_splits=3, num_cus=8)),
+    (8, 8, 128, [1300], {}), (4, 4, 64, [400], {}),  # MHA decodes beside prefills
+    (14, 2, 128, [333], {}), (4, 2, 128, [1100], {})])
+def test_equal_rows_of_v(dev, fmt, hq, hkv, d, prefills, kw):
+    """Where all rows of V are the same, so is every output, whatever the weights: what multiplies V and
+    what the sum is divided by are the same numbers. Values that both formats hold, so that cached and
+    fresh rows agree, under scores of deviation 8, whose largest weights round far from 1. Products of
+    two bf16 numbers are exact and sums of up to 1500 of one sign are off by 1500 * 2^-24 of themselves,
+    as is the divisor: 2^-12, below the 2^-9 at which a bf16 number rounds to another."""
+    print(f"[case] kvq {fmt} equal rows of V {hq}/{hkv} heads of {d}, prefills {prefills} {kw}", flush=True)
+    wl = workloads.make_workload("equal", 8, hq=hq, hkv=hkv, d=d, decodes=[(64, 1000), (3, 450), (0, 33), (600, 1500)], prefills=prefills)
+    row = np.random.default_rng(hq + d).choice([0.5, -1.0, 1.5, -2.0, 3.0, 4.0, -6.0], size=(hkv, d))
+    assert np.array_equal(mx.values(*mx.quantise(row, fmt), fmt), row)
+
+    def value_fn(item, kind):
+        n = {workloads.KIND_VCTX: int(wl.kv_len[item]), workloads.KIND_VNEW: wl.n(item)}.get(kind)
+        return None if n is None else torch.from_numpy(row).float().expand(n, hkv, d)
+    t, cache, _, _ = quant_inputs(dataclasses.replace(wl, value_fn=value_fn, q_scale=8.0), dev, fmt)
+    out, _ = kvq.forward(plan_of(wl, dev, **kw), t["q"], t["k_new"], t["v_new"], cache, t["page_ids"])
+    want = np.broadcast_to(row.repeat(hq // hkv, 0), out.shape)
+    equal(out.float().cpu().numpy(), want.astype(np.float32), "outputs")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FMTS)
 def test_values_that_are_no_numbers(dev, fmt):
     """A NaN block of one KV head's cached row makes that head's query heads
     NaN and no others; infinite fresh rows are written as NaN blocks."""
