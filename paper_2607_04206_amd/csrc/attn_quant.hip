@@ -18,6 +18,7 @@
 #include "entry.h"
 #include "mixed_order.h"
 #include "plan_format.h"
+#include "xcd_order.h"
 
 using namespace sangam;
 
@@ -62,20 +63,9 @@ struct MixedQuantArgs {
     const TileRec* decode_tiles;
     MixedOrder order;
     int32_t wide;
-    int32_t round;  // prefill blocks on the chip at a time: one per CU
+    int32_t round;       // prefill blocks on the chip at a time: one per CU
+    int32_t plan_chunk;  // xcd_plan_chunk of the plan's prefill tiles
 };
-
-constexpr int kXcds = 8;  // each with its own L2; block b runs on XCD b mod 8
-
-// Block `index` of n in an order in which each XCD has consecutive blocks of
-// every round: row blocks of the same heads, which read the same K and V (16
-// decodes beside prefills of 1819 and 1201 rows, 32/32 heads, 177 -> 170.5 us; 8
-// beside 2500 rows 150 -> 145; smaller batches within 1 %).
-__device__ __forceinline__ int xcd_order(int index, int n, int round) {
-    const int base = index / round * round;
-    const int each = min(round, n - base) / kXcds, q = index - base;
-    return q < each * kXcds ? base + q % kXcds * each + q / kXcds : index;
-}
 
 template <typename Fmt, int D>
 __global__ __launch_bounds__(256, waves(D, 4)) void attn_quant_mixed_kernel(MixedQuantArgs m) {
@@ -89,10 +79,13 @@ __global__ __launch_bounds__(256, waves(D, 4)) void attn_quant_mixed_kernel(Mixe
         attn_tile<D, 1, KW, 1, 1, 1, true, 4 - KW, QuantCache<Fmt>>(m.a, t, m.a.items[t.item], shared);
         return;
     }
-    const int index = xcd_order(b.index, m.order.n_prefill, m.round);
-    TileRec t = m.a.tiles[index >> m.wide];
+    // Each XCD has consecutive blocks of every round (16 decodes beside prefills
+    // of 1819 and 1201 rows, 32/32 heads, 177 -> 170.5 us; 8 beside 2500 rows 150
+    // -> 145; smaller batches within 1 %).
+    const XcdTile x = xcd_mixed_tile(b.index, m.order.n_prefill, m.wide, m.round, m.plan_chunk);
+    TileRec t = m.a.tiles[x.tile];
     const ItemRec it = m.a.items[t.item];
-    if (m.wide) t.row0 += kPrefillRows * (index & 1);
+    t.row0 += kPrefillRows * x.half;
     if (t.row0 < it.n) attn_tile<D, 4, 1, 1, 2, 2, false, 0, QuantCache<Fmt>>(m.a, t, it, shared);
 }
 
@@ -120,7 +113,9 @@ struct QuantKernels {
                      unsigned blocks, hipStream_t stream, LaunchEvents ev) const {
         const void* fn = h.d == 64 ? reinterpret_cast<const void*>(&attn_quant_mixed_kernel<Fmt, 64>)
                                    : reinterpret_cast<const void*>(&attn_quant_mixed_kernel<Fmt, 128>);
-        return launch(fn, dim3(blocks), 256u, MixedQuantArgs{args, decodes, order, h.prefill_rows == kWidePrefillRows, h.cus > 0 ? h.cus : 256},
+        const int cus = h.cus > 0 ? h.cus : 256;
+        return launch(fn, dim3(blocks), 256u,
+                      MixedQuantArgs{args, decodes, order, h.prefill_rows == kWidePrefillRows, cus, xcd_plan_chunk(h.n_prefill_tiles, h.prefill_rows, cus)},
                       stream, ev);
     }
 

@@ -35,6 +35,7 @@
 #include "../../include/sangam_attn.h"
 #include "page_check.h"
 #include "plan_format.h"
+#include "xcd_order.h"
 
 namespace sangam {
 
@@ -83,11 +84,6 @@ static int64_t min_chunk_idle(int qw) { return qw == 1 ? 256 : 512; }
 // What a whole-group decode tile costs beside its stages, in 64-key stages (of
 // about 2.2 us at 28/4 heads): start-up and epilogue, partials, a merge launch.
 constexpr int64_t kTileStages = 3, kSplitStages = 2, kMergeStages = 3;
-
-// XCDs of the chip (each with its own L2), and the rounds of tiles per
-// work-group slot from which a prefill-shaped launch takes the XCD-aware order
-constexpr int kXcds = 8;
-constexpr size_t kXcdOrderMinRounds = 8;
 
 // Whether a batch of prefills and block decodes of one query head per KV head
 // takes a launch for each kind instead of one for both (attn_mixed_kernel; the
@@ -512,34 +508,19 @@ extern "C" sangam_status sangam_attn_plan(const sangam_attn_desc* d, void* plan_
     };
     lpt(dec, dec_cost);
     lpt(pre, pre_cost);
-    // XCD-aware order of a long prefill-shaped launch. The dispatcher deals
-    // work-groups to the kXcds XCDs in turn (block b to XCD b mod kXcds, up
-    // to a fixed rotation), and each XCD has its own L2. Cut the
-    // longest-first list into chunks of kXcds x C tiles (C = the launch's
-    // slots per XCD) and give each XCD C consecutive tiles of every chunk:
-    // they are row blocks of one query head, so the XCD's work-groups stream
-    // the same K/V at once and share it in L2 (prefill-heavy: 46 % less
-    // traffic beyond L2, time unchanged). Only with at least
-    // kXcdOrderMinRounds rounds of tiles per slot: in a shorter launch the
-    // chunks split the longest-first balance unevenly across XCDs.
-    {
-        const size_t C = size_t(std::max(1, num_cus / kXcds)) * (prefill_rows == kWidePrefillRows ? 1 : 2);
-        const size_t C8 = C * kXcds;
-        if (pre.size() >= kXcdOrderMinRounds * C8) {
-            std::vector<TileRec> out(pre.size());
-            for (size_t base = 0; base < pre.size(); base += C8) {
-                const size_t M = std::min(C8, pre.size() - base);
-                const size_t c = M / kXcds;  // a last, partial chunk keeps its remainder in order
-                for (size_t q = 0; q < M; ++q) {
-                    const size_t dst = q < c * kXcds ? base + kXcds * (q % c) + q / c : base + q;
-                    out[dst] = pre[base + q];
-                }
-            }
-            pre.swap(out);
-        }
-    }
     if (dec.size() > size_t(INT32_MAX) || pre.size() > size_t(INT32_MAX))
         return fail(SANGAM_ERR_INVALID_ARG, "batch too large");
+    // XCD-aware order (xcd_order.h) of a long prefill-shaped launch, in chunks
+    // of the launch's slots: each XCD's work-groups stream the same K/V at once
+    // and share it in L2 (prefill-heavy: 46 % less traffic beyond L2, time
+    // unchanged). Only with at least kXcdOrderMinRounds rounds of tiles per
+    // slot: in a shorter launch the chunks split the longest-first balance
+    // unevenly across XCDs.
+    if (const int chunk = xcd_plan_chunk(int64_t(pre.size()), prefill_rows, num_cus)) {
+        std::vector<TileRec> out(pre.size());
+        for (size_t k = 0; k < pre.size(); ++k) out[size_t(xcd_place(int(k), int(pre.size()), chunk))] = pre[k];
+        pre.swap(out);
+    }
 
     bool separate = false;
     if (qw == 1 && !dec.empty() && !pre.empty()) {
