@@ -356,6 +356,35 @@ def test_listed_positions(dev, fmt, hq, hkv, d):
     run_case(wl, dev, fmt, force_kv_splits=3)
 
 
+def listed_decodes(hq, hkv, d, prefills=()):
+    """Decodes of listed positions beside block decodes: few and many rows, within a page and far apart, at the ends of the
+    context and of pages, across 64-key stages that hold none."""
+    rng = np.random.default_rng(hq + d)
+    pos = [(np.sort(rng.choice(n, min(32, r), replace=False)), n) for n, r in ((300, 32), (1100, 17), (700, 32), (40, 9), (1500, 2))]
+    pos += [([0, 33], 34), ([15, 16, 63, 64, 127, 128, 191], 192), ([5, 900], 901), (np.r_[0:16, 500:516], 600), ([70], 71)]
+    return workloads.make_workload("listed", 9, hq=hq, hkv=hkv, d=d, decodes=[(40, 300), (200, 1100)], prefills=list(prefills), pos_decodes=pos)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group", range(1, 9))
+def test_listed_positions_in_decode_tiles(dev, fmt, group, d):
+    """The tiles of every group size, whose staging differs, whole and split."""
+    for splits in (0, 3):
+        p, *_ = run_case(listed_decodes(2 * group, 2, d), dev, fmt, num_cus=8, force_kv_splits=splits)
+        assert p.info.num_decode_tiles > 0 and p.info.num_fused_decode_tiles == 0 and p.info.decode_q_waves == group
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("hq,hkv,d,prefills", [(8, 8, 128, [1300, 1025]), (8, 8, 128, [333]), (8, 8, 64, [400, 77]), (14, 2, 128, [333]), (8, 2, 64, [400])])
+def test_listed_positions_beside_prefills(dev, fmt, hq, hkv, d, prefills):
+    p, *_ = run_case(listed_decodes(hq, hkv, d, prefills), dev, fmt)
+    assert p.launches()[:2] == (True, False)  # with MHA decodes in one launch, groups fused into the prefills' tiles
+    assert (p.info.num_decode_tiles > 0) == (hq == hkv) and (p.info.num_fused_decode_tiles > 0) == (hq != hkv)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("hq,hkv,d,decodes,prefills", [
