@@ -18,7 +18,17 @@
  *   SANGAM_ROPE_YARN    g f_j + (1 - g) f_j / s, g = (t - beta_slow) /
  *                       (beta_fast - beta_slow) clipped to [0, 1], t =
  *                       original_len f_j / 2 pi the turns of the pair over the
- *                       original length; m = 0.1 ln(s) + 1 (Peng et al., 2023)
+ *                       original length; m = 0.1 ln(s) + 1 (Peng et al., 2023,
+ *                       by the paper's equations)
+ *   SANGAM_ROPE_YARN_INDEX  the same with another ramp, linear in the pair and
+ *                       not in its turns: g = (hi - j) / (hi - lo) clipped to
+ *                       [0, 1], lo = max(0, floor(i(beta_fast))) and hi =
+ *                       min(R - 1, ceil(i(beta_slow))), i(t) = R ln(original_len
+ *                       / 2 pi t) / (2 ln base) the index at which a pair turns
+ *                       t times (a step behind lo where hi = lo). It is the one
+ *                       that released YaRN checkpoints are trained and served
+ *                       with; rates between the two ends differ (R 128, base
+ *                       10^6, original_len 32768, s 4: 16 pairs, by up to 1.7)
  * m is 1 otherwise, and `magnitude` in either case where that is not 0.
  *
  * Angles are exact to about 2^-52 of themselves (products in 64 bits, reduced
@@ -40,6 +50,7 @@ extern "C" {
 #define SANGAM_ROPE_LINEAR 1
 #define SANGAM_ROPE_NTK 2
 #define SANGAM_ROPE_YARN 3
+#define SANGAM_ROPE_YARN_INDEX 4
 
 #define SANGAM_DTYPE_BF16 0
 #define SANGAM_DTYPE_FP16 1
@@ -52,10 +63,10 @@ typedef struct sangam_rope_desc {
     int32_t reserved;    /* 0 */
     double base;         /* > 1 */
     double factor;       /* s >= 1; read unless scaling is SANGAM_ROPE_NONE */
-    double original_len; /* > 0; SANGAM_ROPE_YARN */
-    double beta_fast;    /* > beta_slow; SANGAM_ROPE_YARN (32 in the paper) */
-    double beta_slow;    /* >= 0; SANGAM_ROPE_YARN (1 in the paper) */
-    double magnitude;    /* m, or 0: 0.1 ln(s) + 1 with SANGAM_ROPE_YARN, else 1 */
+    double original_len; /* > 0; both SANGAM_ROPE_YARN (_INDEX: so long that hi >= lo) */
+    double beta_fast;    /* > beta_slow; both SANGAM_ROPE_YARN (32 in the paper) */
+    double beta_slow;    /* >= 0; both SANGAM_ROPE_YARN (1 in the paper) */
+    double magnitude;    /* m, or 0: 0.1 ln(s) + 1 with both SANGAM_ROPE_YARN, else 1 */
 } sangam_rope_desc;
 
 /*

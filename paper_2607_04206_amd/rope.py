@@ -14,7 +14,7 @@ from . import _lib
 from ._lib import RopeDesc, RopeTensor, check, lib
 from .kvq import _launch, _new, _on_device, _stream
 
-SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "yarn_index": 4}
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
@@ -42,9 +42,11 @@ def plan(*, rot_dim: int, interleaved: bool = False, base: float = 10000.0, scal
          original_len: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0, magnitude: Optional[float] = None,
          device=None) -> RopePlan:
     """sangam_rope_plan: the rates of rot_dim / 2 pairs (host only). scaling:
-    "none", "linear", "ntk" or "yarn", by `factor` beyond original_len
-    positions; magnitude: the factor on cos and sin, by default the scaling's
-    own. With ``device`` the blob is also copied to that device."""
+    "none", "linear", "ntk", "yarn" or "yarn_index", by `factor` beyond
+    original_len positions; magnitude: the factor on cos and sin, by default the
+    scaling's own. "yarn" is the paper's ramp, in the turns of a pair;
+    checkpoints released with YaRN scaling take "yarn_index", in its index. With
+    ``device`` the blob is also copied to that device."""
     if scaling not in SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(SCALINGS)}, got {scaling!r}")
     if magnitude is not None and not magnitude > 0:

@@ -72,6 +72,47 @@ def test_rates(rot, scale):
     assert p.host[24:28].view(np.float32)[0] == np.float32(m)
 
 
+def index_rates(rot, base, original_len, factor, beta_fast=32.0, beta_slow=1.0):
+    """f_j of YaRN scaling by index from its formula: the pair's own rate up to index lo, a factor-th from hi on, linear between."""
+    at = lambda turns: rot * math.log(original_len / (2 * math.pi * turns)) / (2 * math.log(base))  # noqa: E731
+    lo = max(0, math.floor(at(beta_fast)))
+    hi = rot - 1 if beta_slow == 0 else min(rot - 1, math.ceil(at(beta_slow)))
+    j = np.arange(rot // 2)
+    share = np.clip((j - lo) / max(hi - lo, 1e-3), 0, 1)  # of the stretched rate
+    f = base ** (-2.0 * j / rot)
+    return f * (1 - share) + f / factor * share, lo, hi
+
+
+INDEXED = [dict(rot=128, base=1e6, original_len=32768.0, factor=4.0), dict(rot=128, base=1e4, original_len=4096.0, factor=16.0),
+           dict(rot=64, base=5e5, original_len=8192.0, factor=8.0), dict(rot=128, base=1e4, original_len=256.0, factor=2.0),
+           dict(rot=32, base=1e4, original_len=4096.0, factor=40.0, beta_fast=8.0, beta_slow=0.0), dict(rot=8, base=1e4, original_len=6.0, factor=3.0)]
+
+
+@pytest.mark.parametrize("c,lo,hi", zip(INDEXED, (23, 20, 9, 1, 7, 0), (40, 46, 18, 26, 31, 0)))
+def test_rates_of_released_checkpoints(c, lo, hi):
+    """YaRN scaling as released checkpoints have it: the ramp is linear in the pair's index between two whole numbers."""
+    f, *ends = index_rates(**c)
+    assert ends == [lo, hi]
+    scale = {**c, "rot_dim": c["rot"]}
+    del scale["rot"]
+    p = rope.plan(scaling="yarn_index", **scale)
+    assert np.allclose(p.host[256:].view(np.float64), f / (2 * math.pi), rtol=1e-14, atol=0)
+    assert p.host[24:28].view(np.float32)[0] == np.float32(0.1 * math.log(c["factor"]) + 1)
+    paper = rope.plan(scaling="yarn", **scale).host[256:].view(np.float64) * 2 * math.pi
+    same = np.isclose(paper, f, rtol=1e-12, atol=0)
+    if c["rot"] > 32:  # (pairs up to lo keep their rates in both; over 6 positions none of the paper's does)
+        assert same[:lo + 1].all() and not same.all()
+    if c == INDEXED[0]:
+        assert (~same).sum() == 16 and (paper / f).min() == pytest.approx(0.58, abs=0.01)
+
+
+def test_yarn_by_index_refuses():
+    for bad in (dict(original_len=0.0), dict(original_len=1e-3), dict(beta_slow=32.0), dict(beta_slow=-1.0), dict(factor=0.5), dict(original_len=float("nan"))):
+        with pytest.raises(_lib.SangamError) as e:
+            rope.plan(rot_dim=64, scaling="yarn_index", **{**dict(factor=2.0, original_len=4096.0), **bad})
+        assert e.value.status == -1 and str(e.value)
+
+
 @pytest.mark.parametrize("bad", [dict(rot_dim=0), dict(rot_dim=7), dict(rot_dim=514), dict(rot_dim=-2), dict(base=1.0), dict(base=float("nan")),
                                  dict(base=float("inf")), dict(scaling="linear", factor=0.5), dict(scaling="linear", factor=float("nan")),
                                  dict(scaling="ntk", factor=2.0, rot_dim=2), dict(scaling="yarn", factor=2.0),
@@ -217,6 +258,22 @@ def test_scalings_at_far_positions(dev, scale):
     for got, x in zip(rope.rotate(p, q, k, pos), (q, k)):
         check(got[torch.from_numpy(near).to(dev)], x[torch.from_numpy(near).to(dev)], pos[torch.from_numpy(near).to(dev)], 128, False, **scale)
         assert torch.isfinite(got).all()
+
+
+@pytest.mark.gpu
+def test_yarn_by_index(dev):
+    """To the bar of an element (above), in fp32."""
+    c = INDEXED[1]
+    q, k, pos = inputs(40, 4, 2, 128, torch.float32, dev, far=65536)
+    p = rope.plan(rot_dim=128, scaling="yarn_index", base=c["base"], original_len=c["original_len"], factor=c["factor"], device=dev)
+    m = 0.1 * math.log(c["factor"]) + 1
+    angle = pos.cpu().numpy()[:, None, None] * index_rates(**c)[0]
+    for got, x in zip(rope.rotate(p, q, k, pos), (q, k)):
+        x = x.double().cpu().numpy()
+        z = (x[..., :64] + 1j * x[..., 64:]) * np.exp(1j * angle) * m
+        want = np.concatenate([z.real, z.imag], -1)
+        bar = 2.0 ** -21 * m * np.tile(np.abs(x[..., :64]) + np.abs(x[..., 64:]), 2) + 2.0 ** -24 * np.abs(want)
+        assert (np.abs(got.double().cpu().numpy() - want) <= bar).all()
 
 
 @pytest.mark.gpu
