@@ -78,9 +78,31 @@ def _expect(t: torch.Tensor, name: str, shape, dtype, dev) -> None:
 
 def _tensor(t: torch.Tensor, out: torch.Tensor, name: str, heads: int) -> RopeTensor:
     (row, head, dim), (out_row, out_head, out_dim) = t.stride(), out.stride()
-    if (dim != 1 or out_dim != 1) and t.shape[2] > 1:
+    if (dim != 1 or out_dim != 1) and t.shape[2] > 1 and t.numel() > 0:
         raise ValueError(f"the dims of a head of {name} and of its output must be consecutive")
     return RopeTensor(t.data_ptr(), out.data_ptr(), row, head, out_row, out_head, heads, 0)
+
+
+class _Rotate(torch.autograd.Function):
+    """rotate for inputs that require gradients, which the transpose gives."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, p, transpose, stream):
+        ctx.save_for_backward(positions)
+        ctx.plan, ctx.transpose = p, transpose
+        ctx.set_materialize_grads(False)
+        out = rotate(p, q, k, positions, transpose=transpose, stream=stream)
+        ctx.mark_non_differentiable(*(y for x, y in zip((q, k), out) if x is not None and not x.requires_grad))
+        return out
+
+    @staticmethod
+    def backward(ctx, *grads):
+        # (on the current stream, on which autograd orders both ends)
+        positions, = ctx.saved_tensors
+        need = [g is not None and n for g, n in zip(grads, ctx.needs_input_grad)]
+        grads = [(g if g.stride(-1) == 1 else g.contiguous()) for g, n in zip(grads, need) if n]
+        got = iter(rotate(ctx.plan, grads[0], grads[1] if len(grads) > 1 else None, positions, transpose=not ctx.transpose) if grads else ())
+        return (*(next(got) if n else None for n in need), None, None, None, None)
 
 
 def rotate(p: RopePlan, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor,
@@ -91,11 +113,17 @@ def rotate(p: RopePlan, q: torch.Tensor, k: Optional[torch.Tensor], positions: t
     heads may lie anywhere (views of a fused projection), rotated at positions,
     int32 [rows] on the device. Allocates the outputs with torch when they are
     not passed; q_out=q and k_out=k rotate in place. transpose gives the
-    gradient with respect to q and k from that of the outputs."""
+    gradient with respect to q and k from that of the outputs. Where q or k
+    requires gradients (and they are enabled), autograd gets them so; outputs
+    that are passed are then refused, as nothing would record them."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in DTYPES:
         raise TypeError("q must be a torch.Tensor [rows, heads, D] of bfloat16, float16 or float32")
     dev, dtype = q.device, q.dtype
     s = _stream(dev, stream)
+    if torch.is_grad_enabled() and (q.requires_grad or (isinstance(k, torch.Tensor) and k.requires_grad)):
+        if q_out is not None or k_out is not None:
+            raise ValueError("q_out and k_out record no gradients, which q or k requires: pass neither, or call under torch.no_grad()")
+        return _Rotate.apply(q, k, positions, p, transpose, stream)
     rows, heads, d = q.shape
     if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32:
         raise TypeError("positions must be an int32 tensor")

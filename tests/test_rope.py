@@ -391,6 +391,84 @@ def test_gradient(dev):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("transpose", [False, True])
+def test_autograd(dev, dtype, transpose):
+    """Outputs are the bits of a call without gradients, and q and k get the transpose's: to its bar (above) from the formula, for
+    gradients in any layout, of one tensor or both."""
+    q, k, pos = inputs(33, 4, 2, 64, dtype, dev)
+    gq, gk, _ = inputs(33, 4, 2, 64, dtype, dev, seed=50)
+    p = rope.plan(rot_dim=48, device=dev)
+    want = rope.rotate(p, q, k, pos, transpose=transpose)
+    assert not want[0].requires_grad
+    q.requires_grad_(), k.requires_grad_()
+    with torch.no_grad():
+        assert not rope.rotate(p, q, k, pos, transpose=transpose)[0].requires_grad
+    for stream in (None, torch.cuda.Stream(dev)):
+        torch.cuda.synchronize()
+        out = rope.rotate(p, q, k, pos, transpose=transpose, stream=stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        wide = torch.stack([gq, gq], -1)[..., 0]  # dims two elements apart
+        for grads in ((gq, gk), (wide, gk)):
+            for d, g in zip(torch.autograd.grad(out, (q, k), grads, retain_graph=True), (gq, gk)):
+                check(d, g, pos, 48, False, transpose=not transpose)
+        d, none = torch.autograd.grad(out[0], (q, k), gq, retain_graph=True, allow_unused=True)
+        check(d, gq, pos, 48, False, transpose=not transpose)
+        assert none is None
+        check(torch.autograd.grad(out[1], k, gk)[0], gk, pos, 48, False, transpose=not transpose)
+    # one tensor that requires none, one alone, none of the rows
+    out = rope.rotate(p, q.detach(), k, pos, transpose=transpose)
+    assert not out[0].requires_grad
+    check(torch.autograd.grad(out[1], k, gk)[0], gk, pos, 48, False, transpose=not transpose)
+    out = rope.rotate(p, q, None, pos, transpose=transpose)
+    assert out[1] is None
+    ones = torch.ones_like(gq)
+    check(torch.autograd.grad(out[0].sum(), q)[0], ones, pos, 48, False, transpose=not transpose)  # (an expanded gradient)
+    assert torch.autograd.grad(rope.rotate(p, q[:0], None, pos[:0])[0].sum(), q)[0].abs().max() == 0
+    # views of one projection, and the gradient's own gradient
+    x = torch.cat([q, k, k], 1).detach().requires_grad_()
+    a, b = rope.rotate(p, x[:, :4], x[:, 4:6], pos, transpose=transpose)
+    dx, = torch.autograd.grad((a * gq).sum() + (b * gk).sum(), x)
+    check(dx[:, :4], gq, pos, 48, False, transpose=not transpose)
+    check(dx[:, 4:6], gk, pos, 48, False, transpose=not transpose)
+    assert not dx[:, 6:].any()
+    g = gq.clone().requires_grad_()
+    dq, = torch.autograd.grad(rope.rotate(p, q, None, pos, transpose=transpose)[0], q, g, create_graph=True)
+    check(torch.autograd.grad(dq, g, gq)[0], gq, pos, 48, False, transpose=transpose)
+    for kw in (dict(q_out=torch.empty_like(q)), dict(k_out=k.detach()), dict(q_out=q, k_out=k)):
+        with pytest.raises(ValueError, match="gradients"):
+            rope.rotate(p, q, k, pos, **kw)
+    with torch.no_grad():
+        rope.rotate(p, q, k, pos, q_out=torch.empty_like(q))
+
+
+@pytest.mark.gpu
+def test_autograd_in_a_graph(dev):
+    """Forward and backward captured together, replayed at other positions."""
+    q, k, pos = inputs(50, 4, 2, 64, torch.bfloat16, dev)
+    gq, gk, _ = inputs(50, 4, 2, 64, torch.bfloat16, dev, seed=50)
+    p = rope.plan(rot_dim=64, device=dev)
+    s = torch.cuda.Stream(dev)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):  # leaves that only this stream knows
+        leaves = [x.clone().requires_grad_() for x in (q, k)]
+        torch.autograd.grad(rope.rotate(p, *leaves, pos), leaves, (gq, gk))
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out = rope.rotate(p, *leaves, pos)
+        grads = torch.autograd.grad(out, leaves, (gq, gk))
+    for _ in range(4):
+        pos.add_(17)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        want = rope.rotate(p, q, k, pos), rope.rotate(p, gq, gk, pos, transpose=True)
+        assert all(torch.equal(a, b) for a, b in zip((*out, *grads), (*want[0], *want[1])))
+
+
+@pytest.mark.gpu
 def test_streams_and_graphs(dev):
     q, k, pos = inputs(100, 8, 2, 128, torch.bfloat16, dev)
     p = rope.plan(rot_dim=128, device=dev)
