@@ -97,7 +97,8 @@ typedef struct sangam_rope_tensor {
  * plan_host is the plan in host memory, plan_dev the same bytes in device
  * memory. head_dim is R to 512; rows 0 or more; dtype a SANGAM_DTYPE_*;
  * transpose 0 or 1.
- * Strides are 2^40 at most, rows and heads times theirs 2^48.
+ * Strides are 2^40 at most, rows and heads times theirs 2^48; the stride of a
+ * single row or head is not read.
  * Errors: SANGAM_ERR_PLAN, SANGAM_ERR_INVALID_ARG (a NULL pointer, a size or
  * stride out of range), SANGAM_ERR_UNSUPPORTED (dtype), SANGAM_ERR_ALIGN (a
  * pointer not aligned to its elements), SANGAM_ERR_HIP. An output that may

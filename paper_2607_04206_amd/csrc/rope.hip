@@ -299,9 +299,14 @@ sangam_status rotate(const void* plan_host, const void* plan_dev, const sangam_r
     bool in_place = true, any_in_place = false;
     RopeArgs args{};
     int heads[2] = {0, 0};
+    sangam_rope_tensor tensors[2] = {};
     for (int i = 0; i < 2; ++i) {
-        const sangam_rope_tensor* t = i ? k : q;
-        if (!t) continue;
+        if (!(i ? k : q)) continue;
+        sangam_rope_tensor* t = &tensors[i];
+        *t = i ? *k : *q;
+        // the step of a single row or head leads nowhere
+        if (rows <= 1) t->in_row_stride = t->out_row_stride = 0;
+        if (t->heads == 1) t->in_head_stride = t->out_head_stride = 0;
         if (t->heads < 1 || t->heads > (1 << 16)) return fail(SANGAM_ERR_INVALID_ARG, "heads must be 1 to 2^16");
         heads[i] = t->heads;
         if (rows == 0) continue;

@@ -205,6 +205,21 @@ def test_overlaps_are_refused():
     assert _refused(x.transpose(0, 1).contiguous().transpose(0, 1), x[:, :6], x, x) and not _refused(x[:1], y[:1], x[1:2], y[1:2])
 
 
+def test_strides_of_single_rows_and_heads_are_not_read():
+    # what passes the checks of the tensors fails for the missing plan_dev
+    p = rope.plan(rot_dim=64)
+
+    def call(rows, **over):
+        st = _lib.lib.sangam_rope_rotate(p.host_ptr(), None, ctypes.byref(_tensor(**over)), None, 64, 0, 4096, rows, 0, None)
+        return st, b"plan_dev" in _lib.lib.sangam_last_error()
+    for stride in (0, 3, 999, -1, 1 << 60):
+        assert call(1, out_row_stride=stride) == call(1, in_row_stride=stride) == (-1, True)
+        assert call(10, heads=1, out_head_stride=stride) == call(10, heads=1, in_head_stride=stride) == (-1, True)
+        assert call(10, out_row_stride=stride)[1] == call(10, in_head_stride=stride)[1] is False
+    x = torch.zeros(10, 6, 8)
+    assert not _refused(x[:1], x[:1].reshape(1, 48).view(1, 6, 8)) and _refused(x[:1, :4], x[:1, 2:6]) and not _refused(x[:1, :3], x[:1, 3:])
+
+
 # ------------------------------------------------------------------------ GPU
 @pytest.fixture(scope="module")
 def dev():
@@ -319,6 +334,21 @@ def test_strides(dev, interleaved):
     assert none is None and torch.equal(got, want[0][:, :1].expand(rows, 4, d))
     same_row = q[:1].expand(rows, h, d)
     check(rope.rotate(p, same_row, None, pos)[0], same_row, pos, d, interleaved)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_single_rows_and_heads(dev, interleaved):
+    """Their odd strides change nothing, in place either."""
+    for rows, h in ((1, 6), (40, 1), (1, 1)):
+        q, k, pos = inputs(rows, h, h, 128, torch.bfloat16, dev)
+        p = rope.plan(rot_dim=128, interleaved=interleaved, device=dev)
+        want = rope.rotate(p, q, k, pos)
+        strides = (13 if rows == 1 else h * 128, 7 if h == 1 else 128, 1)
+        odd = [x.as_strided(x.shape, strides) for x in (q, k)]
+        assert all(torch.equal(a, b) for a, b in zip(rope.rotate(p, *odd, pos), want))
+        rope.rotate(p, q, k, pos, q_out=odd[0], k_out=odd[1])
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1])
 
 
 @pytest.mark.gpu
