@@ -139,6 +139,20 @@ def test_plan_refuses_in_python_and_by_size():
     assert f(ctypes.byref(d), None, 0, ctypes.byref(used)) == -1
 
 
+def test_entries_without_memory(tmp_path, monkeypatch):
+    """An exception in a C entry becomes a status of its own and a message, and plan() takes it for no size."""
+    if shutil.which("g++"):
+        exe = str(tmp_path / "driver")
+        subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", os.path.join(os.path.dirname(os.path.abspath(__file__)), "sanitize", "entry_driver.cpp"),
+                        "-o", exe], check=True)
+        r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+        assert r.returncode == 0, r.stdout
+    monkeypatch.setattr(rope.lib, "sangam_rope_plan", lambda *a: -9)
+    with pytest.raises(_lib.SangamError) as e:
+        rope.plan(rot_dim=64)
+    assert e.value.status == -9
+
+
 def _tensor(**over):
     t = dict(in_=4096, out=4096, in_row_stride=256, in_head_stride=64, out_row_stride=256, out_head_stride=64, heads=4, reserved=0)
     t.update(over)
