@@ -31,9 +31,11 @@
  *                       10^6, original_len 32768, s 4: 16 pairs, by up to 1.7)
  * m is 1 otherwise, and `magnitude` in either case where that is not 0.
  *
- * Angles are exact to about 2^-52 of themselves (products in 64 bits, reduced
- * there), the rotation is done in fp32 and rounded once. Positions are any
- * int32, in any order.
+ * Rates and angles are computed in 64 bits, and turns reduced there: an angle is
+ * off by a few 2^-53 of itself where R is a power of two, by ln(base) 2^-53 more
+ * elsewhere, and with both YARN by up to s 2^-50 (at 2^31 positions the fastest
+ * pair is off by 2^-20 rad). The rotation is done in fp32 and rounded once.
+ * Positions are any int32, in any order.
  *
  * Ownership and errors: as in sangam_attn.h.
  */

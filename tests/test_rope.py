@@ -290,6 +290,40 @@ def test_scalings_at_far_positions(dev, scale):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("scale", SCALES)
+def test_furthest_positions(dev, scale):
+    """Positions from 2^28 on, whose angles in float64 are off by more than the bar of an element allows, against 80-bit ones.
+    Errors of an angle, in 2^-53 of itself: pow() 2, the constant 2 pi 0.4, the quotient by it 1, the product with the position 1,
+    and a factor 1: below 8. NTK's base adds 5.1 (its power of the factor 4.1, its product 1): below 16. YaRN's share g is off
+    by up to 3.3 times turns / (beta_fast - beta_slow), at most 1.1, and f by the factor times that where g is small: below 8 factors."""
+    if np.finfo(np.longdouble).nmant < 63:
+        pytest.skip("needs an 80-bit long double")
+    q, k, _ = inputs(7, 4, 2, 128, torch.float32, dev)
+    pos = torch.tensor([1 << 28, (1 << 28) + 1, (1 << 30) - 7, 2 ** 31 - 1, -2 ** 31, -2 ** 29 - 3, 1234567891], dtype=torch.int32, device=dev)
+    p = rope.plan(rot_dim=128, device=dev, **scale)
+    L, kind, s = np.longdouble, scale.get("scaling", "none"), scale.get("factor", 1.0)
+    two_pi, j = 8 * np.arctan(L(1)), np.arange(64, dtype=L)
+    base = L(scale.get("base", 10000.0)) * (L(s) ** (L(128) / 126) if kind == "ntk" else 1)
+    f, m = base ** (-2 * j / 128), L(scale.get("magnitude") or (1 + L(0.1) * np.log(L(s)) if kind == "yarn" else 1))
+    if kind == "linear":
+        f = f / L(s)
+    elif kind == "yarn":
+        fast, slow = L(scale.get("beta_fast", 32.0)), L(scale.get("beta_slow", 1.0))
+        g = np.clip((L(scale["original_len"]) * f / two_pi - slow) / (fast - slow), 0, 1)
+        f = g * f + (1 - g) * f / L(s)
+    angle = pos.cpu().numpy().astype(L)[:, None, None] * f
+    off = 2.0 ** -53 * {"ntk": 16, "yarn": 8 * s}.get(kind, 8) * np.abs(angle).astype(np.float64)
+    for got, x in zip(rope.rotate(p, q, k, pos), (q, k)):
+        x = x.double().cpu().numpy()
+        lo, hi = x[..., :64], x[..., 64:]
+        c, t = np.cos(angle) * m, np.sin(angle) * m
+        want = np.concatenate([lo * c - hi * t, hi * c + lo * t], -1).astype(np.float64)
+        bar = np.tile(float(m) * (np.abs(lo) + np.abs(hi)) * (2.0 ** -21 + off), 2) + 2.0 ** -24 * np.abs(want)
+        assert (np.abs(got.double().cpu().numpy() - want) <= bar).all()
+        assert off[:, :, 32:].max() < 2.0 ** -22 * (4 * s if kind == "yarn" else 1)  # half of the pairs to 2^-22 rad
+
+
+@pytest.mark.gpu
 def test_yarn_by_index(dev):
     """To the bar of an element (above), in fp32."""
     c = INDEXED[1]
