@@ -61,7 +61,8 @@ typedef struct sangam_kvq_cache {
  * k_new / v_new, unquantised. One call, the same launches. The LSE is that of
  * unrounded softmax weights. Outputs that an infinity or a NaN reaches are
  * infinite or NaN. events: NULL, or the six of
- * sangam_attn_forward_timed.
+ * sangam_attn_forward_timed. (No form of it takes split partials to a library
+ * array as sangam_attn_forward_noalloc does: the workspace is the caller's.)
  * Errors: as sangam_attn_forward, SANGAM_ERR_INVALID_ARG for a NULL cache, and
  * SANGAM_ERR_UNSUPPORTED for an unknown format.
  */

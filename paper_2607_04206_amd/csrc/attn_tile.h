@@ -1178,6 +1178,10 @@ __device__ __forceinline__ void attn_tile(const typename Cache::Args& a, const T
     // in the lower half-wave and the full one in the upper one. O is divided by
     // the former, so that it is an average of V's rows (equal rows give
     // themselves); the LSE, by which splits are weighed, is that of the latter.
+    // (The second sum: 48 decodes of 28/4 heads e4m3 39.2 -> 40.6 us, prefills of
+    // 2304 and 3328 rows of them 244 -> 250, both in one launch 276 -> 285; 16 MHA
+    // decodes beside prefills of 1819 and 1201 rows 165 -> 167.6, MHA decodes alone
+    // nothing.)
     if constexpr (QUANT && !SOLO)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) l_run[qb] = half_sums(l_run[qb], l_full[qb]);

@@ -103,7 +103,9 @@ __device__ __forceinline__ void put(void* p, V v) {
 // what it reads of its neighbour may be rotated already, it writes its own
 // elements only. 4748 rows of 28 + 4 heads of 128 dims, 126 of them rotated, fp16:
 // one element at a time 48.5 us, so 22.9, in place 38.9 and 22.8; 15,000 of 32 + 8 heads
-// of 64, 18 rotated, bf16: 118.6 and 47.0, in place 34.0 and 29.8.
+// of 64, 18 rotated, bf16: 118.6 and 47.0, in place 34.0 and 29.8. (Twice what the
+// bytes take: most vectors cross a line of 128 bytes, dims that only pass are
+// units of their own, and the stores are plain ones at every size.)
 template <typename T, int V, bool INTERLEAVED, bool STREAM, bool EDGES>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     typedef T Vec __attribute__((ext_vector_type(V)));
