@@ -31,8 +31,8 @@ SANGAM_HD inline int xcd_entry(int place, int n, int chunk) {
 
 // Chunk of the order that the planner gave n tiles (the launch's slots), or 0: in list order.
 inline int xcd_plan_chunk(int64_t n, int prefill_rows, int cus) {
-    const int slots = (cus / kXcds > 1 ? cus / kXcds : 1) * (prefill_rows == kWidePrefillRows ? 1 : 2) * kXcds;
-    return n >= int64_t(kXcdOrderMinRounds) * slots ? slots : 0;
+    const int64_t slots = int64_t(cus / kXcds > 1 ? cus / kXcds : 1) * (prefill_rows == kWidePrefillRows ? 1 : 2) * kXcds;
+    return n >= kXcdOrderMinRounds * slots ? int(slots) : 0;  // (n counts as int)
 }
 
 // A mixed launch's prefill block `index` of n, in rounds of `round`: the tile

@@ -43,6 +43,16 @@ def test_every_block_once(blocks, rows):
         assert np.array_equal(np.sort(got), want), (tiles, cus)
 
 
+@pytest.mark.parametrize("cus", [1 << 28, 1 << 30, 2 ** 31 - 1])
+def test_plans_for_any_number_of_cus(blocks, cus):
+    for rows, wide in ((128, 1), (256, 2)):
+        chunk, got = blocks(70, rows, cus)
+        assert chunk == 0 and np.array_equal(np.sort(got), np.arange(70 * wide) * (2 // wide))
+    wl = workloads.make_workload("cus", 1, hq=4, hkv=4, d=64, decodes=[(30, 100)], prefills=[300, 70])
+    few, many = plan_of(wl), plan_of(wl, num_cus=cus)
+    assert few.info.num_prefill_tiles == many.info.num_prefill_tiles
+
+
 # a short launch, long ones that the planner orders (of 256 and 128 rows a tile)
 @pytest.mark.parametrize("prefills,d,ordered,heads", [([1819, 1201], 128, False, 4.5), ([900] * 16, 128, True, 8.8),
                                                       ([3400] * 5, 128, True, 2.8), ([3400] * 5, 64, True, 2.2), ([900] * 16, 64, True, 8.8)])
