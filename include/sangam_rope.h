@@ -22,8 +22,8 @@
  *                       by the paper's equations)
  *   SANGAM_ROPE_YARN_INDEX  the same with another ramp, linear in the pair and
  *                       not in its turns: g = (hi - j) / (hi - lo) clipped to
- *                       [0, 1], lo = max(0, floor(i(beta_fast))) and hi =
- *                       min(R - 1, ceil(i(beta_slow))), i(t) = R ln(original_len
+ *                       [0, 1], lo = floor(i(beta_fast)) within [0, R - 1] and
+ *                       hi = min(R - 1, ceil(i(beta_slow))), i(t) = R ln(original_len
  *                       / 2 pi t) / (2 ln base) the index at which a pair turns
  *                       t times (a step behind lo where hi = lo). It is the one
  *                       that released YaRN checkpoints are trained and served

@@ -55,7 +55,7 @@ sangam_status rope_plan(const sangam_rope_desc* d, void* plan_buf, size_t cap, s
     double lo = 0.0, hi = 0.0;
     if (d->scaling == SANGAM_ROPE_YARN_INDEX) {
         auto index = [&](double turns) { return R * std::log(d->original_len / (two_pi * turns)) / (2.0 * std::log(d->base)); };
-        lo = std::fmax(0.0, std::floor(index(d->beta_fast)));
+        lo = std::fmin(double(R - 1), std::fmax(0.0, std::floor(index(d->beta_fast))));
         hi = std::fmin(double(R - 1), std::ceil(index(d->beta_slow)));
         if (!(hi >= lo)) return rope_fail(SANGAM_ERR_INVALID_ARG, "original_len is too short for YaRN scaling by index");
     }

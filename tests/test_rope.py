@@ -106,6 +106,13 @@ def test_rates_of_released_checkpoints(c, lo, hi):
         assert (~same).sum() == 16 and (paper / f).min() == pytest.approx(0.58, abs=0.01)
 
 
+@pytest.mark.parametrize("original_len", [1e9, 1e12])
+def test_yarn_by_index_of_long_lengths(original_len):
+    """Where every pair turns more than beta_fast times, all keep their rates."""
+    p = rope.plan(rot_dim=64, scaling="yarn_index", factor=4.0, original_len=original_len)
+    assert np.allclose(p.host[256:].view(np.float64), rates(64)[0] / (2 * math.pi), rtol=1e-14, atol=0)
+
+
 def test_yarn_by_index_refuses():
     for bad in (dict(original_len=0.0), dict(original_len=1e-3), dict(beta_slow=32.0), dict(beta_slow=-1.0), dict(factor=0.5), dict(original_len=float("nan"))):
         with pytest.raises(_lib.SangamError) as e:
