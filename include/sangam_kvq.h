@@ -58,11 +58,12 @@ typedef struct sangam_kvq_cache {
  * sangam_attn_forward over a quantised cache: the fresh rows are written into
  * the pages quantised, and every query row attends to the cached rows' values
  * and, as in sangam_attn_forward, to the item's own fresh rows as they are in
- * k_new / v_new, unquantised. One call, the same launches. The LSE is that of
- * unrounded softmax weights. Outputs that an infinity or a NaN reaches are
- * infinite or NaN. events: NULL, or the six of
- * sangam_attn_forward_timed. (No form of it takes split partials to a library
- * array as sangam_attn_forward_noalloc does: the workspace is the caller's.)
+ * k_new / v_new, unquantised. One call, the same launches. An output is an
+ * average of V's rows by softmax weights rounded to bf16; the LSE is that of
+ * unrounded ones. Outputs that an infinity or a NaN reaches are infinite or
+ * NaN. events: NULL, or the six of sangam_attn_forward_timed. (No form of it
+ * takes split partials to a library array as sangam_attn_forward_noalloc does:
+ * the workspace is the caller's.)
  * Errors: as sangam_attn_forward, SANGAM_ERR_INVALID_ARG for a NULL cache, and
  * SANGAM_ERR_UNSUPPORTED for an unknown format.
  */

@@ -88,10 +88,10 @@ class _Rotate(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, positions, p, transpose, stream):
+        out = rotate(p, q, k, positions, transpose=transpose, stream=stream)
         ctx.save_for_backward(positions)
         ctx.plan, ctx.transpose = p, transpose
         ctx.set_materialize_grads(False)
-        out = rotate(p, q, k, positions, transpose=transpose, stream=stream)
         ctx.mark_non_differentiable(*(y for x, y in zip((q, k), out) if x is not None and not x.requires_grad))
         return out
 

@@ -529,6 +529,18 @@ def test_autograd(dev, dtype, transpose):
 
 
 @pytest.mark.gpu
+def test_refusals_with_gradients(dev):
+    """The words of a call without them."""
+    q, k, pos = inputs(10, 4, 2, 64, torch.bfloat16, dev)
+    p = rope.plan(rot_dim=64, device=dev)
+    q.requires_grad_()
+    for err, a, words in ((TypeError, (q, k, pos.tolist()), "positions"), (TypeError, (q, k, None), "positions"), (ValueError, (q, k, pos[:9]), "positions"),
+                          (TypeError, (q, k.float(), pos), "k must"), (TypeError, (q, [k], pos), "k must"), (ValueError, (q, k[..., :32], pos), "k must")):
+        with pytest.raises(err, match=words):
+            rope.rotate(p, *a)
+
+
+@pytest.mark.gpu
 def test_autograd_in_a_graph(dev):
     """Forward and backward captured together, replayed at other positions."""
     q, k, pos = inputs(50, 4, 2, 64, torch.bfloat16, dev)
