@@ -65,7 +65,7 @@ typedef int32_t sangam_status;
 #define SANGAM_ERR_ALIGN (-6)       /* a tensor pointer not 16-byte aligned */
 #define SANGAM_ERR_HIP (-7)         /* a HIP runtime error during launch */
 #define SANGAM_ERR_PLAN (-8)        /* not a plan of this library version */
-#define SANGAM_ERR_MEMORY (-9)      /* host memory ran out (sangam_kvq.h, sangam_rope.h) */
+#define SANGAM_ERR_MEMORY (-9)      /* host memory ran out (sangam_kvq.h, sangam_rope.h, sangam_tables.h, sangam_sample.h) */
 
 /* Batch descriptor. All arrays are host memory, read only during the call. */
 typedef struct sangam_attn_desc {

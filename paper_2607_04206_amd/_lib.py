@@ -1,5 +1,6 @@
 """ctypes declarations of the C ABI in include/sangam_attn.h, sangam_sched.h,
-sangam_kv.h, sangam_kvq.h, sangam_rope.h and sangam_probe.h.
+sangam_kv.h, sangam_kvq.h, sangam_rope.h, sangam_tables.h, sangam_sample.h and
+sangam_probe.h.
 
 Loads the in-tree ``libsangam_attn.so``; there is no fallback: if the
 library is missing or does not load, importing this module raises.
@@ -27,6 +28,7 @@ STATUS_NAMES = {
     -6: "SANGAM_ERR_ALIGN",
     -7: "SANGAM_ERR_HIP",
     -8: "SANGAM_ERR_PLAN",
+    -9: "SANGAM_ERR_MEMORY",
 }
 
 EXPORTS = (
@@ -51,6 +53,11 @@ EXPORTS = (
     "sangam_kvq_import",
     "sangam_rope_plan",
     "sangam_rope_rotate",
+    "sangam_tables_resize",
+    "sangam_tables_build",
+    "sangam_sample_workspace_bytes",
+    "sangam_sample_tokens",
+    "sangam_sample_unmask",
     "sangam_probe_hbm_read",
     "sangam_probe_mfma_bf16",
 )
@@ -129,6 +136,68 @@ class RopeTensor(ctypes.Structure):
     ]
 
 
+class BlockTable(ctypes.Structure):
+    _fields_ = [
+        ("pages", ctypes.c_void_p),
+        ("row_stride", ctypes.c_int64),
+        ("requests", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+    ]
+
+
+class TablesBatch(ctypes.Structure):
+    _fields_ = [
+        ("num_items", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("request", ctypes.c_void_p),
+        ("kv_len", ctypes.c_void_p),
+        ("q_indptr", ctypes.c_void_p),
+        ("q_offset", ctypes.c_void_p),
+        ("q_pos", ctypes.c_void_p),
+    ]
+
+
+class SampleDesc(ctypes.Structure):
+    _fields_ = [
+        ("logits", ctypes.c_void_p),
+        ("rows", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+        ("vocab", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("u", ctypes.c_void_p),
+        ("params_of", ctypes.c_void_p),
+        ("num_params", ctypes.c_int64),
+        ("temperatures", ctypes.c_void_p),
+        ("top_ks", ctypes.c_void_p),
+        ("top_ps", ctypes.c_void_p),
+        ("min_ps", ctypes.c_void_p),
+        ("temperature", ctypes.c_float),
+        ("top_k", ctypes.c_int32),
+        ("top_p", ctypes.c_float),
+        ("min_p", ctypes.c_float),
+        ("confidence", ctypes.c_int32),
+        ("forbid", ctypes.c_int32),
+    ]
+
+
+class UnmaskDesc(ctypes.Structure):
+    _fields_ = [
+        ("tokens", ctypes.c_void_p),
+        ("confidence", ctypes.c_void_p),
+        ("ids", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p),
+        ("row_indptr", ctypes.c_void_p),
+        ("counts", ctypes.c_void_p),
+        ("thresholds", ctypes.c_void_p),
+        ("rows", ctypes.c_int64),
+        ("num_ids", ctypes.c_int64),
+        ("num_blocks", ctypes.c_int32),
+        ("mask_id", ctypes.c_int32),
+        ("count", ctypes.c_int32),
+        ("threshold", ctypes.c_float),
+    ]
+
+
 class PlanInfo(ctypes.Structure):
     _fields_ = [
         ("num_items", ctypes.c_int32),
@@ -202,6 +271,17 @@ def _load():
     lib.sangam_rope_plan.restype = ctypes.c_int32
     lib.sangam_rope_rotate.argtypes = [P, P, tensor, tensor, ctypes.c_int32, ctypes.c_int32, P, I64, ctypes.c_int32, P]
     lib.sangam_rope_rotate.restype = ctypes.c_int32
+    table = ctypes.POINTER(BlockTable)
+    lib.sangam_tables_resize.argtypes = [table, P, P, P, ctypes.c_int32, P, P, P]
+    lib.sangam_tables_resize.restype = ctypes.c_int32
+    lib.sangam_tables_build.argtypes = [table, ctypes.POINTER(TablesBatch), P, P, I64, P, P, P, I64, P]
+    lib.sangam_tables_build.restype = ctypes.c_int32
+    lib.sangam_sample_workspace_bytes.argtypes = [I64, ctypes.c_int32, ctypes.c_int32]
+    lib.sangam_sample_workspace_bytes.restype = S
+    lib.sangam_sample_tokens.argtypes = [ctypes.POINTER(SampleDesc), P, P, P, S, P]
+    lib.sangam_sample_tokens.restype = ctypes.c_int32
+    lib.sangam_sample_unmask.argtypes = [ctypes.POINTER(UnmaskDesc), P, P, P]
+    lib.sangam_sample_unmask.restype = ctypes.c_int32
     lib.sangam_probe_hbm_read.argtypes = [P, S, P, ctypes.c_int32, P]
     lib.sangam_probe_hbm_read.restype = ctypes.c_int32
     lib.sangam_probe_mfma_bf16.argtypes = [P, ctypes.c_int32, ctypes.c_int32, P]

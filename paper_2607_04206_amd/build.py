@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsangam_attn.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["plan.cpp", "sched.cpp", "kv_plan.cpp", "rope_plan.cpp", "attn_fwd.hip", "attn_quant.hip",
-           "kv_copy.hip", "kvq_copy.hip", "rope.hip", "probe.hip"]
+           "kv_copy.hip", "kvq_copy.hip", "rope.hip", "tables.hip", "sample.hip", "unmask.hip", "probe.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,0 +1,369 @@
+"""Sampling (include/sangam_sample.h, paper_2607_04206_amd/sample.py) against its
+definition in 64 bits on the host: filters and draws by rank order, confidences,
+ties, masked and infinite logits, odd sizes and strides, parameters a row or a
+request, refusals."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_04206_amd import _lib, sample
+
+INF = math.inf
+DTYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+def ranked(x, temperature, top_k=0, top_p=1.0, min_p=0.0):
+    """Tokens in rank order, the weights of the kept ones (0 behind them) and (x - X) / T of each; None: a row with nothing."""
+    x = np.asarray(x, np.float64)
+    x = np.where(np.isnan(x), -INF, x)
+    if x.max() == INF:
+        x = np.where(x == INF, 0.0, -INF)
+    if x.max() == -INF:
+        return None
+    order = np.argsort(-x, kind="stable")
+    with np.errstate(invalid="ignore", over="ignore"):
+        z = (x[order] - x.max()) / (temperature if temperature > 0 else 1.0)
+    z = np.where(x[order] == -INF, -INF, z)
+    w = np.exp(z)
+    n = np.arange(len(x))
+    if top_k > 0:
+        w = np.where(n < top_k, w, 0.0)
+    keep = np.cumsum(w) - w < top_p * w.sum() if top_p < 1 else np.ones(len(x), bool)
+    if min_p > 0:
+        keep &= z >= math.log(min_p)
+    return order, np.where(keep | (n == 0), w, 0.0), z
+
+
+def check(x, token, conf, u, temperature, kind, top_k=0, top_p=1.0, min_p=0.0, forbid=-1):
+    """One row's answer against the definition. Tokens are equal, but where the draw falls within 1e-9 of the border to the
+    token that came (weights are held to 2^-33, sums to 2^-44 of the largest weight a bin). Confidences: one rounding to 32 bits
+    (2^-24 of the value), weights to 2^-33, which the margin's difference and the entropy's factors (|t| up to 64 ln 2) keep as
+    2^-32 and 2^-27; where nothing filters and T is 0, weights in 32 bits: 2^-23 (1 + ln(2) |t|) each, weighted sums of |t| are
+    under log2(vocab) + 2 times the weights: 2^-19 at 2^18 tokens, and for the entropy that times 2 + log(vocab)."""
+    x = np.array(x, np.float64)
+    if forbid >= 0:
+        x[forbid] = -INF
+    got = ranked(x, temperature, top_k, top_p, min_p)
+    if got is None:
+        assert (token, conf) == (-1, 0.0)
+        return
+    order, w, z = got
+    total = w.sum()
+    place = int(np.flatnonzero(order == token)[0])
+    if temperature == 0:
+        assert place == 0, (token, order[0])
+    else:
+        up_to = np.cumsum(w)
+        target = min(max(u, 0.0), 1.0) * total
+        last = int((w > 0).sum()) - 1
+        want = min(int(np.searchsorted(up_to, target, side="right")), last)
+        if place != want:
+            border = up_to[min(place, want)]
+            assert w[place] > 0 and abs(border - target) <= 1e-9 * total and abs(place - want) <= max(1, int((w[min(place, want):max(place, want)] <= 1e-9 * total).sum()) + 1), \
+                (token, order[want], place, want, border / total, target / total)
+    if kind == "probability":
+        ref = w[place] / total
+    elif kind == "margin":
+        ref = (w[0] - (w[1] if len(w) > 1 else 0.0)) / total
+    else:
+        kept = w > 0
+        ref = float((w[kept] * z[kept]).sum() / total - math.log(total))
+    plain = temperature == 0 and not (0 < top_k < len(x)) and top_p >= 1 and min_p <= 0
+    if plain:
+        bar = 2.0 ** -19 * ((2 + math.log(len(x))) if kind == "entropy" else w[0] / total)
+    else:
+        bar = 2.0 ** -24 * (1 + 2.0 ** -6) * abs(ref) + {"probability": 2.0 ** -33 * w[place] / total, "margin": 2.0 ** -32, "entropy": 2.0 ** -27}[kind]
+    assert abs(conf - ref) <= bar, (kind, conf, ref, abs(conf - ref) / bar)
+
+
+def make(shape, how, dtype, gen):
+    rows, vocab = shape
+    n = lambda: torch.randn(shape, generator=gen)  # noqa: E731
+    if how == "normal":
+        x = 2.5 * n()
+    elif how == "peaked":
+        x = 2.0 * n()
+        x.scatter_(1, torch.randint(0, vocab, (rows, 8), generator=gen), 14.0 + n()[:, :1].expand(rows, 8))
+    elif how == "equal":
+        x = torch.full(shape, -3.25)
+    elif how == "near":  # within a bin or two of weights
+        x = 5.0 + 1e-3 * n()
+    elif how == "ties":
+        x = torch.round(2 * n())
+    elif how == "zeros":  # of both signs, among others
+        x = torch.where(n() > 0, 0.0, -0.0) - (n() > 1).float()
+    elif how == "wide":
+        x = n() * 10 ** (8 * torch.rand(shape, generator=gen) - 4 if dtype is torch.float16 else 60 * torch.rand(shape, generator=gen) - 25)
+    elif how == "masked":
+        x = torch.where(torch.rand(shape, generator=gen) < 0.9, -INF, 3 * n())
+    elif how == "holes":
+        x = 3 * n()
+        x = torch.where(torch.rand(shape, generator=gen) < 0.2, math.nan, x)
+        x = torch.where(torch.rand(shape, generator=gen) < 0.2, -INF, x)
+        x[0] = -INF
+        if rows > 1:
+            x[1] = math.nan
+        if rows > 2:
+            x[2] = torch.where(torch.rand((vocab,), generator=gen) < 0.3, INF, x[2])
+        if rows > 3:
+            x[3] = torch.finfo(dtype).min
+    elif how == "rising":
+        x = torch.linspace(-20, 12, vocab).expand(shape) + 0.01 * n()
+    return x.to(dtype)
+
+
+PARAMS = [dict(temperature=0.0), dict(temperature=1.0), dict(temperature=0.7, top_k=40), dict(temperature=1.3, top_p=0.9), dict(temperature=0.9, min_p=0.05),
+          dict(temperature=0.8, top_k=200, top_p=0.95, min_p=0.02), dict(temperature=0.0, top_p=0.5), dict(temperature=3.0, top_k=3, top_p=0.99),
+          dict(temperature=0.05), dict(temperature=INF, top_p=0.25), dict(temperature=1e-30), dict(temperature=1.0, top_p=0.0), dict(temperature=2.0, min_p=1.0),
+          dict(temperature=1.0, top_k=1), dict(temperature=1.0, top_k=10 ** 6, top_p=0.5)]
+
+
+def run_rows(logits, u, params, kind, dev, forbid=-1, **more):
+    """Rows of a host tensor on the device, each against the definition."""
+    t = logits.to(dev) if not logits.is_cuda else logits
+    there = {k: v.to(dev) if torch.is_tensor(v) else v for k, v in params.items()}
+    tokens, conf = sample.tokens(t, u.to(dev), confidence=kind, forbid=forbid, **there, **more)
+    torch.cuda.synchronize()
+    for r, x in enumerate(logits.double().cpu().numpy()):
+        one = {k: (float(v[r]) if torch.is_tensor(v) else (float(np.float32(v)) if k != "top_k" else v)) for k, v in params.items()}
+        check(x, int(tokens[r]), float(conf[r]), float(u[r]), kind=kind, forbid=forbid, **{k: (int(v) if k == "top_k" else v) for k, v in one.items()})
+    return tokens, conf
+
+
+@pytest.fixture
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    return torch.device("cuda:0")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", list(sample.CONFIDENCES))
+@pytest.mark.parametrize("which", range(len(PARAMS)))
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_parameters(dev, dtype, which, kind):
+    gen = torch.Generator().manual_seed(7 + which)
+    for how in ("normal", "peaked", "ties"):
+        run_rows(make((5, 2003), how, DTYPES[dtype], gen), torch.rand(5, generator=gen), PARAMS[which], kind, dev)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [0, 1, 2, 3, 4, 5, 9, 11])
+@pytest.mark.parametrize("how", ["equal", "near", "zeros", "wide", "masked", "holes", "rising"])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_values(dev, dtype, how, which):
+    gen = torch.Generator().manual_seed(31 + which)
+    for kind in sample.CONFIDENCES:
+        run_rows(make((6, 4099), how, DTYPES[dtype], gen), torch.rand(6, generator=gen), PARAMS[which], kind, dev)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [1, 2, 3, 7, 8, 9, 63, 64, 65, 127, 511, 513, 1025, 4096, 32000, 50257, 126464, 152064, 262143, 262144])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_sizes(dev, dtype, vocab):
+    gen = torch.Generator().manual_seed(vocab)
+    for n, params in enumerate((PARAMS[0], PARAMS[1], PARAMS[5])):
+        run_rows(make((3, vocab), ("normal", "peaked")[n % 2], DTYPES[dtype], gen), torch.rand(3, generator=gen), params, list(sample.CONFIDENCES)[n], dev)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (5, 3), (64, 0), (7, 8)])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_strides(dev, dtype, pad, offset):
+    """Rows at any distance and address; what lies between and around them is not read."""
+    gen = torch.Generator().manual_seed(pad + 100 * offset)
+    rows, vocab = 7, 1237
+    logits = make((rows, vocab), "normal", DTYPES[dtype], gen)
+    buffer = torch.full((offset + rows * (vocab + pad) + 64,), INF, dtype=DTYPES[dtype], device=dev)
+    view = torch.as_strided(buffer, (rows, vocab), (vocab + pad, 1), offset)
+    view.copy_(logits)
+    for params in (PARAMS[0], PARAMS[1], PARAMS[5]):
+        run_rows(view, torch.rand(rows, generator=gen), params, "entropy", dev)
+    one = view[:1].expand(4, vocab)  # a single row, over and over
+    run_rows(one, torch.rand(4, generator=gen), PARAMS[1], "probability", dev)
+
+
+@pytest.mark.gpu
+def test_uniform_numbers(dev):
+    """The ends of u, and numbers that are none of it."""
+    gen = torch.Generator().manual_seed(3)
+    logits = make((8, 777), "normal", torch.float32, gen)
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, 7.0, -1.0, math.nan, 2.0 ** -149, 0.5])
+    tokens, _ = sample.tokens(logits.to(dev), u.to(dev), temperature=1.0, top_p=0.9)
+    tokens = tokens.cpu()
+    for r in range(8):
+        order, w, _ = ranked(logits[r].numpy(), 1.0, top_p=float(np.float32(0.9)))
+        last = order[int((w > 0).sum()) - 1]
+        if r in (0, 4, 5, 6):
+            assert tokens[r] == order[0]
+        elif r in (1, 2, 3):
+            assert tokens[r] == last
+    # halves to the last bit: six equal tokens, u M = 3 exactly
+    equal = torch.full((4, 6), 2.5, device=dev)
+    tokens, conf = sample.tokens(equal, torch.tensor([0.0, 0.5, 0.5 - 2.0 ** -25, 1.0], device=dev), temperature=0.7)
+    assert tokens.tolist() == [0, 3, 2, 5] and conf.tolist() == [float(np.float32(1 / 6))] * 4
+    tokens, conf = sample.tokens(equal, torch.full((4,), 0.99, device=dev), temperature=0.7, top_p=0.5)
+    assert tokens.tolist() == [2] * 4 and conf.tolist() == [float(np.float32(1 / 3))] * 4
+    many = torch.zeros((2, 4096), device=dev)  # more of them than are sorted
+    tokens, conf = sample.tokens(many, torch.tensor([0.5, 0.25], device=dev), temperature=1.0, top_p=0.5)
+    assert tokens.tolist() == [1024, 512] and conf.tolist() == [1 / 2048] * 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_parameters_of_requests(dev, dtype):
+    """Parameters by request, rows in any order of requests, rows of none."""
+    gen = torch.Generator().manual_seed(11)
+    rows, vocab, requests = 40, 5003, 9
+    logits = make((rows, vocab), "peaked", DTYPES[dtype], gen)
+    u = torch.rand(rows, generator=gen)
+    each = dict(temperature=torch.tensor([0.0, 0.5, 1.0, 1.5, 0.7, -1.0, math.nan, 1.0, 0.9]), top_k=torch.tensor([0, 5, 0, 100, -3, 0, 0, 1, 4000], dtype=torch.int32),
+                top_p=torch.tensor([1.0, 0.9, 0.3, 1.0, 2.0, 1.0, math.nan, 1.0, 0.99]), min_p=torch.tensor([0.0, 0.0, 0.1, 0.01, -1.0, 0.0, math.nan, 0.0, 0.0]))
+    of = torch.randint(0, requests, (rows,), generator=gen, dtype=torch.int32)
+    of[5], of[17] = -1, requests
+    tokens, conf = sample.tokens(logits.to(dev), u.to(dev), **{k: v.to(dev) for k, v in each.items()}, params_of=of.to(dev), confidence="margin")
+    plain = lambda v, off, ok: float(v) if ok(v) else off  # noqa: E731
+    for r in range(rows):
+        p = int(of[r])
+        if not 0 <= p < requests:
+            assert (int(tokens[r]), float(conf[r])) == (-1, 0.0)
+            continue
+        check(logits[r].double().numpy(), int(tokens[r]), float(conf[r]), float(u[r]), plain(each["temperature"][p], 0.0, lambda v: v > 0), "margin",
+              max(0, int(each["top_k"][p])), plain(each["top_p"][p], 1.0, lambda v: v < 1), plain(each["min_p"][p], 0.0, lambda v: v > 0))
+    # an entry a row, numbers beside it; and rows that are skipped without any array
+    t = torch.rand(rows, generator=gen) + 0.3
+    run_rows(logits, u, dict(temperature=t, top_k=30), "probability", dev)
+    of = torch.where(torch.arange(rows) % 3 == 0, -1, 4).int()
+    tokens, _ = sample.tokens(logits.to(dev), u.to(dev), temperature=0.0, params_of=of.to(dev))
+    assert (tokens.cpu()[of < 0] == -1).all() and (tokens.cpu()[of >= 0] >= 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_forbidden_token(dev, dtype):
+    gen = torch.Generator().manual_seed(5)
+    for vocab in (1, 9, 1000, 4097):
+        logits = make((4, vocab), "normal", DTYPES[dtype], gen)
+        for forbid in sorted({0, vocab // 2, vocab - 1, int(logits[0].argmax())}):
+            for params in (PARAMS[0], PARAMS[5]):
+                tokens, _ = run_rows(logits, torch.rand(4, generator=gen), params, "probability", dev, forbid=forbid)
+                assert (tokens != forbid).all()
+
+
+@pytest.mark.gpu
+def test_streams_outputs_and_graphs(dev):
+    gen = torch.Generator().manual_seed(9)
+    logits = make((33, 3001), "peaked", torch.bfloat16, gen).to(dev)
+    u = torch.rand(33, generator=gen).to(dev)
+    want = sample.tokens(logits, u, temperature=0.8, top_k=50, confidence="entropy")
+    for _ in range(3):  # the same bits every time
+        assert all(torch.equal(a, b) for a, b in zip(want, sample.tokens(logits, u, temperature=0.8, top_k=50, confidence="entropy")))
+    out, conf = torch.full((33,), -7, dtype=torch.int32, device=dev), torch.zeros(33, device=dev)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = sample.tokens(logits, u, temperature=0.8, top_k=50, confidence="entropy", out=out, confidence_out=conf, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert got[0] is out and all(torch.equal(a, b) for a, b in zip(want, got))
+    # a captured step: tokens, then the rows that take them, on new numbers before each replay
+    ids0 = torch.full((33,), 3001, dtype=torch.int32, device=dev)
+    indptr = torch.tensor([0, 1, 1, 20, 33], dtype=torch.int32, device=dev)
+    with torch.cuda.stream(side):
+        sample.unmask(*sample.tokens(logits, u, temperature=0.8, top_k=50), ids0, indptr, mask_id=3001)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g = sample.tokens(logits, u, temperature=0.8, top_k=50)
+        h = sample.unmask(*g, ids0, indptr, mask_id=3001, count=2)
+    for k in range(4):
+        u.copy_(torch.rand(33, generator=gen))
+        logits.copy_(make((33, 3001), ("peaked", "normal", "ties", "equal")[k], torch.bfloat16, gen))
+        graph.replay()
+        a = sample.tokens(logits, u, temperature=0.8, top_k=50)
+        b = sample.unmask(*a, ids0, indptr, mask_id=3001, count=2)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(a + b, g + h))
+
+
+@pytest.mark.gpu
+def test_no_rows(dev):
+    tokens, conf = sample.tokens(torch.empty((0, 50), device=dev), torch.empty(0, device=dev))
+    assert tokens.shape == conf.shape == (0,)
+
+
+def test_definition():
+    """The oracle's own words on a row that can be followed by hand."""
+    x = np.log([0.1, 0.4, 0.2, 0.2, 0.1])
+    order, w, _ = ranked(x, 1.0)
+    assert order.tolist() == [1, 2, 3, 0, 4]
+    np.testing.assert_allclose(w / w.sum(), [0.4, 0.2, 0.2, 0.1, 0.1], rtol=1e-12)
+    assert (ranked(x, 1.0, top_k=3)[1] > 0).tolist() == [True, True, True, False, False]
+    assert (ranked(x, 1.0, top_p=0.55)[1] > 0).tolist() == [True, True, False, False, False]
+    assert (ranked(x, 1.0, top_k=2, top_p=0.65)[1] > 0).tolist() == [True, False, False, False, False]
+    assert (ranked(x, 1.0, min_p=0.45)[1] > 0).tolist() == [True, True, True, False, False]
+    assert (ranked(x, 1.0, top_p=0.0)[1] > 0).tolist() == [True, False, False, False, False]
+    assert ranked([-INF, math.nan], 1.0) is None
+    assert ranked([1.0, INF, INF, -INF], 1.0)[1].tolist() == [1.0, 1.0, 0.0, 0.0]
+
+
+# ------------------------------------------------------------------ refusals
+def c_desc(**kw):
+    d = _lib.SampleDesc(4096, 4, 100, 100, 0, 4096, None, 0, None, None, None, None, 1.0, 0, 1.0, 0.0, 0, -1)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+@pytest.mark.parametrize("status,kw", [
+    (-2, dict(dtype=3)), (-2, dict(dtype=-1)), (-1, dict(rows=-1)), (-1, dict(rows=2 ** 31)), (-1, dict(vocab=0)), (-1, dict(vocab=2 ** 18 + 1)),
+    (-1, dict(confidence=3)), (-1, dict(confidence=-1)), (-1, dict(forbid=-2)), (-1, dict(forbid=100)), (-1, dict(temperature=-0.5)),
+    (-1, dict(temperature=math.nan)), (-1, dict(top_k=-1)), (-1, dict(top_p=1.5)), (-1, dict(top_p=-0.1)), (-1, dict(top_p=math.nan)), (-1, dict(min_p=2.0)),
+    (-1, dict(min_p=math.nan)), (-1, dict(num_params=-1)), (-1, dict(temperatures=4096, num_params=3)), (-1, dict(logits=None)), (-1, dict(u=None)),
+    (-1, dict(row_stride=-1)), (-1, dict(row_stride=2 ** 40 + 1)), (-6, dict(logits=4097)), (-6, dict(dtype=2, logits=4098)), (-6, dict(u=4098)),
+    (-6, dict(params_of=4097, num_params=4)), (-6, dict(top_ks=4099, num_params=4))])
+def test_c_refusals(status, kw):
+    """Fake addresses: every check fails before any HIP call."""
+    assert _lib.lib.sangam_sample_tokens(ctypes.byref(c_desc(**kw)), 4096, 4096, None, 0, None) == status
+    assert len(_lib.lib.sangam_last_error()) > 0
+
+
+def test_c_outputs_refused():
+    lib = _lib.lib
+    assert lib.sangam_sample_tokens(None, 4096, 4096, None, 0, None) == -1
+    assert lib.sangam_sample_tokens(ctypes.byref(c_desc()), None, 4096, None, 0, None) == -1
+    assert lib.sangam_sample_tokens(ctypes.byref(c_desc()), 4097, 4096, None, 0, None) == -6
+    assert lib.sangam_sample_tokens(ctypes.byref(c_desc()), 4096, 4098, None, 0, None) == -6
+    assert lib.sangam_sample_tokens(ctypes.byref(c_desc(rows=0, logits=None, u=None)), None, None, None, 0, None) == 0
+
+
+def test_python_refusals():
+    x, u = torch.zeros((4, 10)), torch.zeros(4)
+    with pytest.raises(ValueError, match="GPU"):
+        sample.tokens(x, u)
+    with pytest.raises(TypeError):
+        sample.tokens(x.double(), u)
+    with pytest.raises(TypeError):
+        sample.tokens(x[0], u)
+    with pytest.raises(ValueError, match="confidence"):
+        sample.tokens(x, u, confidence="mean")
+
+
+@pytest.mark.gpu
+def test_python_refusals_on_device(dev):
+    x, u = torch.zeros((4, 10), device=dev), torch.zeros(4, device=dev)
+    ints = lambda n: torch.zeros(n, dtype=torch.int32, device=dev)  # noqa: E731
+    for error, kw in [(ValueError, dict(temperature=-1.0)), (ValueError, dict(temperature=math.nan)), (ValueError, dict(top_k=-1)), (ValueError, dict(top_p=1.01)),
+                      (ValueError, dict(min_p=-0.5)), (ValueError, dict(forbid=10)), (ValueError, dict(forbid=-2)), (TypeError, dict(temperature=ints(4))),
+                      (ValueError, dict(temperature=u[:3])), (TypeError, dict(top_k=u)), (ValueError, dict(top_k=ints(5))), (ValueError, dict(params_of=ints(3))),
+                      (TypeError, dict(params_of=u)), (ValueError, dict(params_of=ints(4), temperature=u[:2], top_k=ints(3))), (ValueError, dict(top_p=u.cpu())),
+                      (TypeError, dict(out=u)), (ValueError, dict(out=ints(3))), (ValueError, dict(confidence_out=torch.zeros(8, device=dev)[::2]))]:
+        with pytest.raises(error):
+            sample.tokens(x, u, **kw)
+    with pytest.raises(ValueError):
+        sample.tokens(x, u[:3])
+    with pytest.raises(ValueError):
+        sample.tokens(x.t(), torch.zeros(10, device=dev))
+    with pytest.raises(ValueError):
+        sample.tokens(torch.zeros((1, 2 ** 18 + 1), device=dev), u[:1])
