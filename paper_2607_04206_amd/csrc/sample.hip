@@ -4,14 +4,18 @@
 // All filters and the draw are places on one axis, the ranks: a prefix of them
 // is kept, and the draw falls at a share u of the prefix's weight. What is
 // needed of a row is therefore how many tokens and how much weight lie above a
-// logit. With t = 64 log2(e) (X - x) / T, a token weighs 2^(-t / 64); bin b
-// holds those with floor(t) = b, as a count and the sum of what their weights
-// miss of the bin's largest, y = 1 - 2^(-frac(t) / 64) in whole steps of 2^-33.
-// Whole numbers, so the order of LDS atomics changes nothing, and 4096 bins
-// reach down to 2^-64 of the largest weight. A place inside a bin is found among
-// the bin's own tokens, which a further look at the row collects: sorted in LDS
-// where they fit (some hundred at most in a row of a language model's logits),
-// else by digits of their logits.
+// logit. With t = -64 log2(e) x / T (and a constant), a token weighs 2^(-t / 64);
+// bin b holds those with floor(t) = b, as a count and the sum of what their
+// weights miss of the bin's largest, y = 1 - 2^(-frac(t) / 64) in whole steps of
+// 2^-33. Whole numbers, so the order of LDS atomics changes nothing, and 4096
+// bins reach down to 2^-64 of the largest weight. A place inside a bin is found
+// among the bin's own tokens, which a further look at the row collects: sorted
+// in LDS where they fit (some hundred at most in a row of a language model's
+// logits), else by digits of their logits.
+//
+// The bins do not hang on the row's largest logit, so one look fills them: they
+// lie in a circle, and where a chunk of the row has a larger logit than all
+// before, the bins that fall out at the far end are cleared for it.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -20,6 +24,7 @@
 
 #include "../../include/sangam_sample.h"
 #include "entry.h"
+#include "nonce.h"
 
 namespace sangam {
 void set_error(const std::string& msg);
@@ -34,11 +39,14 @@ constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 4096;
 constexpr int kEach = kBins / kThreads;  // bins of a thread
-constexpr int kList = 1024;              // tokens of a bin that are sorted
-constexpr int kDigits = 2048;
+constexpr int kList = kThreads;          // tokens of a bin that are sorted
 constexpr int kMaxVocab = 1 << 18;
-constexpr int kGroups = kMaxVocab / 4 / 64;  // of 64 vectors of 16 bytes
-constexpr int kLoads = 4;                    // vectors of a thread on their way together
+constexpr int kLoads = 8;                // vectors of 16 bytes of a thread in a chunk
+constexpr int kChunk = kThreads * kLoads;
+constexpr int kTops = kMaxVocab / 8 / kLoads;
+
+// t's constant: whole, and as small as leaves f at 2^-30 (|x / T| up to 45,000).
+constexpr double kOrigin = 0x1p22;
 
 // A bin or digit: tokens, and what their weights miss, in units of 2^-33 of the
 // bin's largest weight. 2^18 tokens miss under 2^44.5 of them.
@@ -48,12 +56,6 @@ __device__ __forceinline__ int tokens_in(uint64_t bin) { return int(bin >> kMiss
 __device__ __forceinline__ uint64_t weight_in(uint64_t bin) {  // in units of 2^-33
     return (bin >> kMissBits) * kOne - (bin & ((uint64_t(1) << kMissBits) - 1));
 }
-__device__ __forceinline__ double bin_weight(int b) { return exp2(b * (-1.0 / 64)); }
-// Units of 2^-33 of a bin's largest weight as units of 2^-44 of the row's.
-__device__ __forceinline__ uint64_t mass_of(int b, uint64_t v) { return uint64_t(__builtin_rint(bin_weight(b) * double(v) * 2048.0)); }
-// And back.
-__device__ __forceinline__ double inside(int b, double mass) { return mass / (bin_weight(b) * 2048.0); }
-
 struct SampleArgs {
     const void* logits;
     int64_t row_stride;
@@ -73,20 +75,29 @@ struct SampleArgs {
 };
 
 struct Shared {
-    uint64_t bins[kBins];
+    uint64_t bins[kBins];  // of floor(t) mod kBins
     union {
         struct {
             uint64_t list[kList];    // key and index; then the weight up to each
             uint64_t sorted[kList];
         };
-        uint64_t digits[kDigits];
+        uint64_t digits[256];
     };
-    float tops[kGroups];  // the largest logit of a group of vectors
-    uint64_t part[2 * kWaves];
-    double sums[kWaves];
+    uint16_t tops[kTops];  // the largest logit of a thread's chunk (rounded up to 16 bits)
+    uint64_t part[kWaves];
+    double sums[2 * kWaves];
+    float wave_top[2][kWaves];
     uint64_t found_mass, found_bin;
     int found, found_tokens, found_last, listed;
     int32_t index;
+    double powers[64];  // 2^(-k / 64)
+
+    // The largest weight of the row's b-th bin.
+    __device__ __forceinline__ double bin_weight(int b) const { return __builtin_ldexp(powers[b & 63], -(b >> 6)); }
+    // Units of 2^-33 of a bin's largest weight as units of 2^-44 of the first bin's.
+    __device__ __forceinline__ uint64_t mass_of(int b, uint64_t v) const { return uint64_t(__builtin_rint(bin_weight(b) * double(v) * 2048.0)); }
+    // And back.
+    __device__ __forceinline__ double inside(int b, double mass) const { return mass / (bin_weight(b) * 2048.0); }
 };
 
 // Keys of 32 bits in rank order: the larger the logit, the smaller the key.
@@ -96,83 +107,13 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float((key >> 31) ? key : ~key & 0x7FFFFFFFu); }
 
-template <typename T>
-struct Row {
-    static constexpr int V = 16 / int(sizeof(T));
-    const T* p;
-    int vocab, forbid;
-    int head, vectors, groups;  // elements before the first aligned vector; vectors; groups of 64 of them
-    bool infinite;              // some logit is +inf: those count as 0, all others as -inf
-    double top, scale;          // t = (top - x) scale
-
-    __device__ float adjusted(float x, int i) const {
-        if (i == forbid) x = -INFINITY;
-        if (infinite) x = x == INFINITY ? 0.0f : -INFINITY;
-        return x;
-    }
-    __device__ float at(int i) const { return adjusted(float(p[i]), i); }
-    __device__ double t_of(float x) const { return (top - double(x)) * scale; }
-    // vectors of the groups that want() asks for: f(group, first index, logits)
-    template <typename Want, typename F>
-    __device__ __forceinline__ void each_vector(Want want, F f) const {
-        typedef T Vec __attribute__((ext_vector_type(V)));
-        const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-        const Vec* const v = reinterpret_cast<const Vec*>(p + head);
-        for (int g0 = wave; g0 < groups; g0 += kWaves * kLoads) {
-            Vec w[kLoads];
-            bool have[kLoads];
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                const int g = g0 + j * kWaves;
-                have[j] = g < groups && want(g);
-                if (have[j] && 64 * g + lane < vectors) w[j] = v[64 * g + lane];
-            }
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                const int g = g0 + j * kWaves;
-                if (!have[j]) continue;
-                float x[V];
-                const int i0 = head + (64 * g + lane) * V;
-                if (64 * g + lane < vectors) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) x[e] = float(w[j][e]);
-                    if (unsigned(forbid - i0) < unsigned(V)) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e)
-                            if (i0 + e == forbid) x[e] = -INFINITY;
-                    }
-                    if (infinite) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e) x[e] = x[e] == INFINITY ? 0.0f : -INFINITY;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) x[e] = -INFINITY;
-                }
-                f(g, i0, x);
-            }
-        }
-    }
-    // the elements outside all vectors
-    template <typename F>
-    __device__ __forceinline__ void each_edge(F f) const {
-        const int rest = vocab - vectors * V;
-        for (int k = threadIdx.x; k < rest; k += kThreads) {
-            const int i = k < head ? k : k + vectors * V;
-            f(i, at(i));
-        }
-    }
-    // all logits with t under `limit`, and some of the others
-    template <typename F>
-    __device__ __forceinline__ void each_under(const float* tops, double limit, F f) const {
-        each_vector([&](int g) { return !(t_of(tops[g]) >= limit); },
-                    [&](int, int i0, const float(&x)[V]) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e) f(i0 + e, x[e]);
-                    });
-        each_edge(f);
-    }
-};
+// The upper 16 bits of the least such number not below x (no number: +inf).
+__device__ __forceinline__ uint16_t rounded_up(float x) {
+    const uint32_t b = __float_as_uint(x);
+    if (!(x == x)) return 0x7F80;
+    return uint16_t(((b >> 31) ? b : b + 0xFFFFu) >> 16);
+}
+__device__ __forceinline__ float from_upper(uint16_t h) { return __uint_as_float(uint32_t(h) << 16); }
 
 // What the weight at a fraction f of a bin misses, in units of 2^-33: the low word
 // of 2^52 + 2^33 (1 - 2^(-f / 64)). (Cubic without constant, fitted over [0, 1);
@@ -180,6 +121,20 @@ struct Row {
 __device__ __forceinline__ uint32_t miss_at(double f) {
     constexpr double q1 = 0x1.62e42fb615b67p-7 * 0x1p33, q2 = -0x1.ebfa827a93283p-15 * 0x1p33, q3 = 0x1.c454fdc63ddabp-23 * 0x1p33;
     return uint32_t(__double2loint(__builtin_fma(f, __builtin_fma(f, __builtin_fma(f, q3, q2), q1), 0x1p52)));
+}
+
+// A value that all lanes hold, in scalar registers.
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float scalar(float x) { return __uint_as_float(uint32_t(scalar(int(__float_as_uint(x))))); }
+__device__ __forceinline__ uint64_t scalar(uint64_t x) { return uint64_t(uint32_t(scalar(int(x >> 32)))) << 32 | uint32_t(scalar(int(x))); }
+__device__ __forceinline__ double scalar(double x) { return __builtin_bit_cast(double, scalar(__builtin_bit_cast(uint64_t, x))); }
+
+__device__ __forceinline__ void add_to(uint64_t* bin, uint64_t more) { atomicAdd(reinterpret_cast<unsigned long long*>(bin), more); }
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
 }
 
 __device__ __forceinline__ uint64_t wave_up_to(uint64_t x) {
@@ -193,7 +148,7 @@ __device__ __forceinline__ uint64_t wave_up_to(uint64_t x) {
 }
 
 // Sum over the threads before this one, and over all.
-__device__ uint64_t sum_before(Shared& sh, uint64_t x, uint64_t* total) {
+__device__ __forceinline__ uint64_t sum_before(Shared& sh, uint64_t x, uint64_t* total) {
     const int wave = threadIdx.x / 64;
     const uint64_t up_to = wave_up_to(x);
     __syncthreads();
@@ -206,21 +161,123 @@ __device__ uint64_t sum_before(Shared& sh, uint64_t x, uint64_t* total) {
         if (w < wave) before += p;
         all += p;
     }
-    *total = all;
+    *total = scalar(all);
     return before + up_to - x;
 }
 
-__device__ double sum_all(Shared& sh, double x) {
+// Sums over all threads, in a fixed order.
+__device__ __forceinline__ void sum_all(Shared& sh, double& x, double& y) {
 #pragma unroll
-    for (int d = 32; d > 0; d /= 2) x += __shfl_xor(x, d);
+    for (int d = 32; d > 0; d /= 2) {
+        x += __shfl_xor(x, d);
+        y += __shfl_xor(y, d);
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.sums[threadIdx.x / 64] = x;
+    if ((threadIdx.x & 63) == 0) {
+        sh.sums[threadIdx.x / 64] = x;
+        sh.sums[kWaves + threadIdx.x / 64] = y;
+    }
     __syncthreads();
-    x = 0.0;
+    x = y = 0.0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) x += sh.sums[w];
-    return x;
+    for (int w = 0; w < kWaves; ++w) {
+        x += sh.sums[w];
+        y += sh.sums[kWaves + w];
+    }
 }
+
+template <typename T>
+struct Row {
+    static constexpr int V = 16 / int(sizeof(T));
+    static constexpr int kPerTop = 8 / V;  // chunks of an entry of tops
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    const T* p;
+    int vocab, forbid;
+    int head, vectors;  // elements before the first aligned vector; vectors
+    bool infinite;      // some logit is +inf: those count as 0, all others as -inf
+    bool wide;          // t is relative to the largest logit, as x / T is large
+    double top, scale;  // wide: t = (top - x) scale, else kOrigin - x scale
+    int base;           // floor(t) of the largest logit
+
+    __device__ __forceinline__ float adjusted(float x, int i) const {
+        if (i == forbid) x = -INFINITY;
+        if (infinite) x = x == INFINITY ? 0.0f : -INFINITY;
+        return x;
+    }
+    __device__ __forceinline__ float at(int i) const { return adjusted(float(p[i]), i); }
+    __device__ __forceinline__ double t_of(float x) const { return wide ? (top - double(x)) * scale : __builtin_fma(-double(x), scale, kOrigin); }
+    __device__ __forceinline__ void unpack(const Vec& w, int i0, float (&x)[V]) const {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = float(w[e]);
+        if (unsigned(forbid - i0) < unsigned(V)) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (i0 + e == forbid) x[e] = -INFINITY;
+        }
+        if (infinite) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = x[e] == INFINITY ? 0.0f : -INFINITY;
+        }
+    }
+    // the vectors, a chunk after the other: f(number of the chunk, vectors, their first index or -1)
+    template <typename F>
+    __device__ __forceinline__ void each_chunk(F f) const {
+        const Vec* const v = reinterpret_cast<const Vec*>(p + head);
+        int chunk = 0;
+        for (int v0 = 0; v0 < vectors; v0 += kChunk, ++chunk) {
+            Vec w[kLoads];
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int k = v0 + j * kThreads + int(threadIdx.x);
+                if (k < vectors) w[j] = v[k];
+            }
+            f(chunk, v0, w);
+        }
+    }
+    // f(first index, logits) of a chunk's vectors
+    template <typename F>
+    __device__ __forceinline__ void each_of(int v0, const Vec (&w)[kLoads], F f) const {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int k = v0 + j * kThreads + int(threadIdx.x);
+            if (k >= vectors) continue;
+            float x[V];
+            unpack(w[j], head + k * V, x);
+            f(head + k * V, x);
+        }
+    }
+    // the elements outside all vectors
+    template <typename F>
+    __device__ __forceinline__ void each_edge(F f) const {
+        const int rest = vocab - vectors * V;
+        for (int k = threadIdx.x; k < rest; k += kThreads) {
+            const int i = k < head ? k : k + vectors * V;
+            f(i, at(i));
+        }
+    }
+    // All logits with t under `limit`, and some of the others: a thread looks at a
+    // chunk of its own again only where tops says that it holds one. (One vector at a
+    // time: mostly few threads have any.)
+    template <typename F>
+    __device__ __forceinline__ void each_under(const Shared& sh, double limit, F f) const {
+        const Vec* const v = reinterpret_cast<const Vec*>(p + head);
+#pragma unroll 1
+        for (int v0 = 0; v0 < vectors; v0 += kChunk) {
+            if (t_of(from_upper(sh.tops[v0 / kChunk / kPerTop * kThreads + threadIdx.x])) >= limit) continue;
+#pragma unroll 1
+            for (int k = v0 + int(threadIdx.x); k < min(v0 + kChunk, vectors); k += kThreads) {
+                float x[V];
+                unpack(v[k], head + k * V, x);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    f(head + k * V + e, x[e]);
+                    __builtin_amdgcn_sched_barrier(0);  // (side by side they take twice the registers)
+                }
+            }
+        }
+        each_edge(f);
+    }
+};
 
 // A prefix of the ranks: all tokens of the bins before `bin`, and the first
 // `tokens` of that bin, which end with `ties` tokens of key `key`.
@@ -230,56 +287,49 @@ struct Prefix {
     uint64_t weight;     // of those of the bin, units of 2^-33 of its largest
     uint64_t mass;       // of the bins before, units of 2^-44
     int before;          // tokens of the bins before
-    __device__ uint64_t all() const { return mass + (tokens ? mass_of(bin, weight) : 0); }
+    __device__ uint64_t all(const Shared& sh) const { return mass + (tokens ? sh.mass_of(bin, weight) : 0); }
 };
 
-// A token inside a bin: the place-th of those with its key, behind `before` tokens of the bin.
-struct Token {
-    uint32_t key;
-    int place, before, index;
-    uint64_t weight_before;  // of the bin's tokens before those of its key
-    int equal;               // tokens with its key
-};
-
-enum class By { kCount, kReach, kAbove };
+// What a place on the axis of ranks is given by: the number of tokens up to it,
+// weight before its token, weight up to its token, a lowest logit.
+enum class By { kCount, kReach, kAbove, kCut };
 
 template <typename T>
 struct Bin {
     Shared& sh;
     const Row<T>& row;
-    int& listed;  // bin whose tokens sh.sorted and sh.list hold
+    int listed;  // bin whose tokens sh.sorted and sh.list hold
 
-    __device__ uint64_t weight_of(uint32_t key, int b) const { return kOne - miss_at(row.t_of(logit_of(key)) - b); }
+    // its place in the bin, 0 to 1; outside: another bin's
+    __device__ __forceinline__ double place(float x, int b) const { return row.t_of(x) - double(row.base + b); }
+    __device__ __forceinline__ uint64_t weight_of(uint32_t key, int b) const { return kOne - miss_at(place(logit_of(key), b)); }
 
     // Tokens of bin b, in rank order, and their weights summed up.
-    __device__ void collect(int b, int n) {
+    __device__ __forceinline__ void collect(int b, int n) {
         if (listed == b) return;
         __syncthreads();
         if (threadIdx.x == 0) sh.listed = 0;
         __syncthreads();
-        row.each_under(sh.tops, double(b + 1), [&](int i, float x) {
-            const double t = row.t_of(x);
-            if (t >= double(b) && t < double(b + 1)) {
+        row.each_under(sh, double(row.base + b + 1), [&](int i, float x) {
+            const double f = place(x, b);
+            if (f >= 0.0 && f < 1.0) {
                 const int k = atomicAdd(&sh.listed, 1);
                 if (k < kList) sh.list[k] = (uint64_t(key_of(x)) << 32) | uint32_t(i);
             }
         });
         __syncthreads();
-        for (int k = threadIdx.x; k < n; k += kThreads) {
+        const int k = threadIdx.x;
+        if (k < n) {
             const uint64_t mine = sh.list[k];
             int rank = 0;
             for (int j = 0; j < n; ++j) rank += sh.list[j] < mine;
             sh.sorted[rank] = mine;
         }
         __syncthreads();
-        static_assert(kList == 2 * kThreads, "two tokens a thread");
-        const int k = 2 * threadIdx.x;
-        const uint64_t w0 = k < n ? weight_of(uint32_t(sh.sorted[k] >> 32), b) : 0;
-        const uint64_t w1 = k + 1 < n ? weight_of(uint32_t(sh.sorted[k + 1] >> 32), b) : 0;
+        const uint64_t w = k < n ? weight_of(uint32_t(sh.sorted[k] >> 32), b) : 0;
         uint64_t total;
-        const uint64_t before = sum_before(sh, w0 + w1, &total);
-        if (k < n) sh.list[k] = before + w0;
-        if (k + 1 < n) sh.list[k + 1] = before + w0 + w1;
+        const uint64_t before = sum_before(sh, w, &total);
+        if (k < n) sh.list[k] = before + w;
         __syncthreads();
         listed = b;
     }
@@ -292,401 +342,405 @@ struct Bin {
             if (f(mid)) lo = mid + 1;
             else hi = mid;
         }
-        return lo;
+        return scalar(lo);
     }
 
-    // The key at which a count or weight is met, by digits of the keys.
-    __device__ Token descend(int b, By by, int count, double weight) {
+    // The bin's first tokens up to a place, by digits of the keys; p.ties - 1 tokens with the last one's key are before it.
+    __device__ __forceinline__ void descend(Prefix& p, By by, int count, double weight, uint32_t cut, int most) {
         listed = -1;
-        Token k{0, 0, 0, -1, 0, 0};
-        constexpr int bits[3] = {11, 11, 10}, shifts[3] = {21, 10, 0};
-        for (int step = 0; step < 3; ++step) {
-            const int shift = shifts[step], width = bits[step];
+        const int d = threadIdx.x, b = p.bin;
+        uint32_t key = 0;
+        int before = 0, equal = 0;
+        uint64_t weight_before = 0;
+#pragma unroll 1
+        for (int shift = 24; shift >= 0; shift -= 8) {
             __syncthreads();
-            for (int d = threadIdx.x; d < kDigits; d += kThreads) sh.digits[d] = 0;
-            if (threadIdx.x == 0) sh.found = sh.found_last = -1;
+            if (d < 256) sh.digits[d] = 0;
+            if (d == 0) sh.found = sh.found_last = -1;
             __syncthreads();
-            row.each_under(sh.tops, double(b + 1), [&](int, float x) {
-                const double t = row.t_of(x);
-                if (!(t >= double(b) && t < double(b + 1))) return;
-                const uint32_t key = key_of(x);
-                if ((uint64_t(key) >> (shift + width)) != (uint64_t(k.key) >> (shift + width))) return;
-                atomicAdd(reinterpret_cast<unsigned long long*>(&sh.digits[(key >> shift) & ((1u << width) - 1)]),
-                          (uint64_t(1) << kMissBits) | miss_at(t - b));
+            row.each_under(sh, double(row.base + b + 1), [&](int, float x) {
+                const double f = place(x, b);
+                if (!(f >= 0.0 && f < 1.0)) return;
+                const uint32_t k = key_of(x);
+                if ((uint64_t(k) >> (shift + 8)) != (uint64_t(key) >> (shift + 8))) return;
+                add_to(&sh.digits[(k >> shift) & 255], (uint64_t(1) << kMissBits) | miss_at(f));
             });
             __syncthreads();
-            uint64_t bin[kDigits / kThreads], tokens = 0, total, v = 0;
-#pragma unroll
-            for (int j = 0; j < kDigits / kThreads; ++j) {
-                bin[j] = sh.digits[threadIdx.x * (kDigits / kThreads) + j];
-                tokens += tokens_in(bin[j]);
-                v += weight_in(bin[j]);
-            }
-            int n = k.before + int(sum_before(sh, tokens, &total));
-            uint64_t w = k.weight_before + sum_before(sh, v, &total);
-#pragma unroll
-            for (int j = 0; j < kDigits / kThreads; ++j) {
-                const int d = threadIdx.x * (kDigits / kThreads) + j, more = tokens_in(bin[j]);
-                const uint64_t after = w + weight_in(bin[j]);
-                const bool here = by == By::kCount   ? n < count && n + more >= count
-                                  : by == By::kReach ? double(w) < weight && double(after) >= weight
-                                                     : double(w) <= weight && double(after) > weight;
-                if (more > 0) atomicMax(&sh.found_last, d);
-                if (here) {
-                    sh.found = d;
-                    sh.found_tokens = n;
-                    sh.found_mass = w;
-                    sh.found_bin = bin[j];
-                }
-                n += more;
-                w = after;
+            const uint64_t bin = d < 256 ? sh.digits[d] : 0;
+            const int more = tokens_in(bin);
+            uint64_t total;
+            const int n = before + int(sum_before(sh, more, &total));
+            const uint64_t w = weight_before + sum_before(sh, weight_in(bin), &total), after = w + weight_in(bin);
+            const bool here = by == By::kCount   ? n < count && n + more >= count
+                              : by == By::kReach ? double(w) < weight && double(after) >= weight
+                              : by == By::kAbove ? double(w) <= weight && double(after) > weight
+                                                 : d == int((cut >> shift) & 255);
+            if (more > 0) atomicMax(&sh.found_last, d);
+            if (here) sh.found = d;
+            __syncthreads();
+            const int at = sh.found >= 0 ? sh.found : sh.found_last;  // (behind all: the last one)
+            if (d == at) {
+                sh.found_tokens = n;
+                sh.found_mass = w;
+                sh.found_bin = bin;
             }
             __syncthreads();
-            const int last = sh.found_last;
-            if (sh.found < 0 && threadIdx.x == last / (kDigits / kThreads)) {  // behind all: the last one
-                const int j = last % (kDigits / kThreads);
-                uint64_t own = 0;
-                int more = 0;
-#pragma unroll
-                for (int e = 0; e < kDigits / kThreads; ++e)
-                    if (e >= j) {
-                        own += weight_in(bin[e]);
-                        more += tokens_in(bin[e]);
-                    }
-                sh.found_tokens = n - more;
-                sh.found_mass = w - own;
-                sh.found_bin = sh.digits[last];
-            }
-            __syncthreads();
-            const int d = sh.found < 0 ? last : sh.found;
-            k.key |= uint32_t(d) << shift;
-            k.before = sh.found_tokens;
-            k.weight_before = sh.found_mass;
-            k.equal = tokens_in(sh.found_bin);
+            key |= uint32_t(scalar(at)) << shift;
+            before = scalar(sh.found_tokens);
+            weight_before = scalar(sh.found_mass);
+            equal = tokens_in(scalar(sh.found_bin));
         }
-        const double each = double(weight_of(k.key, b));
-        if (by == By::kCount) {
-            k.place = count - k.before - 1;
-        } else {
-            // kReach: the last token that has less than `weight` before it; kAbove: the first with more up to it
-            const double into = (weight - double(k.weight_before)) / each;
-            k.place = by == By::kReach ? int(ceil(into)) - 1 : int(floor(into));
+        const uint64_t each = scalar(weight_of(key, b));
+        // tokens with this key up to the place; kReach: the last that has less than `weight` before it; kAbove: the first with more up to it
+        const double into = (weight - double(weight_before)) / double(each);
+        int ties = equal;
+        if (by != By::kCut) {
+            ties = by == By::kCount ? count - before : by == By::kReach ? int(ceil(into)) : int(floor(into)) + 1;
+            ties = scalar(max(1, min(ties, min(equal, most - before))));
         }
-        k.place = min(max(k.place, 0), k.equal - 1);
-        return k;
+        p.tokens = before + ties;
+        p.ties = ties;
+        p.key = key;
+        p.weight = weight_before + uint64_t(ties) * each;
     }
-    // Index of a token among those with its key.
-    __device__ int index_of(const Token& k) {
+    // Index of the last of p's tokens.
+    __device__ __forceinline__ int index_of(const Prefix& p) {
         uint64_t before = 0;
+#pragma unroll 1
         for (int i0 = 0; i0 < row.vocab; i0 += 8 * kThreads) {
             const int i = i0 + 8 * int(threadIdx.x);
             uint64_t mine = 0, total;
+#pragma unroll 1
             for (int e = 0; e < 8; ++e)
                 if (i + e < row.vocab) {
                     const float x = row.at(i + e);
-                    mine += x == x && key_of(x) == k.key;
+                    mine += x == x && key_of(x) == p.key;
                 }
-            const uint64_t place = uint64_t(k.place) - before - sum_before(sh, mine, &total);
-            if (place < mine) {
-                uint64_t left = place;
+            uint64_t left = uint64_t(p.ties - 1) - before - sum_before(sh, mine, &total);
+            if (left < mine) {
+#pragma unroll 1
                 for (int e = 0; e < 8; ++e)
                     if (i + e < row.vocab) {
                         const float x = row.at(i + e);
-                        if (x == x && key_of(x) == k.key && left-- == 0) sh.index = i + e;
+                        if (x == x && key_of(x) == p.key && left-- == 0) sh.index = i + e;
                     }
             }
             before += total;
-            if (before > uint64_t(k.place)) break;
+            if (before >= uint64_t(p.ties)) break;
         }
         __syncthreads();
-        return sh.index;
+        return scalar(sh.index);
     }
 
-    // The first `count` tokens of bin b, or those with less than `weight` before them.
-    __device__ void first(Prefix& p, int b, int n, By by, int count, double weight) {
-        if (n <= kList) {
-            collect(b, n);
-            const int m = by == By::kCount ? count : max(1, leading(n, [&](int i) { return i == 0 || double(sh.list[i - 1]) < weight; }));
-            ends(p, m);
-        } else {
-            const Token k = descend(b, by, count, weight);
-            p.tokens = k.before + k.place + 1;
-            p.ties = k.place + 1;
-            p.key = k.key;
-            p.weight = k.weight_before + uint64_t(k.place + 1) * weight_of(k.key, b);
+    // p's first tokens of its bin (which holds n): up to `count` of them, or those with less than `weight` before them, or up
+    // to the first with more than `weight` up to it (at most `most`), or those with a key up to `cut`. Returns the last one's
+    // index where it is at hand, else -1.
+    __device__ __forceinline__ int first(Prefix& p, int n, By by, int count, double weight, uint32_t cut, int most) {
+        if (n > kList) {
+            descend(p, by, count, weight, cut, most);
+            return -1;
         }
-    }
-    // p's end from the list, m > 0 tokens in.
-    __device__ void ends(Prefix& p, int m) {
+        collect(p.bin, n);
+        const int m = by == By::kCount   ? count
+                      : by == By::kReach ? max(1, leading(n, [&](int i) { return i == 0 || double(sh.list[i - 1]) < weight; }))
+                      : by == By::kAbove ? min(leading(n, [&](int i) { return double(sh.list[i]) <= weight; }), most - 1) + 1
+                                         : leading(n, [&](int i) { return uint32_t(sh.sorted[i] >> 32) <= cut; });
         p.tokens = m;
-        p.key = uint32_t(sh.sorted[m - 1] >> 32);
+        p.weight = 0;
+        if (m == 0) return -1;
+        const uint64_t last = scalar(sh.sorted[m - 1]);
+        p.key = uint32_t(last >> 32);
         p.ties = m - leading(m, [&](int i) { return uint32_t(sh.sorted[i] >> 32) < p.key; });
-        p.weight = sh.list[m - 1];
-    }
-    // Those of bin b whose logit is at least `cut`.
-    __device__ void at_least(Prefix& p, int b, int n, float cut) {
-        const uint32_t key = key_of(cut);
-        if (n <= kList) {
-            collect(b, n);
-            const int m = leading(n, [&](int i) { return uint32_t(sh.sorted[i] >> 32) <= key; });
-            if (m > 0) ends(p, m);
-            else p.tokens = 0, p.weight = 0;
-            return;
-        }
-        uint64_t mine = 0, total;
-        row.each_under(sh.tops, double(b + 1), [&](int, float x) {
-            const double t = row.t_of(x);
-            if (t >= double(b) && t < double(b + 1) && key_of(x) <= key) mine += (uint64_t(1) << kMissBits) | miss_at(t - b);
-        });
-        sum_before(sh, mine, &total);
-        p.tokens = tokens_in(total);
-        p.weight = weight_in(total);
-        p.key = key + 1;  // (with no ties: all up to the cut)
-        p.ties = 0;
-    }
-    // The first token of bin b (n tokens, of which `most` are kept) with more than `weight` up to it: index and weight.
-    __device__ void draw(int b, int n, int most, double weight, int* index, uint64_t* w) {
-        uint32_t key;
-        if (n <= kList) {
-            collect(b, n);
-            const int i = min(leading(n, [&](int k) { return double(sh.list[k]) <= weight; }), most - 1);
-            key = uint32_t(sh.sorted[i] >> 32);
-            *index = int(uint32_t(sh.sorted[i]));
-        } else {
-            Token k = descend(b, By::kAbove, 0, weight);
-            if (k.before + k.place >= most) k = descend(b, By::kCount, most, 0.0);
-            key = k.key;
-            *index = index_of(k);
-        }
-        *w = weight_of(key, b);
+        p.weight = scalar(sh.list[m - 1]);
+        return int(uint32_t(last));
     }
 };
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
-    __shared__ Shared sh;
-    constexpr int V = Row<T>::V;
-    const int64_t r = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+// Parameters of a row, as the header defines them.
+struct Params {
+    float temperature, top_p, min_p;
+    int top_k;
+    bool none;  // the row's entry is outside: nothing is taken
+};
+
+__device__ __forceinline__ Params params_of(const SampleArgs& a, int64_t r) {
+    Params p{};
     const int64_t of = a.params_of ? a.params_of[r] : r;
-    const bool arrays = a.temperatures || a.top_ks || a.top_ps || a.min_ps;
-    if ((arrays || a.params_of) && (of < 0 || of >= a.num_params)) {
-        if (tid == 0) {
-            a.tokens[r] = -1;
-            if (a.conf) a.conf[r] = 0.0f;
-        }
-        return;
+    p.none = (a.params_of || a.temperatures || a.top_ks || a.top_ps || a.min_ps) && (of < 0 || of >= a.num_params);
+    if (p.none) return p;
+    p.temperature = a.temperatures ? a.temperatures[of] : a.temperature;
+    if (!(p.temperature > 0.0f)) p.temperature = 0.0f;
+    p.top_k = a.top_ks ? a.top_ks[of] : a.top_k;
+    if (p.top_k < 1 || p.top_k >= a.vocab) p.top_k = 0;
+    p.top_p = a.top_ps ? a.top_ps[of] : a.top_p;
+    if (!(p.top_p < 1.0f)) p.top_p = 1.0f;
+    p.min_p = a.min_ps ? a.min_ps[of] : a.min_p;
+    if (!(p.min_p > 0.0f)) p.min_p = 0.0f;
+    return p;
+}
+
+__device__ __forceinline__ void answer(const SampleArgs& a, int64_t r, int token, double c) {
+    if (threadIdx.x == 0) {
+        a.tokens[r] = token;
+        if (a.conf) a.conf[r] = float(c);
     }
-    float temperature = a.temperatures ? a.temperatures[of] : a.temperature;
-    if (!(temperature > 0.0f)) temperature = 0.0f;
-    int top_k = a.top_ks ? a.top_ks[of] : a.top_k;
-    float top_p = a.top_ps ? a.top_ps[of] : a.top_p;
-    if (!(top_p < 1.0f)) top_p = 1.0f;
-    float min_p = a.min_ps ? a.min_ps[of] : a.min_p;
-    if (!(min_p > 0.0f)) min_p = 0.0f;
-    const bool greedy = temperature == 0.0f;
-    const double T_ = greedy ? 1.0 : double(temperature);
+}
 
-    Row<T> row;
-    row.p = static_cast<const T*>(a.logits) + r * a.row_stride;
-    row.vocab = a.vocab;
-    row.forbid = a.forbid;
-    row.infinite = false;
-    row.head = min(int((16 - (reinterpret_cast<uintptr_t>(row.p) & 15)) & 15) / int(sizeof(T)), a.vocab);
-    row.vectors = (a.vocab - row.head) / V;
-    row.groups = (row.vectors + 63) / 64;
-
-    // the largest logit, its first index, and the second largest
-    float best = -INFINITY, second = -INFINITY;
-    int at = INT32_MAX;
-    auto look = [&](float x) {
-        x = fmaxf(x, -INFINITY);  // (no number)
-        second = fmaxf(second, fminf(best, x));
-        best = fmaxf(best, x);
+// The bins of a whole row, whose largest logit becomes `top`; false: its x / T is
+// too large, or infinite, for bins that do not hang on it.
+template <typename T>
+__device__ __forceinline__ bool fill(Shared& sh, Row<T>& row, float& top) {
+    constexpr int V = Row<T>::V;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    top = -INFINITY;
+    int parity = 0;
+    // a chunk's largest logit is in: whether its logits are to be added
+    auto raise = [&](float mine) {
+        mine = wave_max(mine);
+        if (lane == 0) sh.wave_top[parity][wave] = mine;
+        __syncthreads();
+        float m = sh.wave_top[parity][0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sh.wave_top[parity][w]);
+        parity ^= 1;
+        if (!(m > top)) return top > -INFINITY;
+        const double t = row.t_of(m);
+        if (t >= 0x1p23) return false;  // so low that bins may not be kept for it
+        const int to = t > 0.0 ? int(t) : 0;
+        if (top > -INFINITY) {
+            for (int b = to + tid; b < row.base && b < to + kBins; b += kThreads) sh.bins[b & (kBins - 1)] = 0;
+            __syncthreads();
+        }
+        top = scalar(m);
+        row.base = scalar(to);
+        return t > 0.0;
     };
-    row.each_vector([](int) { return true; },
-                    [&](int g, int i0, const float(&x)[V]) {
-                        float m = x[0];
+    auto add = [&](float x, double limit) {
+        const double t = __builtin_fma(-double(x), row.scale, kOrigin);
+        if (t < limit)
+            add_to(&sh.bins[unsigned(t) & (kBins - 1)], (uint64_t(1) << kMissBits) | miss_at(__builtin_amdgcn_fract(t)));
+    };
+    for (int b = tid; b < kBins; b += kThreads) sh.bins[b] = 0;
+    float kept_top = -INFINITY;
+    row.each_chunk([&](int chunk, int v0, const typename Row<T>::Vec(&w)[kLoads]) {
+        float m = -INFINITY;
+        row.each_of(v0, w, [&](int, const float(&x)[V]) {
 #pragma unroll
-                        for (int e = 1; e < V; ++e) m = fmaxf(m, x[e]);
-                        if (m > best) at = i0;
+            for (int e = 0; e < V; ++e) m = fmaxf(m, x[e]);
+        });
+        kept_top = chunk % Row<T>::kPerTop ? fmaxf(kept_top, m) : m;
+        sh.tops[chunk / Row<T>::kPerTop * kThreads + tid] = rounded_up(kept_top);
+        if (!raise(m)) return;
+        const double limit = double(row.base + kBins);
+        row.each_of(v0, w, [&](int, const float(&x)[V]) {
 #pragma unroll
-                        for (int e = 0; e < V; ++e) look(x[e]);
-#pragma unroll
-                        for (int d = 32; d > 0; d /= 2) m = fmaxf(m, __shfl_xor(m, d));
-                        if (lane == 0) sh.tops[g] = m;
-                    });
-    row.each_edge([&](int i, float x) {
-        if (x > best || (x == best && i < at)) at = i;
-        look(x);
+            for (int e = 0; e < V; ++e) add(x[e], limit);
+        });
     });
-    float top = best;
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane == 0) sh.sums[wave] = top;
-    if (tid == 0) sh.index = INT32_MAX;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, float(sh.sums[w]));
-    if (!(top > -INFINITY)) {  // nothing to take
-        if (tid == 0) {
-            a.tokens[r] = -1;
-            if (a.conf) a.conf[r] = 0.0f;
+    if (row.vocab > row.vectors * V) {
+        float m = -INFINITY;
+        row.each_edge([&](int, float x) { m = fmaxf(m, x); });
+        if (raise(m)) {
+            const double limit = double(row.base + kBins);
+            row.each_edge([&](int, float x) { add(x, limit); });
         }
-        return;
     }
-    if (best == top)
-        for (int e = 0; e < V && at + e < a.vocab; ++e)
-            if (row.at(at + e) == top) {
-                atomicMin(&sh.index, at + e);
-                break;
-            }
-    // the second of all: the first of the others, or this one's second where it holds the first
-    int holders = __syncthreads_count(best == top);
-    float next = best == top && holders == 1 ? second : best;
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) next = fmaxf(next, __shfl_xor(next, d));
     __syncthreads();
-    if (lane == 0) sh.sums[wave] = next;
+    return top > -INFINITY && row.base > 0 && row.base + kBins <= 0x800000;
+}
+
+// The same by two looks, for any row. False: the row has no weight.
+template <typename T>
+__device__ __forceinline__ bool fill_wide(Shared& sh, Row<T>& row, float& top) {
+    constexpr int V = Row<T>::V;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    float m = -INFINITY;
+    row.each_chunk([&](int, int v0, const typename Row<T>::Vec(&w)[kLoads]) {
+        row.each_of(v0, w, [&](int, const float(&x)[V]) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) m = fmaxf(m, x[e]);
+        });
+    });
+    row.each_edge([&](int, float x) { m = fmaxf(m, x); });
+    m = wave_max(m);
+    __syncthreads();
+    if (lane == 0) sh.wave_top[0][wave] = m;
     for (int b = tid; b < kBins; b += kThreads) sh.bins[b] = 0;
     __syncthreads();
-    for (int w = 0; w < kWaves; ++w) next = fmaxf(next, float(sh.sums[w]));
-    const int first_index = sh.index;
-    if (top == INFINITY) {
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sh.wave_top[0][w]);
+    if (m == -INFINITY) return false;
+    if (m == INFINITY) {
         row.infinite = true;
-        top = 0.0f;
-        next = next == INFINITY ? 0.0f : -INFINITY;
-        for (int g = tid; g < row.groups; g += kThreads) sh.tops[g] = sh.tops[g] == INFINITY ? 0.0f : -INFINITY;
+        m = 0.0f;
+        for (int k = tid; k < kTops; k += kThreads) sh.tops[k] = 0x7F80;  // (+inf: every chunk is looked at)
         __syncthreads();
     }
-    row.top = double(top);
-    row.scale = 64.0 * 1.4426950408889634074 / T_;
-
-    // bins
-    row.each_under(sh.tops, double(kBins), [&](int, float x) {
+    top = scalar(m);
+    row.wide = true;
+    row.top = scalar(double(m));
+    row.base = 0;
+    row.each_under(sh, double(kBins), [&](int, float x) {
         const double t = row.t_of(x);
-        if (t < double(kBins)) {
-            const int b = int(t);
-            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bins[b]), (uint64_t(1) << kMissBits) | miss_at(t - b));
-        }
+        if (t < double(kBins)) add_to(&sh.bins[int(t)], (uint64_t(1) << kMissBits) | miss_at(__builtin_amdgcn_fract(t)));
     });
     __syncthreads();
-    uint64_t mass[kEach], tokens = 0, mine = 0, all_tokens, all_mass;
-#pragma unroll
+    return true;
+}
+
+// A row's answer from its bins: one place on the axis of ranks after the other.
+template <typename T>
+__device__ __forceinline__ void choose(Shared& sh, const Row<T>& row, const SampleArgs& a, const Params& p, int64_t r, float top) {
+    const int tid = threadIdx.x;
+    const bool greedy = p.temperature == 0.0f;
+    const double T_ = scalar(greedy ? 1.0 : double(p.temperature));
+    auto slot = [&](int b) -> uint64_t { return sh.bins[(row.base + b) & (kBins - 1)]; };
+    uint64_t tokens = 0, mine = 0, all_tokens, all_mass;
+#pragma unroll 2
     for (int j = 0; j < kEach; ++j) {
-        const uint64_t bin = sh.bins[tid * kEach + j];
-        mass[j] = bin ? mass_of(tid * kEach + j, weight_in(bin)) : 0;
+        const uint64_t bin = slot(tid * kEach + j);
         tokens += tokens_in(bin);
-        mine += mass[j];
+        mine += sh.mass_of(tid * kEach + j, weight_in(bin));
     }
     const int tokens_before = int(sum_before(sh, tokens, &all_tokens));
     const uint64_t mass_before = sum_before(sh, mine, &all_mass);
-    // the bin for which here(bin, tokens before, tokens, mass before, mass) holds; at most one; -1: none
-    auto find = [&](auto here) {
+    Bin<T> bin{sh, row, -1};
+    const double low = scalar(p.min_p > 0.0f ? log(double(p.min_p)) : 0.0);
+    const uint64_t top_weight = scalar(kOne - miss_at(bin.place(top, 0)));
+    Prefix kept{kBins, 0, 0, 0, 0, all_mass, int(all_tokens)};
+    const Prefix only_first{0, 1, 1, key_of(top), top_weight, 0, 0};
+    double unit = 0.0, weight = 0.0, second = 0.0;  // 2^44 / M; of the token; of the second token, if it is kept
+    int token = -1;
+    enum Stage { kTopK, kTopP, kMinP, kDraw, kSecond, kStages };
+#pragma unroll 1
+    for (int stage = kTopK; stage < kStages; ++stage) {
+        // the place: the bin whose end is the first at or above `reach`, counted in tokens, weight or bins
+        By by = By::kCount;
+        uint64_t reach = 0;
+        double target = 0.0;
+        uint32_t cut_key = 0;
+        if (stage == kTopK) {
+            if (p.top_k == 0 || p.top_k >= int(all_tokens)) continue;
+            reach = uint64_t(p.top_k);
+        } else if (stage == kTopP) {
+            if (!(p.top_p < 1.0f)) continue;
+            target = scalar(ceil(double(p.top_p) * double(kept.all(sh))));
+            if (!(target > 0.0)) {
+                kept = only_first;
+                continue;
+            }
+            by = By::kReach;
+            reach = uint64_t(target);
+        } else if (stage == kMinP) {
+            if (!(p.min_p > 0.0f)) continue;
+            if (!(low <= 0.0)) {
+                kept = only_first;
+                continue;
+            }
+            // the lowest logit that is kept: an estimate, then by the definition
+            auto keeps = [&](float x) { return (double(x) - double(top)) / T_ >= low; };
+            float cut = float(fmax(double(top) + T_ * low, -3.4e38));
+            for (int k = 0; k < 4 && !keeps(cut); ++k) cut = nextafterf(cut, INFINITY);
+            for (int k = 0; k < 4; ++k) {
+                const float lower = nextafterf(cut, -INFINITY);
+                if (!(lower > -INFINITY) || !keeps(lower)) break;
+                cut = lower;
+            }
+            cut = fminf(cut, top);
+            const double t = row.t_of(cut) - double(row.base);
+            if (!(t < double(kBins)) || int(t) > kept.bin) continue;
+            by = By::kCut;
+            reach = uint64_t(scalar(int(t))) + 1;
+            cut_key = uint32_t(scalar(int(key_of(cut))));
+        } else if (stage == kDraw) {
+            const uint64_t M = scalar(kept.all(sh));
+            unit = scalar(0x1p44 / double(M));
+            const float u = greedy ? 0.0f : a.u[r];
+            target = scalar(fmin(u > 0.0f ? double(u) * double(M) : 0.0, double(M - 1)));
+            by = By::kAbove;
+            reach = uint64_t(target) + 1;
+        } else {
+            if (a.confidence != SANGAM_CONFIDENCE_MARGIN || kept.before + kept.tokens < 2) continue;
+            reach = 2;
+        }
         __syncthreads();
         if (tid == 0) sh.found = -1;
         __syncthreads();
         int n = tokens_before;
         uint64_t w = mass_before;
-#pragma unroll
+#pragma unroll 2
         for (int j = 0; j < kEach; ++j) {
-            const int b = tid * kEach + j, more = tokens_in(sh.bins[b]);
-            if (here(b, n, more, w, mass[j])) {
+            const int b = tid * kEach + j, more = tokens_in(slot(b));
+            const uint64_t mass = sh.mass_of(b, weight_in(slot(b)));
+            const uint64_t lo = by == By::kCount ? uint64_t(n) : by == By::kCut ? uint64_t(b) : w;
+            const uint64_t hi = by == By::kCount ? uint64_t(n + more) : by == By::kCut ? uint64_t(b + 1) : w + mass;
+            if (lo < reach && hi >= reach) {
                 sh.found = b;
                 sh.found_tokens = n;
                 sh.found_mass = w;
             }
             n += more;
-            w += mass[j];
+            w += mass;
         }
         __syncthreads();
-        return sh.found;
-    };
-    int listed = -1;
-    Bin<T> bin{sh, row, listed};
-    Prefix kept{kBins, 0, 0, 0, 0, all_mass, int(all_tokens)};
-    auto only_first = [&] {
-        kept = Prefix{0, 1, 1, key_of(top), kOne, 0, 0};
-    };
-    if (top_k > 0 && top_k < int(all_tokens)) {
-        const int b = find([&](int, int n, int more, uint64_t, uint64_t) { return n < top_k && n + more >= top_k; });
-        kept.bin = b;
-        kept.before = sh.found_tokens;
-        kept.mass = sh.found_mass;
-        bin.first(kept, b, tokens_in(sh.bins[b]), By::kCount, top_k - kept.before, 0.0);
-    }
-    if (top_p < 1.0f) {
-        const double share = ceil(double(top_p) * double(kept.all()));
-        if (!(share > 0.0)) {
-            only_first();
+        Prefix q{scalar(sh.found), 0, 0, 0, 0, scalar(sh.found_mass), scalar(sh.found_tokens)};
+        if (q.bin < 0 || q.bin > kept.bin) continue;  // (not met within what is kept)
+        n = tokens_in(scalar(slot(q.bin)));
+        const double into = by == By::kReach || by == By::kAbove ? scalar(fmax(0.0, sh.inside(q.bin, target - double(q.mass)))) : 0.0;
+        int index = -1;
+        if (n > 0) index = bin.first(q, n, by, int(reach) - q.before, into, cut_key, q.bin == kept.bin ? kept.tokens : n);
+        if (stage <= kMinP) {
+            if (q.bin < kept.bin || q.tokens < kept.tokens) kept = q;
+        } else if (stage == kDraw) {
+            token = index >= 0 ? index : bin.index_of(q);
+            weight = scalar(sh.bin_weight(q.bin) * double(bin.weight_of(q.key, q.bin)) * 0x1p-33);
         } else {
-            const uint64_t reach = uint64_t(share);
-            const int b = find([&](int, int, int, uint64_t w, uint64_t m) { return w < reach && w + m >= reach; });
-            if (b >= 0 && b <= kept.bin) {
-                Prefix p{b, 0, 0, 0, 0, sh.found_mass, sh.found_tokens};
-                bin.first(p, b, tokens_in(sh.bins[b]), By::kReach, 0, inside(b, double(reach - p.mass)));
-                if (b < kept.bin || p.tokens < kept.tokens) kept = p;
-            }
-        }
-    }
-    if (min_p > 0.0f) {
-        const double low = log(double(min_p));
-        if (!(low <= 0.0)) {
-            only_first();
-        } else {
-            // the lowest logit that is kept: an estimate, then by the definition
-            auto keeps = [&](float x) { return (double(x) - double(top)) / T_ >= low; };
-            float cut = float(fmax(double(top) + T_ * low, -3.4e38));
-            for (int k = 0; k < 4 && !keeps(cut); ++k) cut = nextafterf(cut, INFINITY);
-            for (int k = 0; k < 4 && keeps(nextafterf(cut, -INFINITY)) && nextafterf(cut, -INFINITY) > -INFINITY; ++k) cut = nextafterf(cut, -INFINITY);
-            cut = fminf(cut, top);
-            const double t = row.t_of(cut);
-            if (t < double(kBins) && int(t) <= kept.bin) {
-                const int b = int(t);
-                find([&](int k, int, int, uint64_t, uint64_t) { return k == b; });
-                Prefix p{b, 0, 0, 0, 0, sh.found_mass, sh.found_tokens};
-                if (tokens_in(sh.bins[b]) > 0) bin.at_least(p, b, tokens_in(sh.bins[b]), cut);
-                if (b < kept.bin || p.tokens < kept.tokens) kept = p;
-            }
-        }
-    }
-    const uint64_t M = kept.all();
-    const double unit = 0x1p44 / double(M);  // weights as shares of M
-    int token = first_index;
-    double weight = 1.0;
-    if (!greedy) {
-        const float u = a.u[r];
-        const double target = fmin(u > 0.0f ? double(u) * double(M) : 0.0, double(M - 1));
-        const uint64_t above = uint64_t(target);
-        const int b = find([&](int, int, int, uint64_t w, uint64_t m) { return w <= above && w + m > above; });
-        if (b >= 0) {
-            const int n = tokens_in(sh.bins[b]);
-            uint64_t v;
-            const double into = fmax(0.0, inside(b, target - double(sh.found_mass)));
-            bin.draw(b, n, b == kept.bin ? kept.tokens : n, into, &token, &v);
-            weight = bin_weight(b) * double(v) * 0x1p-33;
+            second = scalar(sh.bin_weight(q.bin) * double(bin.weight_of(q.key, q.bin)) * 0x1p-33);
         }
     }
     double c = weight * unit;
     if (a.confidence == SANGAM_CONFIDENCE_MARGIN) {
-        double other = 0.0;
-        const double t = row.t_of(next);
-        if (kept.before + kept.tokens > 1 && t < double(kBins)) other = bin_weight(int(t)) * double(kOne - miss_at(t - int(t))) * 0x1p-33;
-        c = (1.0 - other) * unit;
+        c = (double(top_weight) * 0x1p-33 - second) * unit;
     } else if (a.confidence == SANGAM_CONFIDENCE_ENTROPY) {
-        double s = 0.0;
-        auto part = [&](double t) { return bin_weight(int(t)) * double(kOne - miss_at(t - int(t))) * 0x1p-33 * t; };
-        row.each_under(sh.tops, double(min(kept.bin + 1, kBins)), [&](int, float x) {
-            const double t = row.t_of(x);
+        double s = 0.0, none = 0.0;
+        auto part = [&](double t) { return sh.bin_weight(int(t)) * double(kOne - miss_at(t - int(t))) * 0x1p-33 * t; };
+        row.each_under(sh, double(row.base + min(kept.bin + 1, kBins)), [&](int, float x) {
+            const double t = bin.place(x, 0);
             if (t < double(kept.bin) || (kept.tokens > 0 && t < double(kept.bin + 1) && key_of(x) < kept.key)) s += part(t);
         });
-        s = sum_all(sh, s);
-        if (kept.tokens > 0 && kept.ties > 0) s += kept.ties * part(row.t_of(logit_of(kept.key)));
-        c = -(s * unit * (0.69314718055994530942 / 64) + log(double(M) * 0x1p-44));
+        sum_all(sh, s, none);
+        if (kept.tokens > 0 && kept.ties > 0) s += kept.ties * part(bin.place(logit_of(kept.key), 0));
+        c = -(s * unit * (0.69314718055994530942 / 64) - log(unit));
     }
-    if (tid == 0) {
-        a.tokens[r] = token;
-        if (a.conf) a.conf[r] = float(c);
+    answer(a, r, token, c);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads, 4) void sample_kernel(SampleArgs a) {
+    __shared__ Shared sh;
+    constexpr int V = Row<T>::V;
+    const int64_t r = blockIdx.x;
+    const Params p = params_of(a, r);
+    if (p.none) {
+        answer(a, r, -1, 0.0);
+        return;
     }
+    Row<T> row;
+    row.p = static_cast<const T*>(a.logits) + r * a.row_stride;
+    row.vocab = a.vocab;
+    row.forbid = a.forbid;
+    row.infinite = row.wide = false;
+    row.head = min(int((16 - (reinterpret_cast<uintptr_t>(row.p) & 15)) & 15) / int(sizeof(T)), a.vocab);
+    row.vectors = (a.vocab - row.head) / V;
+    row.top = 0.0;
+    row.base = 0;
+    row.scale = scalar(64.0 * 1.4426950408889634074 / (p.temperature == 0.0f ? 1.0 : double(p.temperature)));
+    if (threadIdx.x < 64) sh.powers[threadIdx.x] = exp2(threadIdx.x * (-1.0 / 64));
+    float top;
+    if (!fill(sh, row, top) && !fill_wide(sh, row, top)) {
+        answer(a, r, -1, 0.0);
+        return;
+    }
+    choose(sh, row, a, p, r, top);
 }
 
 sangam_status fail(sangam_status code, const std::string& msg) {
