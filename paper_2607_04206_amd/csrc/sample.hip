@@ -16,10 +16,16 @@
 // The bins do not hang on the row's largest logit, so one look fills them: they
 // lie in a circle, and where a chunk of the row has a larger logit than all
 // before, the bins that fall out at the far end are cleared for it.
+//
+// Logits in bf16 take few values: from 2^-28 to 2^8 there are 4608 of either
+// sign. There a row is counted by its values themselves, six instructions a
+// logit and no exponential but one a value; rows that reach beyond (an
+// infinity, a place among the tiny ones) go the way of the others.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 #include <string>
 
 #include "../../include/sangam_sample.h"
@@ -41,21 +47,36 @@ constexpr int kBins = 4096;
 constexpr int kEach = kBins / kThreads;  // bins of a thread
 constexpr int kList = kThreads;          // tokens of a bin that are sorted
 constexpr int kMaxVocab = 1 << 18;
-constexpr int kLoads = 8;                // vectors of 16 bytes of a thread in a chunk
-constexpr int kChunk = kThreads * kLoads;
-constexpr int kTops = kMaxVocab / 8 / kLoads;
+// Logits of a thread in a chunk, all on their way together: where a work-group
+// takes a whole row, and where it takes a part of one.
+template <typename T>
+constexpr int kWhole = 128 / int(sizeof(T));
+constexpr int kPart = 16;
 
-// t's constant: whole, and as small as leaves f at 2^-30 (|x / T| up to 45,000).
-constexpr double kOrigin = 0x1p22;
+// t's constant. From 2^20 to 2^21 a double's upper word ends in its whole part
+// (|x / T| up to 5,600), and its fraction has steps of 2^-32.
+constexpr double kOrigin = 0x1.8p20, kLowest = 0x1p20, kHighest = 0x1p21;
 
-// A bin or digit: tokens, and what their weights miss, in units of 2^-33 of the
-// bin's largest weight. 2^18 tokens miss under 2^44.5 of them.
+// A bin or digit: the sum over its tokens of 2^52 + 2^45 + y, y what the weight
+// misses in units of 2^-33 of the bin's largest weight, as the bits of that double:
+// the bits from 45 on add up an odd number a token modulo 2^19, those below y
+// (2^18 tokens miss under 2^44.5 units). So what is added is what the last step of
+// the polynomial gives, without a further instruction.
 constexpr int kMissBits = 45;
+constexpr double kCounted = 0x1p52 + 0x1p45;
 constexpr uint64_t kOne = uint64_t(1) << 33;
-__device__ __forceinline__ int tokens_in(uint64_t bin) { return int(bin >> kMissBits); }
-__device__ __forceinline__ uint64_t weight_in(uint64_t bin) {  // in units of 2^-33
-    return (bin >> kMissBits) * kOne - (bin & ((uint64_t(1) << kMissBits) - 1));
+constexpr uint32_t kCode = 0x43302000u >> 13;  // of a token
+constexpr uint32_t inverse(uint32_t x) {       // modulo 2^32
+    uint32_t y = x;
+    for (int k = 0; k < 5; ++k) y *= 2 - x * y;
+    return y;
 }
+static_assert(kCode * inverse(kCode) == 1);
+__device__ __forceinline__ int tokens_in(uint64_t bin) { return int((uint32_t(bin >> kMissBits) * inverse(kCode)) & 0x7FFFFu); }
+__device__ __forceinline__ uint64_t weight_in(uint64_t bin) {  // in units of 2^-33
+    return tokens_in(bin) * kOne - (bin & ((uint64_t(1) << kMissBits) - 1));
+}
+
 struct SampleArgs {
     const void* logits;
     int64_t row_stride;
@@ -74,21 +95,42 @@ struct SampleArgs {
     float* conf;
 };
 
+// Values of bf16 by the bits without the sign: those up to kTiny count as 0, those
+// from kHuge on have no value (infinities and what is no number among them).
+constexpr int kTiny = (127 - 28) * 128 - 1, kHuge = (127 + 8) * 128;
+constexpr int kSide = kHuge - kTiny + 1;           // counts of a sign: tiny, the values, huge
+constexpr int kValues = kSide - 2;                 // of a sign
+constexpr int kRanked = 2 * kValues + 1;           // values in rank order, 0 (tiny) at kValues
+constexpr int kOwn = (kRanked + kThreads - 1) / kThreads;  // of a thread
+static_assert(kOwn <= 64, "a wave looks at a thread's values");
+
+// E: logits of a thread in a chunk.
+template <int E>
 struct Shared {
-    uint64_t bins[kBins];  // of floor(t) mod kBins
+    static constexpr int kTops = kMaxVocab / E;
+    union {
+        struct {
+            uint64_t bins[kBins];  // of floor(t) mod kBins
+            uint64_t beyond;       // where what is too low for a bin goes
+        };
+        uint32_t counts[2 * kSide];
+    };
     union {
         struct {
             uint64_t list[kList];    // key and index; then the weight up to each
-            uint64_t sorted[kList];
+            union {
+                uint64_t sorted[kList];
+                uint16_t queue[4 * kList];  // entries of tops to be looked at again
+            };
         };
         uint64_t digits[256];
     };
-    uint16_t tops[kTops];  // the largest logit of a thread's chunk (rounded up to 16 bits)
+    uint16_t tops[kTops];  // the largest logit of a thread's chunk (rounded up to 16 bits); entry chunk * kThreads + thread
     uint64_t part[kWaves];
     double sums[2 * kWaves];
     float wave_top[2][kWaves];
     uint64_t found_mass, found_bin;
-    int found, found_tokens, found_last, listed;
+    int found, found_tokens, found_last, listed, queued;
     int32_t index;
     double powers[64];  // 2^(-k / 64)
 
@@ -115,13 +157,18 @@ __device__ __forceinline__ uint16_t rounded_up(float x) {
 }
 __device__ __forceinline__ float from_upper(uint16_t h) { return __uint_as_float(uint32_t(h) << 16); }
 
-// What the weight at a fraction f of a bin misses, in units of 2^-33: the low word
-// of 2^52 + 2^33 (1 - 2^(-f / 64)). (Cubic without constant, fitted over [0, 1);
-// off by 5.3e-12 = 0.05 units.)
-__device__ __forceinline__ uint32_t miss_at(double f) {
+// What a token at a fraction f of a bin adds to it: y = 2^33 (1 - 2^(-f / 64)) by
+// a cubic without constant, fitted over [0, 1) and off by 5.3e-12 = 0.05 units.
+// (Written as instructions: the compiler copies constants for the shorter v_fmac.)
+__device__ __forceinline__ uint64_t added_at(double f) {
     constexpr double q1 = 0x1.62e42fb615b67p-7 * 0x1p33, q2 = -0x1.ebfa827a93283p-15 * 0x1p33, q3 = 0x1.c454fdc63ddabp-23 * 0x1p33;
-    return uint32_t(__double2loint(__builtin_fma(f, __builtin_fma(f, __builtin_fma(f, q3, q2), q1), 0x1p52)));
+    double y;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(y) : "v"(f), "s"(q3), "v"(q2));
+    asm("v_fma_f64 %0, %1, %0, %2" : "+v"(y) : "v"(f), "v"(q1));
+    asm("v_fma_f64 %0, %1, %0, %2" : "+v"(y) : "v"(f), "v"(kCounted));
+    return __builtin_bit_cast(uint64_t, y);
 }
+__device__ __forceinline__ uint32_t miss_at(double f) { return uint32_t(added_at(f)); }
 
 // A value that all lanes hold, in scalar registers.
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -148,7 +195,8 @@ __device__ __forceinline__ uint64_t wave_up_to(uint64_t x) {
 }
 
 // Sum over the threads before this one, and over all.
-__device__ __forceinline__ uint64_t sum_before(Shared& sh, uint64_t x, uint64_t* total) {
+template <int E>
+__device__ __forceinline__ uint64_t sum_before(Shared<E>& sh, uint64_t x, uint64_t* total) {
     const int wave = threadIdx.x / 64;
     const uint64_t up_to = wave_up_to(x);
     __syncthreads();
@@ -166,7 +214,8 @@ __device__ __forceinline__ uint64_t sum_before(Shared& sh, uint64_t x, uint64_t*
 }
 
 // Sums over all threads, in a fixed order.
-__device__ __forceinline__ void sum_all(Shared& sh, double& x, double& y) {
+template <int E>
+__device__ __forceinline__ void sum_all(Shared<E>& sh, double& x, double& y) {
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) {
         x += __shfl_xor(x, d);
@@ -186,14 +235,18 @@ __device__ __forceinline__ void sum_all(Shared& sh, double& x, double& y) {
     }
 }
 
-template <typename T>
+// A row of logits, or a part of one: vectors [first, last) of it, and with the
+// first part the elements outside all vectors.
+template <typename T, int E>
 struct Row {
     static constexpr int V = 16 / int(sizeof(T));
-    static constexpr int kPerTop = 8 / V;  // chunks of an entry of tops
+    static constexpr int kLoads = E / V;
+    static constexpr int kChunk = kThreads * kLoads;  // vectors of a chunk
     typedef T Vec __attribute__((ext_vector_type(V)));
     const T* p;
     int vocab, forbid;
-    int head, vectors;  // elements before the first aligned vector; vectors
+    int head, vectors;  // elements before the first aligned vector; vectors of the row
+    int first, last;
     bool infinite;      // some logit is +inf: those count as 0, all others as -inf
     bool wide;          // t is relative to the largest logit, as x / T is large
     double top, scale;  // wide: t = (top - x) scale, else kOrigin - x scale
@@ -206,6 +259,7 @@ struct Row {
     }
     __device__ __forceinline__ float at(int i) const { return adjusted(float(p[i]), i); }
     __device__ __forceinline__ double t_of(float x) const { return wide ? (top - double(x)) * scale : __builtin_fma(-double(x), scale, kOrigin); }
+    __device__ __forceinline__ const Vec* body() const { return reinterpret_cast<const Vec*>(p + head); }
     __device__ __forceinline__ void unpack(const Vec& w, int i0, float (&x)[V]) const {
 #pragma unroll
         for (int e = 0; e < V; ++e) x[e] = float(w[e]);
@@ -219,19 +273,19 @@ struct Row {
             for (int e = 0; e < V; ++e) x[e] = x[e] == INFINITY ? 0.0f : -INFINITY;
         }
     }
-    // the vectors, a chunk after the other: f(number of the chunk, vectors, their first index or -1)
+    // the part's vectors, a chunk after the other: f(number of the chunk in the row, first vector of the chunk, vectors)
     template <typename F>
     __device__ __forceinline__ void each_chunk(F f) const {
-        const Vec* const v = reinterpret_cast<const Vec*>(p + head);
-        int chunk = 0;
-        for (int v0 = 0; v0 < vectors; v0 += kChunk, ++chunk) {
+        const Vec* const v = body();
+#pragma unroll 1
+        for (int v0 = first; v0 < last; v0 += kChunk) {
             Vec w[kLoads];
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 const int k = v0 + j * kThreads + int(threadIdx.x);
-                if (k < vectors) w[j] = v[k];
+                if (k < last) w[j] = v[k];
             }
-            f(chunk, v0, w);
+            f(v0 / kChunk, v0, w);
         }
     }
     // f(first index, logits) of a chunk's vectors
@@ -240,42 +294,80 @@ struct Row {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int k = v0 + j * kThreads + int(threadIdx.x);
-            if (k >= vectors) continue;
+            if (k >= last) continue;
             float x[V];
             unpack(w[j], head + k * V, x);
             f(head + k * V, x);
         }
     }
-    // the elements outside all vectors
+    // the elements outside all vectors, with the first part
     template <typename F>
     __device__ __forceinline__ void each_edge(F f) const {
-        const int rest = vocab - vectors * V;
+        const int rest = first == 0 ? vocab - vectors * V : 0;
         for (int k = threadIdx.x; k < rest; k += kThreads) {
             const int i = k < head ? k : k + vectors * V;
             f(i, at(i));
         }
     }
-    // All logits with t under `limit`, and some of the others: a thread looks at a
-    // chunk of its own again only where tops says that it holds one. (One vector at a
-    // time: mostly few threads have any.)
+    // A little under all logits of the row's first n bins, and a little above those behind the first n.
+    __device__ __forceinline__ float lowest(int n) const {
+        const double x = wide ? top - n / scale : (kOrigin - double(base + n)) / scale;
+        return scale > 0.0 ? scalar(float(fmax(x - fabs(x) * 0x1p-22, -3.5e38))) : -INFINITY;
+    }
+    __device__ __forceinline__ float highest(int n) const {
+        const double x = wide ? top - n / scale : (kOrigin - double(base + n)) / scale;
+        return scale > 0.0 ? scalar(float(x + fabs(x) * 0x1p-22)) : INFINITY;
+    }
+    // All logits of the row from `low` to `high`. Where tops says that few chunks of
+    // threads hold any, these are listed, and the vectors in them dealt over all
+    // threads, so that they come in one or two rounds of loads (a thread that walked
+    // its own chunks took one after the other: 18 us for a bin of a row of 152,064).
     template <typename F>
-    __device__ __forceinline__ void each_under(const Shared& sh, double limit, F f) const {
-        const Vec* const v = reinterpret_cast<const Vec*>(p + head);
+    __device__ __forceinline__ void each_within(Shared<E>& sh, float low, float high, F f) const {
+        constexpr int kRound = 2;
+        __syncthreads();
+        if (threadIdx.x == 0) sh.queued = 0;
+        __syncthreads();
+        const int entries = (vectors + kChunk - 1) / kChunk * kThreads;
+        for (int e = threadIdx.x; e < entries; e += kThreads) {
+            if (from_upper(sh.tops[e]) < low) continue;
+            const int k = atomicAdd(&sh.queued, 1);
+            if (k < 4 * kList) sh.queue[k] = uint16_t(e);
+        }
+        __syncthreads();
+        const int queued = scalar(sh.queued);
+        const bool all = queued > 4 * kList;
+        const int items = all ? vectors : queued * kLoads;
+        const Vec* const v = body();
 #pragma unroll 1
-        for (int v0 = 0; v0 < vectors; v0 += kChunk) {
-            if (t_of(from_upper(sh.tops[v0 / kChunk / kPerTop * kThreads + threadIdx.x])) >= limit) continue;
-#pragma unroll 1
-            for (int k = v0 + int(threadIdx.x); k < min(v0 + kChunk, vectors); k += kThreads) {
+        for (int k0 = threadIdx.x; k0 < items; k0 += kRound * kThreads) {
+            Vec w[kRound];
+            int k[kRound];
+#pragma unroll
+            for (int j = 0; j < kRound; ++j) {
+                const int item = k0 + j * kThreads;
+                k[j] = vectors;
+                if (item < items) {
+                    const int e = all ? 0 : sh.queue[item / kLoads];
+                    k[j] = all ? item : e / kThreads * kChunk + item % kLoads * kThreads + e % kThreads;
+                }
+                if (k[j] < vectors) w[j] = v[k[j]];
+            }
+#pragma unroll
+            for (int j = 0; j < kRound; ++j) {
+                if (k[j] >= vectors) continue;
                 float x[V];
-                unpack(v[k], head + k * V, x);
+                unpack(w[j], head + k[j] * V, x);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    f(head + k * V + e, x[e]);
+                    if (x[e] >= low && x[e] <= high) f(head + k[j] * V + e, x[e]);
                     __builtin_amdgcn_sched_barrier(0);  // (side by side they take twice the registers)
                 }
             }
         }
-        each_edge(f);
+        each_edge([&](int i, float x) {
+            if (x >= low && x <= high) f(i, x);
+        });
     }
 };
 
@@ -287,17 +379,18 @@ struct Prefix {
     uint64_t weight;     // of those of the bin, units of 2^-33 of its largest
     uint64_t mass;       // of the bins before, units of 2^-44
     int before;          // tokens of the bins before
-    __device__ uint64_t all(const Shared& sh) const { return mass + (tokens ? sh.mass_of(bin, weight) : 0); }
+    template <int E>
+    __device__ uint64_t all(const Shared<E>& sh) const { return mass + (tokens ? sh.mass_of(bin, weight) : 0); }
 };
 
 // What a place on the axis of ranks is given by: the number of tokens up to it,
 // weight before its token, weight up to its token, a lowest logit.
 enum class By { kCount, kReach, kAbove, kCut };
 
-template <typename T>
+template <typename T, int E>
 struct Bin {
-    Shared& sh;
-    const Row<T>& row;
+    Shared<E>& sh;
+    const Row<T, E>& row;
     int listed;  // bin whose tokens sh.sorted and sh.list hold
 
     // its place in the bin, 0 to 1; outside: another bin's
@@ -310,7 +403,7 @@ struct Bin {
         __syncthreads();
         if (threadIdx.x == 0) sh.listed = 0;
         __syncthreads();
-        row.each_under(sh, double(row.base + b + 1), [&](int i, float x) {
+        row.each_within(sh, row.lowest(b + 1), row.highest(b), [&](int i, float x) {
             const double f = place(x, b);
             if (f >= 0.0 && f < 1.0) {
                 const int k = atomicAdd(&sh.listed, 1);
@@ -358,12 +451,12 @@ struct Bin {
             if (d < 256) sh.digits[d] = 0;
             if (d == 0) sh.found = sh.found_last = -1;
             __syncthreads();
-            row.each_under(sh, double(row.base + b + 1), [&](int, float x) {
+            row.each_within(sh, row.lowest(b + 1), row.highest(b), [&](int, float x) {
                 const double f = place(x, b);
                 if (!(f >= 0.0 && f < 1.0)) return;
                 const uint32_t k = key_of(x);
                 if ((uint64_t(k) >> (shift + 8)) != (uint64_t(key) >> (shift + 8))) return;
-                add_to(&sh.digits[(k >> shift) & 255], (uint64_t(1) << kMissBits) | miss_at(f));
+                add_to(&sh.digits[(k >> shift) & 255], added_at(f));
             });
             __syncthreads();
             const uint64_t bin = d < 256 ? sh.digits[d] : 0;
@@ -488,11 +581,12 @@ __device__ __forceinline__ void answer(const SampleArgs& a, int64_t r, int token
 
 // The bins of a whole row, whose largest logit becomes `top`; false: its x / T is
 // too large, or infinite, for bins that do not hang on it.
-template <typename T>
-__device__ __forceinline__ bool fill(Shared& sh, Row<T>& row, float& top) {
-    constexpr int V = Row<T>::V;
+template <typename T, int E>
+__device__ __forceinline__ bool fill(Shared<E>& sh, Row<T, E>& row, float& top, uint16_t* tops) {
+    constexpr int V = Row<T, E>::V;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
     top = -INFINITY;
+    if (!(row.scale > 1e-30)) return false;  // (all that is finite may weigh the same)
     int parity = 0;
     // a chunk's largest logit is in: whether its logits are to be added
     auto raise = [&](float mine) {
@@ -505,61 +599,69 @@ __device__ __forceinline__ bool fill(Shared& sh, Row<T>& row, float& top) {
         parity ^= 1;
         if (!(m > top)) return top > -INFINITY;
         const double t = row.t_of(m);
-        if (t >= 0x1p23) return false;  // so low that bins may not be kept for it
-        const int to = t > 0.0 ? int(t) : 0;
+        if (t >= kHighest) return false;  // so low that bins may not be kept for it
+        const int to = t >= kLowest ? int(t) : 0;
         if (top > -INFINITY) {
             for (int b = to + tid; b < row.base && b < to + kBins; b += kThreads) sh.bins[b & (kBins - 1)] = 0;
             __syncthreads();
         }
         top = scalar(m);
         row.base = scalar(to);
-        return t > 0.0;
+        return to > 0;
     };
-    auto add = [&](float x, double limit) {
+    // the lowest logit that has a bin, with the last one to spare (those below weigh nothing)
+    auto cut = [&] {
+        const float x = float(fmax((kOrigin - double(row.base + kBins - 1)) / row.scale, -3.4e38));
+        return scalar(x + fabsf(x) * 0x1p-21f);
+    };
+    uint64_t* const bins = sh.bins;
+    auto add = [&](float x, float lowest) {
         const double t = __builtin_fma(-double(x), row.scale, kOrigin);
-        if (t < limit)
-            add_to(&sh.bins[unsigned(t) & (kBins - 1)], (uint64_t(1) << kMissBits) | miss_at(__builtin_amdgcn_fract(t)));
+        const int at = x >= lowest ? __double2hiint(t) & (kBins - 1) : kBins;
+        static_assert(offsetof(Shared<E>, beyond) == kBins * sizeof(uint64_t), "beyond lies behind the bins");
+        add_to(bins + at, added_at(__builtin_amdgcn_fract(t)));
     };
     for (int b = tid; b < kBins; b += kThreads) sh.bins[b] = 0;
-    float kept_top = -INFINITY;
-    row.each_chunk([&](int chunk, int v0, const typename Row<T>::Vec(&w)[kLoads]) {
+    row.each_chunk([&](int chunk, int v0, const auto& w) {
         float m = -INFINITY;
         row.each_of(v0, w, [&](int, const float(&x)[V]) {
 #pragma unroll
             for (int e = 0; e < V; ++e) m = fmaxf(m, x[e]);
         });
-        kept_top = chunk % Row<T>::kPerTop ? fmaxf(kept_top, m) : m;
-        sh.tops[chunk / Row<T>::kPerTop * kThreads + tid] = rounded_up(kept_top);
+        tops[chunk * kThreads + tid] = rounded_up(m);
         if (!raise(m)) return;
-        const double limit = double(row.base + kBins);
+        const float lowest = cut();
         row.each_of(v0, w, [&](int, const float(&x)[V]) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) add(x[e], limit);
+            for (int e = 0; e < V; ++e) add(x[e], lowest);
         });
     });
     if (row.vocab > row.vectors * V) {
         float m = -INFINITY;
         row.each_edge([&](int, float x) { m = fmaxf(m, x); });
         if (raise(m)) {
-            const double limit = double(row.base + kBins);
-            row.each_edge([&](int, float x) { add(x, limit); });
+            const float lowest = cut();
+            row.each_edge([&](int, float x) { add(x, lowest); });
         }
     }
     __syncthreads();
-    return top > -INFINITY && row.base > 0 && row.base + kBins <= 0x800000;
+    return top > -INFINITY && row.base > 0 && row.base + kBins <= int(kHighest);
 }
 
 // The same by two looks, for any row. False: the row has no weight.
-template <typename T>
-__device__ __forceinline__ bool fill_wide(Shared& sh, Row<T>& row, float& top) {
-    constexpr int V = Row<T>::V;
+template <typename T, int E>
+__device__ __forceinline__ bool fill_wide(Shared<E>& sh, Row<T, E>& row, float& top) {
+    constexpr int V = Row<T, E>::V;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
     float m = -INFINITY;
-    row.each_chunk([&](int, int v0, const typename Row<T>::Vec(&w)[kLoads]) {
+    row.each_chunk([&](int chunk, int v0, const auto& w) {
+        float own = -INFINITY;
         row.each_of(v0, w, [&](int, const float(&x)[V]) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) m = fmaxf(m, x[e]);
+            for (int e = 0; e < V; ++e) own = fmaxf(own, x[e]);
         });
+        sh.tops[chunk * kThreads + tid] = rounded_up(own);
+        m = fmaxf(m, own);
     });
     row.each_edge([&](int, float x) { m = fmaxf(m, x); });
     m = wave_max(m);
@@ -572,27 +674,26 @@ __device__ __forceinline__ bool fill_wide(Shared& sh, Row<T>& row, float& top) {
     if (m == INFINITY) {
         row.infinite = true;
         m = 0.0f;
-        for (int k = tid; k < kTops; k += kThreads) sh.tops[k] = 0x7F80;  // (+inf: every chunk is looked at)
+        for (int k = tid; k < Shared<E>::kTops; k += kThreads) sh.tops[k] = 0x7F80;  // (+inf: every chunk is looked at)
         __syncthreads();
     }
     top = scalar(m);
     row.wide = true;
     row.top = scalar(double(m));
     row.base = 0;
-    row.each_under(sh, double(kBins), [&](int, float x) {
+    row.each_within(sh, row.lowest(kBins), INFINITY, [&](int, float x) {
         const double t = row.t_of(x);
-        if (t < double(kBins)) add_to(&sh.bins[int(t)], (uint64_t(1) << kMissBits) | miss_at(__builtin_amdgcn_fract(t)));
+        if (t < double(kBins)) add_to(&sh.bins[int(t)], added_at(__builtin_amdgcn_fract(t)));
     });
     __syncthreads();
     return true;
 }
 
 // A row's answer from its bins: one place on the axis of ranks after the other.
-template <typename T>
-__device__ __forceinline__ void choose(Shared& sh, const Row<T>& row, const SampleArgs& a, const Params& p, int64_t r, float top) {
+template <typename T, int E>
+__device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, const SampleArgs& a, const Params& p, int64_t r, float top) {
     const int tid = threadIdx.x;
     const bool greedy = p.temperature == 0.0f;
-    const double T_ = scalar(greedy ? 1.0 : double(p.temperature));
     auto slot = [&](int b) -> uint64_t { return sh.bins[(row.base + b) & (kBins - 1)]; };
     uint64_t tokens = 0, mine = 0, all_tokens, all_mass;
 #pragma unroll 2
@@ -603,8 +704,27 @@ __device__ __forceinline__ void choose(Shared& sh, const Row<T>& row, const Samp
     }
     const int tokens_before = int(sum_before(sh, tokens, &all_tokens));
     const uint64_t mass_before = sum_before(sh, mine, &all_mass);
-    Bin<T> bin{sh, row, -1};
-    const double low = scalar(p.min_p > 0.0f ? log(double(p.min_p)) : 0.0);
+    Bin<T, E> bin{sh, row, -1};
+    // min_p: the lowest logit that is kept, an estimate and then by the definition, and its bin
+    uint32_t cut_key = 0;
+    int cut_bin = kBins;
+    if (p.min_p > 0.0f && p.min_p <= 1.0f) {
+        const double T_ = greedy ? 1.0 : double(p.temperature), low = log(double(p.min_p));
+        auto keeps = [&](float x) { return (double(x) - double(top)) / T_ >= low; };
+        float cut = float(fmax(double(top) + T_ * low, -3.4e38));
+#pragma unroll 1
+        for (int k = 0; k < 4 && !keeps(cut); ++k) cut = nextafterf(cut, INFINITY);
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+            const float lower = nextafterf(cut, -INFINITY);
+            if (!(lower > -INFINITY) || !keeps(lower)) break;
+            cut = lower;
+        }
+        cut = fminf(cut, top);
+        const double t = row.t_of(cut) - double(row.base);
+        cut_key = uint32_t(scalar(int(key_of(cut))));
+        cut_bin = t < double(kBins) ? scalar(int(t)) : kBins + 1;
+    }
     const uint64_t top_weight = scalar(kOne - miss_at(bin.place(top, 0)));
     Prefix kept{kBins, 0, 0, 0, 0, all_mass, int(all_tokens)};
     const Prefix only_first{0, 1, 1, key_of(top), top_weight, 0, 0};
@@ -617,7 +737,6 @@ __device__ __forceinline__ void choose(Shared& sh, const Row<T>& row, const Samp
         By by = By::kCount;
         uint64_t reach = 0;
         double target = 0.0;
-        uint32_t cut_key = 0;
         if (stage == kTopK) {
             if (p.top_k == 0 || p.top_k >= int(all_tokens)) continue;
             reach = uint64_t(p.top_k);
@@ -632,25 +751,13 @@ __device__ __forceinline__ void choose(Shared& sh, const Row<T>& row, const Samp
             reach = uint64_t(target);
         } else if (stage == kMinP) {
             if (!(p.min_p > 0.0f)) continue;
-            if (!(low <= 0.0)) {
+            if (p.min_p > 1.0f) {
                 kept = only_first;
                 continue;
             }
-            // the lowest logit that is kept: an estimate, then by the definition
-            auto keeps = [&](float x) { return (double(x) - double(top)) / T_ >= low; };
-            float cut = float(fmax(double(top) + T_ * low, -3.4e38));
-            for (int k = 0; k < 4 && !keeps(cut); ++k) cut = nextafterf(cut, INFINITY);
-            for (int k = 0; k < 4; ++k) {
-                const float lower = nextafterf(cut, -INFINITY);
-                if (!(lower > -INFINITY) || !keeps(lower)) break;
-                cut = lower;
-            }
-            cut = fminf(cut, top);
-            const double t = row.t_of(cut) - double(row.base);
-            if (!(t < double(kBins)) || int(t) > kept.bin) continue;
+            if (cut_bin > kept.bin) continue;
             by = By::kCut;
-            reach = uint64_t(scalar(int(t))) + 1;
-            cut_key = uint32_t(scalar(int(key_of(cut))));
+            reach = uint64_t(cut_bin) + 1;
         } else if (stage == kDraw) {
             const uint64_t M = scalar(kept.all(sh));
             unit = scalar(0x1p44 / double(M));
@@ -703,7 +810,7 @@ __device__ __forceinline__ void choose(Shared& sh, const Row<T>& row, const Samp
     } else if (a.confidence == SANGAM_CONFIDENCE_ENTROPY) {
         double s = 0.0, none = 0.0;
         auto part = [&](double t) { return sh.bin_weight(int(t)) * double(kOne - miss_at(t - int(t))) * 0x1p-33 * t; };
-        row.each_under(sh, double(row.base + min(kept.bin + 1, kBins)), [&](int, float x) {
+        row.each_within(sh, row.lowest(min(kept.bin + 1, kBins)), INFINITY, [&](int, float x) {
             const double t = bin.place(x, 0);
             if (t < double(kept.bin) || (kept.tokens > 0 && t < double(kept.bin + 1) && key_of(x) < kept.key)) s += part(t);
         });
@@ -714,29 +821,300 @@ __device__ __forceinline__ void choose(Shared& sh, const Row<T>& row, const Samp
     answer(a, r, token, c);
 }
 
+// ---------------------------------------------------------------- rows of bf16
+
+// Adds a part of a row to the counts, which are all there behind the next barrier.
+template <int E>
+__device__ __forceinline__ void count(Shared<E>& sh, const Row<__bf16, E>& row, uint16_t* tops) {
+    uint32_t* const counts = sh.counts;
+    // (a value: its bits without the sign, held to [kTiny, kHuge], and the side: sign 0 or -1)
+    auto add = [&](uint32_t bits, int32_t sign) {
+        const uint32_t v = min(max(bits, uint32_t(kTiny)), uint32_t(kHuge));
+        atomicAdd(counts + (int(v) + ((sign & (kSide - kTiny)) | (~sign & -kTiny))), 1u);
+    };
+    row.each_chunk([&](int chunk, int v0, const auto& w) {
+        // the largest as whole numbers: where some are positive that of int32, else the smallest of uint32
+        int32_t most = INT32_MIN;
+        uint32_t least = UINT32_MAX;
+#pragma unroll
+        for (int j = 0; j < Row<__bf16, E>::kLoads; ++j) {
+            if (v0 + j * kThreads + int(threadIdx.x) >= row.last) continue;
+            typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+            const U4 u = __builtin_bit_cast(U4, w[j]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t low = u[e] << 16;
+                add(u[e] & 0x7FFFu, int32_t(low) >> 31);
+                add((u[e] >> 16) & 0x7FFFu, int32_t(u[e]) >> 31);
+                // (the lower half behind the upper one changes no order of upper halves)
+                most = max(max(most, int32_t(low)), int32_t(u[e]));
+                least = min(min(least, low), u[e]);
+            }
+        }
+        tops[chunk * kThreads + threadIdx.x] = uint16_t((most >= 0 ? uint32_t(most) : least) >> 16);
+    });
+    const int rest = row.first == 0 ? row.vocab - row.vectors * row.V : 0;
+    auto bits_of = [&](int i) { return uint32_t(__builtin_bit_cast(uint16_t, row.p[i])); };
+    if (int(threadIdx.x) < rest) {
+        const uint32_t u = bits_of(int(threadIdx.x) < row.head ? int(threadIdx.x) : int(threadIdx.x) + row.vectors * row.V);
+        add(u & 0x7FFFu, -int32_t(u >> 15));
+    }
+}
+
+// Takes the forbidden token out of the counts again.
+template <int E>
+__device__ __forceinline__ void uncount(Shared<E>& sh, const Row<__bf16, E>& row) {
+    if (threadIdx.x != 0 || row.forbid < 0) return;
+    const uint32_t u = __builtin_bit_cast(uint16_t, row.p[row.forbid]);
+    const int v = min(max(int(u & 0x7FFFu), kTiny), kHuge) - kTiny;
+    sh.counts[v + ((u & 0x8000u) ? kSide : 0)] -= 1;
+}
+
+// Values in rank order: place q's logit, and how many tokens have it.
+__device__ __forceinline__ float value_at(int q) {
+    if (q == kValues) return 0.0f;
+    return __uint_as_float(q < kValues ? uint32_t(kTiny + kValues - q) << 16 : (uint32_t(kTiny + q - kValues) << 16) | 0x80000000u);
+}
+template <int E>
+__device__ __forceinline__ int count_at(const Shared<E>& sh, int q) {
+    if (q >= kRanked) return 0;
+    if (q == kValues) return int(sh.counts[0] + sh.counts[kSide]);
+    return int(sh.counts[q < kValues ? kValues - q : kSide + q - kValues]);
+}
+
+// A prefix of the ranks: all tokens of the values before q, and the first
+// `tokens` of that value.
+struct ValuePrefix {
+    int q, tokens, before;
+    uint64_t mass;  // of the values before, units of 2^-44 of the largest weight
+};
+
+// A row's answer from its counts; false: they do not tell.
+template <int E>
+__device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& row, const SampleArgs& a, const Params& p, int64_t r) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    // the largest value
+    int q0 = kRanked;
+#pragma unroll 1
+    for (int j = kOwn - 1; j >= 0; --j)
+        if (count_at(sh, tid * kOwn + j) > 0) q0 = tid * kOwn + j;
+    if (tid == 0) sh.found = kRanked;
+    __syncthreads();
+    if (q0 < kRanked) atomicMin(&sh.found, q0);
+    __syncthreads();
+    q0 = scalar(sh.found);
+    const float top = value_at(q0);
+    if (q0 == kRanked || sh.counts[kSide - 1] > 0) return false;
+    // (no weight below -2^8, or none is there)
+    if (sh.counts[2 * kSide - 1] > 0 && !((double(top) + 0x1p8) * row.scale >= double(kBins))) return false;
+    const double scale = row.scale;
+    auto t_of = [&](float x) { return (double(top) - double(x)) * scale; };
+    // weight of a token: bin, and units of 2^-33 of its largest
+    auto token_weight = [&](double t, int* b) -> uint64_t {
+        *b = t < double(kBins) ? int(t) : 0;
+        return t < double(kBins) ? kOne - miss_at(t - double(*b)) : 0;
+    };
+    auto mass_at = [&](int q, int n) -> uint64_t {
+        if (n == 0) return 0;
+        int b;
+        const uint64_t v = token_weight(t_of(value_at(q)), &b);
+        return sh.mass_of(b, uint64_t(n) * v);
+    };
+    uint64_t tokens = 0, mine = 0, all_tokens, all_mass;
+#pragma unroll 1
+    for (int j = 0; j < kOwn; ++j) {
+        const int q = tid * kOwn + j, n = count_at(sh, q);
+        tokens += n;
+        mine += mass_at(q, n);
+    }
+    const int tokens_before = int(sum_before(sh, tokens, &all_tokens));
+    const uint64_t mass_before = sum_before(sh, mine, &all_mass);
+    // what the tiny ones weigh may be off by 2^-28 of it
+    if (mass_at(kValues, count_at(sh, kValues)) > all_mass / 32) return false;
+    ValuePrefix kept{kRanked, 0, int(all_tokens), all_mass};
+    auto per_token = [&](int q) -> double {
+        int b;
+        const uint64_t v = token_weight(t_of(value_at(q)), &b);
+        return sh.bin_weight(b) * double(v) * 2048.0;
+    };
+    auto all_of = [&](const ValuePrefix& x) -> uint64_t { return x.mass + (x.tokens ? mass_at(x.q, x.tokens) : 0); };
+    double unit = 0.0, weight = 0.0, second = 0.0;
+    int drawn = 0, place = 0, drawn_tokens = 0;
+    int cut_q = kRanked;  // min_p: the first value that is not kept
+    if (p.min_p > 0.0f && p.min_p <= 1.0f) {
+        const double T_ = p.temperature == 0.0f ? 1.0 : double(p.temperature), low = log(double(p.min_p));
+        int lo = q0, hi = kRanked;  // (kept at lo)
+#pragma unroll 1
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if ((double(value_at(mid)) - double(top)) / T_ >= low) lo = mid;
+            else hi = mid;
+        }
+        cut_q = scalar(hi);
+    }
+    enum Stage { kTopK, kTopP, kMinP, kDraw, kSecond, kStages };
+#pragma unroll 1
+    for (int stage = kTopK; stage < kStages; ++stage) {
+        By by = By::kCount;
+        uint64_t reach = 0;
+        double target = 0.0;
+        if (stage == kTopK) {
+            if (p.top_k == 0 || p.top_k >= int(all_tokens)) continue;
+            reach = uint64_t(p.top_k);
+        } else if (stage == kTopP) {
+            if (!(p.top_p < 1.0f)) continue;
+            target = scalar(ceil(double(p.top_p) * double(all_of(kept))));
+            if (!(target > 0.0)) {
+                kept = ValuePrefix{q0, 1, 0, 0};
+                continue;
+            }
+            by = By::kReach;
+            reach = uint64_t(target);
+        } else if (stage == kMinP) {
+            if (!(p.min_p > 0.0f)) continue;
+            if (p.min_p > 1.0f) {
+                kept = ValuePrefix{q0, 1, 0, 0};
+                continue;
+            }
+            if (cut_q > kept.q) continue;
+            by = By::kCut;
+            reach = uint64_t(cut_q);
+        } else if (stage == kDraw) {
+            const uint64_t M = scalar(all_of(kept));
+            unit = scalar(0x1p44 / double(M));
+            const float u = p.temperature == 0.0f ? 0.0f : a.u[r];
+            target = scalar(fmin(u > 0.0f ? double(u) * double(M) : 0.0, double(M - 1)));
+            by = By::kAbove;
+            reach = uint64_t(target) + 1;
+        } else {
+            if (a.confidence != SANGAM_CONFIDENCE_MARGIN || kept.before + kept.tokens < 2) continue;
+            reach = 2;
+        }
+        // the thread whose values the place lies in, then the value: its end is the first at or above `reach`
+        __syncthreads();
+        if (tid == 0) sh.found = -1;
+        __syncthreads();
+        const uint64_t lo = by == By::kCount ? uint64_t(tokens_before) : by == By::kCut ? uint64_t(tid) * kOwn : mass_before;
+        const uint64_t more = by == By::kCount ? tokens : by == By::kCut ? uint64_t(kOwn) : mine;
+        if (lo < reach && lo + more >= reach) {
+            sh.found = tid;
+            sh.found_tokens = tokens_before;
+            sh.found_mass = mass_before;
+        }
+        __syncthreads();
+        const int owner = scalar(sh.found);
+        if (owner < 0) continue;
+        const int q = owner * kOwn + lane, n = lane < kOwn ? count_at(sh, q) : 0;
+        const uint64_t m = lane < kOwn ? mass_at(q, n) : 0;
+        const uint64_t n_end = uint64_t(scalar(sh.found_tokens)) + wave_up_to(uint64_t(n)), m_end = scalar(sh.found_mass) + wave_up_to(m);
+        const uint64_t end = by == By::kCount ? n_end : by == By::kCut ? uint64_t(q) + 1 : m_end;
+        const int at = __builtin_ctzll(__ballot(lane < kOwn && end >= reach) | (uint64_t(1) << 63));
+        ValuePrefix x{owner * kOwn + at, 0, int(scalar(int(__shfl(int(n_end), at) - __shfl(n, at)))), 0};
+        x.mass = scalar(uint64_t(__shfl(m_end, at) - __shfl(m, at)));
+        const int here = scalar(__shfl(n, at));
+        if (x.q > kept.q) continue;  // (not met within what is kept)
+        const int most = x.q == kept.q ? kept.tokens : here;
+        const double each = scalar(per_token(x.q));
+        x.tokens = here;
+        if (by == By::kCount) x.tokens = int(reach) - x.before;
+        if (by == By::kReach) x.tokens = scalar(max(1, min(here, int(ceil((target - double(x.mass)) / each)))));
+        if (by == By::kAbove) x.tokens = scalar(max(1, min(most, int(floor((target - double(x.mass)) / each)) + 1)));
+        if (x.q == kValues && x.tokens > 0) return false;
+        if (stage <= kMinP) {
+            if (x.q < kept.q || x.tokens < kept.tokens) kept = x;
+        } else if (stage == kDraw) {
+            drawn = x.q;
+            place = x.tokens;
+            drawn_tokens = here;
+            weight = scalar(each * 0x1p-44);
+        } else {
+            second = scalar(each * 0x1p-44);
+        }
+    }
+    // the token: the place-th by index among those with its logit
+    const float x = value_at(drawn);
+    int token;
+    if (drawn_tokens <= kList) {
+        __syncthreads();
+        if (tid == 0) sh.listed = 0;
+        row.each_within(sh, x, x, [&](int i, float) {
+            const int k = atomicAdd(&sh.listed, 1);
+            if (k < kList) sh.list[k] = uint32_t(i);
+        });
+        __syncthreads();
+        if (tid < drawn_tokens) {
+            const uint64_t mine_ = sh.list[tid];
+            int rank = 1;
+            for (int j = 0; j < drawn_tokens; ++j) rank += sh.list[j] < mine_;
+            if (rank == place) sh.index = int(mine_);
+        }
+        __syncthreads();
+        token = sh.index;
+    } else {
+        Bin<__bf16, E> bin{sh, row, -1};
+        token = bin.index_of(Prefix{0, 0, place, key_of(x), 0, 0, 0});
+    }
+    double c = weight * unit;
+    if (a.confidence == SANGAM_CONFIDENCE_MARGIN) {
+        c = (1.0 - second) * unit;
+    } else if (a.confidence == SANGAM_CONFIDENCE_ENTROPY) {
+        double s = 0.0, none = 0.0;
+#pragma unroll 1
+        for (int j = 0; j < kOwn; ++j) {
+            const int q = tid * kOwn + j, n = q < kept.q ? count_at(sh, q) : q == kept.q ? kept.tokens : 0;
+            const double t = t_of(value_at(q));
+            int b;
+            if (n > 0 && t < double(kBins)) s += double(n) * sh.bin_weight(int(t)) * double(token_weight(t, &b)) * 0x1p-33 * t;
+        }
+        sum_all(sh, s, none);
+        c = -(s * unit * (0.69314718055994530942 / 64) - log(unit));
+    }
+    answer(a, r, token, c);
+    return true;
+}
+
+template <typename T, int E>
+__device__ __forceinline__ Row<T, E> row_of(const SampleArgs& a, int64_t r, const Params& p) {
+    Row<T, E> row;
+    row.p = static_cast<const T*>(a.logits) + r * a.row_stride;
+    row.vocab = a.vocab;
+    row.forbid = a.forbid;
+    row.infinite = row.wide = false;
+    row.head = min(int((16 - (reinterpret_cast<uintptr_t>(row.p) & 15)) & 15) / int(sizeof(T)), a.vocab);
+    row.vectors = (a.vocab - row.head) / row.V;
+    row.first = 0;
+    row.last = row.vectors;
+    row.top = 0.0;
+    row.base = 0;
+    row.scale = scalar(64.0 * 1.4426950408889634074 / (p.temperature == 0.0f ? 1.0 : double(p.temperature)));
+    return row;
+}
+
+// A work-group takes a row.
 template <typename T>
-__global__ __launch_bounds__(kThreads, 4) void sample_kernel(SampleArgs a) {
-    __shared__ Shared sh;
-    constexpr int V = Row<T>::V;
+__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
+    constexpr int E = kWhole<T>;
+    __shared__ Shared<E> sh;
     const int64_t r = blockIdx.x;
     const Params p = params_of(a, r);
     if (p.none) {
         answer(a, r, -1, 0.0);
         return;
     }
-    Row<T> row;
-    row.p = static_cast<const T*>(a.logits) + r * a.row_stride;
-    row.vocab = a.vocab;
-    row.forbid = a.forbid;
-    row.infinite = row.wide = false;
-    row.head = min(int((16 - (reinterpret_cast<uintptr_t>(row.p) & 15)) & 15) / int(sizeof(T)), a.vocab);
-    row.vectors = (a.vocab - row.head) / V;
-    row.top = 0.0;
-    row.base = 0;
-    row.scale = scalar(64.0 * 1.4426950408889634074 / (p.temperature == 0.0f ? 1.0 : double(p.temperature)));
+    Row<T, E> row = row_of<T, E>(a, r, p);
     if (threadIdx.x < 64) sh.powers[threadIdx.x] = exp2(threadIdx.x * (-1.0 / 64));
+    if constexpr (__is_same(T, __bf16)) {
+        for (int k = threadIdx.x; k < 2 * kSide; k += kThreads) sh.counts[k] = 0;
+        __syncthreads();
+        count(sh, row, sh.tops);
+        __syncthreads();
+        uncount(sh, row);
+        __syncthreads();
+        if (choose_by_value(sh, row, a, p, r)) return;
+        __syncthreads();
+    }
     float top;
-    if (!fill(sh, row, top) && !fill_wide(sh, row, top)) {
+    if (!fill(sh, row, top, sh.tops) && !fill_wide(sh, row, top)) {
         answer(a, r, -1, 0.0);
         return;
     }
