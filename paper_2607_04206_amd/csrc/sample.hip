@@ -17,7 +17,7 @@
 // lie in a circle, and where a chunk of the row has a larger logit than all
 // before, the bins that fall out at the far end are cleared for it.
 //
-// Logits in bf16 take few values: from 2^-28 to 2^8 there are 4608 of either
+// Logits in bf16 take few values: from 2^-24 to 2^8 there are 4096 of either
 // sign. There a row is counted by its values themselves, six instructions a
 // logit and no exponential but one a value; rows that reach beyond (an
 // infinity, a place among the tiny ones) go the way of the others.
@@ -97,17 +97,15 @@ struct SampleArgs {
 
 // Values of bf16 by the bits without the sign: those up to kTiny count as 0, those
 // from kHuge on have no value (infinities and what is no number among them).
-constexpr int kTiny = (127 - 28) * 128 - 1, kHuge = (127 + 8) * 128;
+constexpr int kTiny = (127 - 24) * 128 - 1, kHuge = (127 + 8) * 128;
 constexpr int kSide = kHuge - kTiny + 1;           // counts of a sign: tiny, the values, huge
 constexpr int kValues = kSide - 2;                 // of a sign
 constexpr int kRanked = 2 * kValues + 1;           // values in rank order, 0 (tiny) at kValues
 constexpr int kOwn = (kRanked + kThreads - 1) / kThreads;  // of a thread
 static_assert(kOwn <= 64, "a wave looks at a thread's values");
 
-// E: logits of a thread in a chunk.
-template <int E>
-struct Shared {
-    static constexpr int kTops = kMaxVocab / E;
+// What a look at a row or a part of it gives.
+struct Counts {
     union {
         struct {
             uint64_t bins[kBins];  // of floor(t) mod kBins
@@ -115,6 +113,13 @@ struct Shared {
         };
         uint32_t counts[2 * kSide];
     };
+    float wave_top[2][kWaves];
+};
+
+// E: logits of a thread in a chunk.
+template <int E>
+struct Shared : Counts {
+    static constexpr int kTops = kMaxVocab / E;
     union {
         struct {
             uint64_t list[kList];    // key and index; then the weight up to each
@@ -126,9 +131,8 @@ struct Shared {
         uint64_t digits[256];
     };
     uint16_t tops[kTops];  // the largest logit of a thread's chunk (rounded up to 16 bits); entry chunk * kThreads + thread
-    uint64_t part[kWaves];
+    uint64_t part[2 * kWaves];
     double sums[2 * kWaves];
-    float wave_top[2][kWaves];
     uint64_t found_mass, found_bin;
     int found, found_tokens, found_last, listed, queued;
     int32_t index;
@@ -184,13 +188,21 @@ __device__ __forceinline__ float wave_max(float x) {
     return x;
 }
 
+// x of the lane that a DPP control names, 0 where there is none.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ uint64_t from_lane(uint64_t x) {
+    const int low = __builtin_amdgcn_update_dpp(0, int(x), CONTROL, ROWS, 0xF, false);
+    const int high = __builtin_amdgcn_update_dpp(0, int(x >> 32), CONTROL, ROWS, 0xF, false);
+    return uint64_t(uint32_t(high)) << 32 | uint32_t(low);
+}
+// Sum over the lanes up to this one: within rows of 16, then from row to row.
 __device__ __forceinline__ uint64_t wave_up_to(uint64_t x) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const uint64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+    x += from_lane<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8
+    x += from_lane<0x112, 0xF>(x);
+    x += from_lane<0x114, 0xF>(x);
+    x += from_lane<0x118, 0xF>(x);
+    x += from_lane<0x142, 0xA>(x);  // row_bcast 15 into rows 1 and 3
+    x += from_lane<0x143, 0xC>(x);  // row_bcast 31 into rows 2 and 3
     return x;
 }
 
@@ -211,6 +223,32 @@ __device__ __forceinline__ uint64_t sum_before(Shared<E>& sh, uint64_t x, uint64
     }
     *total = scalar(all);
     return before + up_to - x;
+}
+
+// The same for two at once: before becomes what lies before this thread, all the sums.
+template <int E>
+__device__ __forceinline__ void sums_before(Shared<E>& sh, uint64_t x, uint64_t y, uint64_t (&before)[2], uint64_t (&all)[2]) {
+    const int wave = threadIdx.x / 64;
+    const uint64_t up_to[2] = {wave_up_to(x), wave_up_to(y)};
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) {
+        sh.part[wave] = up_to[0];
+        sh.part[kWaves + wave] = up_to[1];
+    }
+    __syncthreads();
+    before[0] = up_to[0] - x;
+    before[1] = up_to[1] - y;
+    uint64_t total[2] = {0, 0};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint64_t p = sh.part[k * kWaves + w];
+            if (w < wave) before[k] += p;
+            total[k] += p;
+        }
+    all[0] = scalar(total[0]);
+    all[1] = scalar(total[1]);
 }
 
 // Sums over all threads, in a fixed order.
@@ -461,9 +499,10 @@ struct Bin {
             __syncthreads();
             const uint64_t bin = d < 256 ? sh.digits[d] : 0;
             const int more = tokens_in(bin);
-            uint64_t total;
-            const int n = before + int(sum_before(sh, more, &total));
-            const uint64_t w = weight_before + sum_before(sh, weight_in(bin), &total), after = w + weight_in(bin);
+            uint64_t up_to[2], total[2];
+            sums_before(sh, uint64_t(more), weight_in(bin), up_to, total);
+            const int n = before + int(up_to[0]);
+            const uint64_t w = weight_before + up_to[1], after = w + weight_in(bin);
             const bool here = by == By::kCount   ? n < count && n + more >= count
                               : by == By::kReach ? double(w) < weight && double(after) >= weight
                               : by == By::kAbove ? double(w) <= weight && double(after) > weight
@@ -579,14 +618,15 @@ __device__ __forceinline__ void answer(const SampleArgs& a, int64_t r, int token
     }
 }
 
-// The bins of a whole row, whose largest logit becomes `top`; false: its x / T is
-// too large, or infinite, for bins that do not hang on it.
+// The bins of a row or part, whose largest logit becomes `top`.
+enum Filled : int32_t { kFar, kFilled, kNothing };  // kFar: its x / T is too large, or infinite, for bins that do not hang on it
 template <typename T, int E>
-__device__ __forceinline__ bool fill(Shared<E>& sh, Row<T, E>& row, float& top, uint16_t* tops) {
+__device__ __forceinline__ Filled fill(Counts& sh, Row<T, E>& row, float& top, uint16_t* tops) {
     constexpr int V = Row<T, E>::V;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
     top = -INFINITY;
-    if (!(row.scale > 1e-30)) return false;  // (all that is finite may weigh the same)
+    if (!(row.scale > 1e-30)) return kFar;  // (all that is finite may weigh the same)
+    bool low = false;  // logits below all bins
     int parity = 0;
     // a chunk's largest logit is in: whether its logits are to be added
     auto raise = [&](float mine) {
@@ -599,7 +639,10 @@ __device__ __forceinline__ bool fill(Shared<E>& sh, Row<T, E>& row, float& top, 
         parity ^= 1;
         if (!(m > top)) return top > -INFINITY;
         const double t = row.t_of(m);
-        if (t >= kHighest) return false;  // so low that bins may not be kept for it
+        if (t >= kHighest) {  // so low that bins may not be kept for it
+            low = true;
+            return false;
+        }
         const int to = t >= kLowest ? int(t) : 0;
         if (top > -INFINITY) {
             for (int b = to + tid; b < row.base && b < to + kBins; b += kThreads) sh.bins[b & (kBins - 1)] = 0;
@@ -618,7 +661,7 @@ __device__ __forceinline__ bool fill(Shared<E>& sh, Row<T, E>& row, float& top, 
     auto add = [&](float x, float lowest) {
         const double t = __builtin_fma(-double(x), row.scale, kOrigin);
         const int at = x >= lowest ? __double2hiint(t) & (kBins - 1) : kBins;
-        static_assert(offsetof(Shared<E>, beyond) == kBins * sizeof(uint64_t), "beyond lies behind the bins");
+        static_assert(offsetof(Counts, beyond) == kBins * sizeof(uint64_t), "beyond lies behind the bins");
         add_to(bins + at, added_at(__builtin_amdgcn_fract(t)));
     };
     for (int b = tid; b < kBins; b += kThreads) sh.bins[b] = 0;
@@ -645,7 +688,8 @@ __device__ __forceinline__ bool fill(Shared<E>& sh, Row<T, E>& row, float& top, 
         }
     }
     __syncthreads();
-    return top > -INFINITY && row.base > 0 && row.base + kBins <= int(kHighest);
+    if (top == -INFINITY) return low ? kFar : kNothing;
+    return row.base > 0 && row.base + kBins <= int(kHighest) ? kFilled : kFar;
 }
 
 // The same by two looks, for any row. False: the row has no weight.
@@ -695,15 +739,17 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
     const int tid = threadIdx.x;
     const bool greedy = p.temperature == 0.0f;
     auto slot = [&](int b) -> uint64_t { return sh.bins[(row.base + b) & (kBins - 1)]; };
-    uint64_t tokens = 0, mine = 0, all_tokens, all_mass;
+    uint64_t tokens = 0, mine = 0;
 #pragma unroll 2
     for (int j = 0; j < kEach; ++j) {
         const uint64_t bin = slot(tid * kEach + j);
         tokens += tokens_in(bin);
         mine += sh.mass_of(tid * kEach + j, weight_in(bin));
     }
-    const int tokens_before = int(sum_before(sh, tokens, &all_tokens));
-    const uint64_t mass_before = sum_before(sh, mine, &all_mass);
+    uint64_t before[2], all[2];
+    sums_before(sh, tokens, mine, before, all);
+    const int tokens_before = int(before[0]);
+    const uint64_t mass_before = before[1], all_tokens = all[0], all_mass = all[1];
     Bin<T, E> bin{sh, row, -1};
     // min_p: the lowest logit that is kept, an estimate and then by the definition, and its bin
     uint32_t cut_key = 0;
@@ -825,7 +871,7 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
 
 // Adds a part of a row to the counts, which are all there behind the next barrier.
 template <int E>
-__device__ __forceinline__ void count(Shared<E>& sh, const Row<__bf16, E>& row, uint16_t* tops) {
+__device__ __forceinline__ void count(Counts& sh, const Row<__bf16, E>& row, uint16_t* tops) {
     uint32_t* const counts = sh.counts;
     // (a value: its bits without the sign, held to [kTiny, kHuge], and the side: sign 0 or -1)
     auto add = [&](uint32_t bits, int32_t sign) {
@@ -893,11 +939,13 @@ struct ValuePrefix {
 template <int E>
 __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& row, const SampleArgs& a, const Params& p, int64_t r) {
     const int tid = threadIdx.x, lane = tid & 63;
-    // the largest value
-    int q0 = kRanked;
-#pragma unroll 1
-    for (int j = kOwn - 1; j >= 0; --j)
-        if (count_at(sh, tid * kOwn + j) > 0) q0 = tid * kOwn + j;
+    // the thread's values' counts, and the largest value
+    int own[kOwn], q0 = kRanked;
+#pragma unroll
+    for (int j = kOwn - 1; j >= 0; --j) {
+        own[j] = count_at(sh, tid * kOwn + j);
+        if (own[j] > 0) q0 = tid * kOwn + j;
+    }
     if (tid == 0) sh.found = kRanked;
     __syncthreads();
     if (q0 < kRanked) atomicMin(&sh.found, q0);
@@ -920,17 +968,24 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
         const uint64_t v = token_weight(t_of(value_at(q)), &b);
         return sh.mass_of(b, uint64_t(n) * v);
     };
-    uint64_t tokens = 0, mine = 0, all_tokens, all_mass;
-#pragma unroll 1
+    uint64_t tokens = 0, mine = 0;
+    double spread = 0.0;  // weights times t
+#pragma unroll
     for (int j = 0; j < kOwn; ++j) {
-        const int q = tid * kOwn + j, n = count_at(sh, q);
-        tokens += n;
-        mine += mass_at(q, n);
+        if (__ballot(own[j] > 0) == 0) continue;
+        const int q = tid * kOwn + j;
+        const uint64_t m = mass_at(q, own[j]);
+        tokens += own[j];
+        mine += m;
+        if (m > 0) spread += double(m) * t_of(value_at(q));
+        if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
-    const int tokens_before = int(sum_before(sh, tokens, &all_tokens));
-    const uint64_t mass_before = sum_before(sh, mine, &all_mass);
-    // what the tiny ones weigh may be off by 2^-28 of it
-    if (mass_at(kValues, count_at(sh, kValues)) > all_mass / 32) return false;
+    uint64_t before[2], all[2];
+    sums_before(sh, tokens, mine, before, all);
+    const int tokens_before = int(before[0]);
+    const uint64_t mass_before = before[1], all_tokens = all[0], all_mass = all[1];
+    // (what the tiny ones weigh may be off by 2^-24 of it)
+    if (mass_at(kValues, count_at(sh, kValues)) > all_mass / 512) return false;
     ValuePrefix kept{kRanked, 0, int(all_tokens), all_mass};
     auto per_token = [&](int q) -> double {
         int b;
@@ -1058,16 +1113,18 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
     if (a.confidence == SANGAM_CONFIDENCE_MARGIN) {
         c = (1.0 - second) * unit;
     } else if (a.confidence == SANGAM_CONFIDENCE_ENTROPY) {
-        double s = 0.0, none = 0.0;
+        double none = 0.0;
+        if (kept.q < kRanked) {
+            spread = 0.0;
 #pragma unroll 1
-        for (int j = 0; j < kOwn; ++j) {
-            const int q = tid * kOwn + j, n = q < kept.q ? count_at(sh, q) : q == kept.q ? kept.tokens : 0;
-            const double t = t_of(value_at(q));
-            int b;
-            if (n > 0 && t < double(kBins)) s += double(n) * sh.bin_weight(int(t)) * double(token_weight(t, &b)) * 0x1p-33 * t;
+            for (int j = 0; j < kOwn && tid * kOwn + j <= kept.q; ++j) {
+                const int q = tid * kOwn + j;
+                const uint64_t m = mass_at(q, q < kept.q ? count_at(sh, q) : kept.tokens);
+                if (m > 0) spread += double(m) * t_of(value_at(q));
+            }
         }
-        sum_all(sh, s, none);
-        c = -(s * unit * (0.69314718055994530942 / 64) - log(unit));
+        sum_all(sh, spread, none);
+        c = -(spread * 0x1p-44 * unit * (0.69314718055994530942 / 64) - log(unit));
     }
     answer(a, r, token, c);
     return true;
@@ -1090,10 +1147,28 @@ __device__ __forceinline__ Row<T, E> row_of(const SampleArgs& a, int64_t r, cons
     return row;
 }
 
-// A work-group takes a row.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
-    constexpr int E = kWhole<T>;
+// A row's answer from its logits alone, whatever they are.
+template <typename T, int E>
+__device__ __forceinline__ void from_logits(Shared<E>& sh, Row<T, E>& row, const SampleArgs& a, const Params& p, int64_t r) {
+    float top;
+    if (fill(sh, row, top, sh.tops) != kFilled && !fill_wide(sh, row, top)) {
+        answer(a, r, -1, 0.0);
+        return;
+    }
+    choose(sh, row, a, p, r, top);
+}
+
+template <int E>
+__device__ __forceinline__ void start(Shared<E>& sh) {
+    if (threadIdx.x < 64) sh.powers[threadIdx.x] = exp2(threadIdx.x * (-1.0 / 64));
+}
+
+constexpr int kPending = -2;  // the token of a row that its values did not tell
+
+// A work-group takes a row of bf16. (What sample_kernel takes more registers for
+// is left to it: three work-groups fit a CU.)
+__global__ __launch_bounds__(kThreads, 6) void sample_values_kernel(SampleArgs a) {
+    constexpr int E = kWhole<__bf16>;
     __shared__ Shared<E> sh;
     const int64_t r = blockIdx.x;
     const Params p = params_of(a, r);
@@ -1101,24 +1176,194 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         answer(a, r, -1, 0.0);
         return;
     }
-    Row<T, E> row = row_of<T, E>(a, r, p);
-    if (threadIdx.x < 64) sh.powers[threadIdx.x] = exp2(threadIdx.x * (-1.0 / 64));
+    Row<__bf16, E> row = row_of<__bf16, E>(a, r, p);
+    start(sh);
+    for (int k = threadIdx.x; k < 2 * kSide; k += kThreads) sh.counts[k] = 0;
+    __syncthreads();
+    count(sh, row, sh.tops);
+    __syncthreads();
+    uncount(sh, row);
+    __syncthreads();
+    if (!choose_by_value(sh, row, a, p, r)) answer(a, r, kPending, 0.0);
+}
+
+// A work-group takes a row, or the pending ones of some rows.
+template <typename T, bool PENDING>
+__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, int64_t rows) {
+    constexpr int E = kWhole<T>;
+    __shared__ Shared<E> sh;
+    const int64_t step = gridDim.x;
+    start(sh);
+    for (int64_t r0 = blockIdx.x; r0 < rows; r0 += 64 * step) {
+        uint64_t todo = 1;
+        if (PENDING) {
+            const int64_t mine = r0 + (threadIdx.x & 63) * step;
+            todo = __ballot(mine < rows && a.tokens[mine] == kPending);
+            __syncthreads();  // (all waves have looked before a row gets its token)
+        }
+        while (todo) {
+            const int64_t r = r0 + __builtin_ctzll(todo) * step;
+            todo &= todo - 1;
+            const Params p = params_of(a, r);
+            if (p.none) {
+                answer(a, r, -1, 0.0);
+                continue;
+            }
+            Row<T, E> row = row_of<T, E>(a, r, p);
+            __syncthreads();
+            from_logits(sh, row, a, p, r);
+        }
+        if (!PENDING) break;
+    }
+}
+
+// Few rows are cut into parts, of some chunks each: a work-group counts a part, and
+// another puts the parts of a row together and goes on from there.
+struct Split {
+    int parts, chunks_each, chunks;
+    int64_t record, row_bytes;  // of a part, of a row's parts and tops
+    uint8_t* workspace;
+};
+
+struct PartHead {
+    float top;
+    int32_t base, filled;
+};
+constexpr int kRecordValues = (2 * kSide * int(sizeof(uint16_t)) + 255) / 256 * 256;
+constexpr int kRecordBins = kBins * int(sizeof(uint64_t)) + 256;
+constexpr int kMostChunks = 65535 / (kThreads * kPart);  // of a part: counts fit 16 bits
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_part_kernel(SampleArgs a, Split s) {
+    __shared__ Counts sh;
+    const int64_t r = blockIdx.x / s.parts;
+    const int part = blockIdx.x % s.parts;
+    const Params p = params_of(a, r);
+    if (p.none) return;
+    Row<T, kPart> row = row_of<T, kPart>(a, r, p);
+    row.first = min(part * s.chunks_each * row.kChunk, row.vectors);
+    row.last = min(row.first + s.chunks_each * row.kChunk, row.vectors);
+    uint8_t* const at = s.workspace + r * s.row_bytes;
+    uint16_t* const tops = reinterpret_cast<uint16_t*>(at + s.parts * s.record);
+    uint8_t* const record = at + part * s.record;
     if constexpr (__is_same(T, __bf16)) {
         for (int k = threadIdx.x; k < 2 * kSide; k += kThreads) sh.counts[k] = 0;
         __syncthreads();
-        count(sh, row, sh.tops);
+        count(sh, row, tops);
+        __syncthreads();
+        for (int k = threadIdx.x; k < kSide; k += kThreads)
+            reinterpret_cast<uint32_t*>(record)[k] = sh.counts[2 * k] | (sh.counts[2 * k + 1] << 16);
+    } else {
+        float top;
+        const Filled filled = fill(sh, row, top, tops);
+        for (int k = threadIdx.x; k < kBins; k += kThreads) reinterpret_cast<uint64_t*>(record)[k] = sh.bins[k];
+        if (threadIdx.x == 0) *reinterpret_cast<PartHead*>(record + kBins * sizeof(uint64_t)) = PartHead{top, row.base, filled};
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_join_kernel(SampleArgs a, Split s) {
+    __shared__ Shared<kPart> sh;
+    const int64_t r = blockIdx.x;
+    const Params p = params_of(a, r);
+    if (p.none) {
+        answer(a, r, -1, 0.0);
+        return;
+    }
+    Row<T, kPart> row = row_of<T, kPart>(a, r, p);
+    start(sh);
+    const uint8_t* const at = s.workspace + r * s.row_bytes;
+    typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+    const U4* const tops = reinterpret_cast<const U4*>(at + s.parts * s.record);
+    static_assert(offsetof(Shared<kPart>, tops) % 16 == 0, "tops are copied 16 bytes at a time");
+#pragma unroll 4
+    for (int k = threadIdx.x; k < s.chunks * kThreads / 8; k += kThreads) reinterpret_cast<U4*>(sh.tops)[k] = tops[k];
+    if constexpr (__is_same(T, __bf16)) {
+        // eight counts at a time, of all the parts
+        constexpr int kPieces = kRecordValues / 16, kMine = (kPieces + kThreads - 1) / kThreads;
+        uint32_t sums[kMine][8] = {};
+#pragma unroll 4
+        for (int part = 0; part < s.parts; ++part) {
+            const U4* const piece = reinterpret_cast<const U4*>(at + part * s.record);
+            U4 w[kMine];
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) w[j] = piece[min(int(threadIdx.x) + j * kThreads, kPieces - 1)];
+#pragma unroll
+            for (int j = 0; j < kMine; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sums[j][2 * e] += w[j][e] & 0xFFFFu;
+                    sums[j][2 * e + 1] += w[j][e] >> 16;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = (int(threadIdx.x) + j * kThreads) * 8 + e;
+                if (k < 2 * kSide) sh.counts[k] = sums[j][e];
+            }
         __syncthreads();
         uncount(sh, row);
         __syncthreads();
         if (choose_by_value(sh, row, a, p, r)) return;
-        __syncthreads();
+    } else {
+        float top = -INFINITY;
+        bool far = false, any = false;
+        for (int part = 0; part < s.parts; ++part) {
+            const PartHead h = *reinterpret_cast<const PartHead*>(at + part * s.record + kBins * sizeof(uint64_t));
+            far = far || h.filled == kFar;
+            if (h.filled == kFilled && h.top > top) {
+                any = true;
+                top = h.top;
+                row.base = h.base;
+            }
+        }
+        if (any && !far) {
+            uint64_t sums[kEach] = {};
+#pragma unroll 2
+            for (int part = 0; part < s.parts; ++part) {
+                const uint8_t* const record = at + part * s.record;
+                const PartHead h = *reinterpret_cast<const PartHead*>(record + kBins * sizeof(uint64_t));
+                uint64_t w[kEach];
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) w[j] = reinterpret_cast<const uint64_t*>(record)[threadIdx.x + j * kThreads];
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    // (the bin whose slot k is; the part's slot may hold the bin a circle on)
+                    const int k = int(threadIdx.x) + j * kThreads, b = row.base + ((k - row.base) & (kBins - 1));
+                    if (h.filled == kFilled && b >= h.base) sums[j] += w[j];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) sh.bins[threadIdx.x + j * kThreads] = sums[j];
+            __syncthreads();
+            choose(sh, row, a, p, r, top);
+            return;
+        }
     }
-    float top;
-    if (!fill(sh, row, top, sh.tops) && !fill_wide(sh, row, top)) {
-        answer(a, r, -1, 0.0);
-        return;
+    __syncthreads();
+    from_logits(sh, row, a, p, r);
+}
+
+// Work-groups that the parts make if they can: three a CU.
+constexpr int64_t kGroups = 3 * 256;
+
+Split split_of(int64_t rows, int32_t vocab, int32_t dtype) {
+    Split s{};
+    constexpr int chunk = kThreads * kPart;
+    s.chunks = (vocab + chunk - 1) / chunk;
+    if (rows < 1 || rows >= kGroups) {
+        s.parts = 1;
+        return s;
     }
-    choose(sh, row, a, p, r, top);
+    const int64_t wanted = std::max<int64_t>((kGroups + rows - 1) / rows, (s.chunks + kMostChunks - 1) / kMostChunks);
+    const int parts = int(std::min<int64_t>(wanted, s.chunks));
+    s.chunks_each = (s.chunks + parts - 1) / parts;
+    s.parts = (s.chunks + s.chunks_each - 1) / s.chunks_each;
+    s.record = dtype == SANGAM_DTYPE_BF16 ? kRecordValues : kRecordBins;
+    s.row_bytes = s.parts * s.record + int64_t(s.chunks) * kThreads * int64_t(sizeof(uint16_t));
+    return s;
 }
 
 sangam_status fail(sangam_status code, const std::string& msg) {
@@ -1158,9 +1403,25 @@ sangam_status sample(const sangam_sample_desc* d, int32_t* tokens, float* confid
     if (need > 0 && reinterpret_cast<uintptr_t>(workspace) % 256) return fail(SANGAM_ERR_ALIGN, "workspace must be 256-byte aligned");
     SampleArgs args{d->logits, d->row_stride, d->u, d->params_of, d->num_params, d->temperatures, d->top_ks, d->top_ps, d->min_ps,
                     d->temperature, d->top_k, d->top_p, d->min_p, d->vocab, d->confidence, d->forbid, tokens, confidence};
-    const void* fn = d->dtype == SANGAM_DTYPE_FP32   ? reinterpret_cast<const void*>(&sample_kernel<float>)
-                     : d->dtype == SANGAM_DTYPE_FP16 ? reinterpret_cast<const void*>(&sample_kernel<_Float16>)
-                                                     : reinterpret_cast<const void*>(&sample_kernel<__bf16>);
+    hipStream_t const on = static_cast<hipStream_t>(stream);
+    Split split = split_of(d->rows, d->vocab, d->dtype);
+    split.workspace = static_cast<uint8_t*>(workspace);
+    auto launch = [&](const void* fn, int64_t groups, void** kargs) {
+        const hipError_t e = hipLaunchKernel(fn, dim3(unsigned(groups)), dim3(kThreads), kargs, 0, on);
+        return e == hipSuccess ? SANGAM_OK : fail(SANGAM_ERR_HIP, std::string("sampling launch: ") + hipGetErrorString(e));
+    };
+    const bool bf16 = d->dtype == SANGAM_DTYPE_BF16, fp32 = d->dtype == SANGAM_DTYPE_FP32;
+    if (split.parts > 1) {
+        void* kargs[] = {&args, &split};
+        const void* part = bf16   ? reinterpret_cast<const void*>(&sample_part_kernel<__bf16>)
+                           : fp32 ? reinterpret_cast<const void*>(&sample_part_kernel<float>)
+                                  : reinterpret_cast<const void*>(&sample_part_kernel<_Float16>);
+        const void* join = bf16   ? reinterpret_cast<const void*>(&sample_join_kernel<__bf16>)
+                           : fp32 ? reinterpret_cast<const void*>(&sample_join_kernel<float>)
+                                  : reinterpret_cast<const void*>(&sample_join_kernel<_Float16>);
+        if (const sangam_status e = launch(part, d->rows * split.parts, kargs)) return e;
+        return launch(join, d->rows, kargs);
+    }
     // a grid's threads are counted in 32 bits
     const int64_t step = (int64_t(1) << 32) / kThreads - 1;
     for (int64_t row = 0; row < d->rows; row += step) {
@@ -1170,16 +1431,27 @@ sangam_status sample(const sangam_sample_desc* d, int32_t* tokens, float* confid
         if (some.params_of) some.params_of += row;
         some.tokens += row;
         if (some.conf) some.conf += row;
-        void* kargs[] = {&some};
-        const hipError_t e = hipLaunchKernel(fn, dim3(unsigned(std::min(step, d->rows - row))), dim3(kThreads), kargs, 0, static_cast<hipStream_t>(stream));
-        if (e != hipSuccess) return fail(SANGAM_ERR_HIP, std::string("sampling launch: ") + hipGetErrorString(e));
+        int64_t rows = std::min(step, d->rows - row);
+        void* kargs[] = {&some, &rows};
+        if (bf16) {
+            if (const sangam_status e = launch(reinterpret_cast<const void*>(&sample_values_kernel), rows, kargs)) return e;
+            if (const sangam_status e = launch(reinterpret_cast<const void*>(&sample_kernel<__bf16, true>), std::min<int64_t>(rows, 256), kargs)) return e;
+        } else if (const sangam_status e = launch(fp32 ? reinterpret_cast<const void*>(&sample_kernel<float, false>)
+                                                       : reinterpret_cast<const void*>(&sample_kernel<_Float16, false>), rows, kargs)) {
+            return e;
+        }
     }
     return SANGAM_OK;
 }
 
 }  // namespace
 
-extern "C" size_t sangam_sample_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
+extern "C" size_t sangam_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t dtype) {
+    const bool known = dtype == SANGAM_DTYPE_BF16 || dtype == SANGAM_DTYPE_FP16 || dtype == SANGAM_DTYPE_FP32;
+    if (!known || rows < 1 || rows > INT32_MAX || vocab < 1 || vocab > kMaxVocab) return 0;
+    const Split s = split_of(rows, vocab, dtype);
+    return s.parts > 1 ? size_t(rows * s.row_bytes) : 0;
+}
 
 extern "C" sangam_status sangam_sample_tokens(const sangam_sample_desc* desc, int32_t* tokens, float* confidence, void* workspace,
                                               size_t workspace_bytes, void* stream) {
