@@ -98,11 +98,9 @@ struct SampleArgs {
 // Values of bf16 by the bits without the sign: those up to kTiny count as 0, those
 // from kHuge on have no value (infinities and what is no number among them).
 constexpr int kTiny = (127 - 24) * 128 - 1, kHuge = (127 + 8) * 128;
-constexpr int kSide = kHuge - kTiny + 1;           // counts of a sign: tiny, the values, huge
-constexpr int kValues = kSide - 2;                 // of a sign
-constexpr int kRanked = 2 * kValues + 1;           // values in rank order, 0 (tiny) at kValues
-constexpr int kOwn = (kRanked + kThreads - 1) / kThreads;  // of a thread
-static_assert(kOwn <= 64, "a wave looks at a thread's values");
+constexpr int kSide = kHuge - kTiny + 1;  // counts of a sign: tiny, the values, huge
+constexpr int kValues = kSide - 2;        // of a sign
+constexpr int kRanked = 2 * kValues;      // values in rank order; the tiny ones lie in the middle, without a place
 
 // What a look at a row or a part of it gives.
 struct Counts {
@@ -130,8 +128,10 @@ struct Shared : Counts {
         };
         uint64_t digits[256];
     };
-    uint16_t tops[kTops];  // the largest logit of a thread's chunk (rounded up to 16 bits); entry chunk * kThreads + thread
+    alignas(16) uint16_t tops[kTops];  // the largest logit of a thread's chunk (rounded up to 16 bits); entry chunk * kThreads + thread
     uint64_t part[2 * kWaves];
+    uint64_t block_mass[kRanked / 64];  // of 64 bins or values
+    int32_t block_tokens[kRanked / 64];
     double sums[2 * kWaves];
     uint64_t found_mass, found_bin;
     int found, found_tokens, found_last, listed, queued;
@@ -204,6 +204,20 @@ __device__ __forceinline__ uint64_t wave_up_to(uint64_t x) {
     x += from_lane<0x142, 0xA>(x);  // row_bcast 15 into rows 1 and 3
     x += from_lane<0x143, 0xC>(x);  // row_bcast 31 into rows 2 and 3
     return x;
+}
+
+__device__ __forceinline__ int wave_up_to(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+__device__ __forceinline__ int lane_of(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
+    return uint64_t(uint32_t(lane_of(int(x >> 32), lane))) << 32 | uint32_t(lane_of(int(x), lane));
 }
 
 // Sum over the threads before this one, and over all.
@@ -367,6 +381,7 @@ struct Row {
         if (threadIdx.x == 0) sh.queued = 0;
         __syncthreads();
         const int entries = (vectors + kChunk - 1) / kChunk * kThreads;
+#pragma unroll 4
         for (int e = threadIdx.x; e < entries; e += kThreads) {
             if (from_upper(sh.tops[e]) < low) continue;
             const int k = atomicAdd(&sh.queued, 1);
@@ -739,18 +754,34 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
     const int tid = threadIdx.x;
     const bool greedy = p.temperature == 0.0f;
     auto slot = [&](int b) -> uint64_t { return sh.bins[(row.base + b) & (kBins - 1)]; };
-    uint64_t tokens = 0, mine = 0;
+    // blocks of 64 bins, of which each lane of every wave holds one, and what lies up to its end
+    static_assert(kBins == 64 * 64, "a block a lane");
+    const int lane = tid & 63, wave = tid / 64;
+    __syncthreads();
 #pragma unroll 2
-    for (int j = 0; j < kEach; ++j) {
-        const uint64_t bin = slot(tid * kEach + j);
-        tokens += tokens_in(bin);
-        mine += sh.mass_of(tid * kEach + j, weight_in(bin));
+    for (int block = wave; block < 64; block += kWaves) {
+        const int b = 64 * block + lane;
+        const uint64_t bin = slot(b), m = sh.mass_of(b, weight_in(bin));
+        const int n = wave_up_to(tokens_in(bin));
+        const uint64_t w = wave_up_to(m);
+        if (lane == 63) {
+            sh.block_tokens[block] = n;
+            sh.block_mass[block] = w;
+        }
     }
-    uint64_t before[2], all[2];
-    sums_before(sh, tokens, mine, before, all);
-    const int tokens_before = int(before[0]);
-    const uint64_t mass_before = before[1], all_tokens = all[0], all_mass = all[1];
+    __syncthreads();
+    const int block_tokens = sh.block_tokens[lane];
+    const uint64_t block_mass = sh.block_mass[lane];
+    const int tokens_end = wave_up_to(block_tokens);
+    const uint64_t mass_end = wave_up_to(block_mass);
+    const int all_tokens = lane_of(tokens_end, 63);
+    const uint64_t all_mass = lane_of(mass_end, 63);
     Bin<T, E> bin{sh, row, -1};
+    const uint64_t top_weight = scalar(kOne - miss_at(bin.place(top, 0)));
+    Prefix kept{kBins, 0, 0, 0, 0, all_mass, all_tokens};
+    const Prefix only_first{0, 1, 1, key_of(top), top_weight, 0, 0};
+    double unit = 0.0, weight = 0.0, second = 0.0;  // 2^44 / M; of the token; of the second token, if it is kept
+    int token = -1;
     // min_p: the lowest logit that is kept, an estimate and then by the definition, and its bin
     uint32_t cut_key = 0;
     int cut_bin = kBins;
@@ -771,11 +802,6 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
         cut_key = uint32_t(scalar(int(key_of(cut))));
         cut_bin = t < double(kBins) ? scalar(int(t)) : kBins + 1;
     }
-    const uint64_t top_weight = scalar(kOne - miss_at(bin.place(top, 0)));
-    Prefix kept{kBins, 0, 0, 0, 0, all_mass, int(all_tokens)};
-    const Prefix only_first{0, 1, 1, key_of(top), top_weight, 0, 0};
-    double unit = 0.0, weight = 0.0, second = 0.0;  // 2^44 / M; of the token; of the second token, if it is kept
-    int token = -1;
     enum Stage { kTopK, kTopP, kMinP, kDraw, kSecond, kStages };
 #pragma unroll 1
     for (int stage = kTopK; stage < kStages; ++stage) {
@@ -784,7 +810,7 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
         uint64_t reach = 0;
         double target = 0.0;
         if (stage == kTopK) {
-            if (p.top_k == 0 || p.top_k >= int(all_tokens)) continue;
+            if (p.top_k == 0 || p.top_k >= all_tokens) continue;
             reach = uint64_t(p.top_k);
         } else if (stage == kTopP) {
             if (!(p.top_p < 1.0f)) continue;
@@ -815,29 +841,19 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
             if (a.confidence != SANGAM_CONFIDENCE_MARGIN || kept.before + kept.tokens < 2) continue;
             reach = 2;
         }
-        __syncthreads();
-        if (tid == 0) sh.found = -1;
-        __syncthreads();
-        int n = tokens_before;
-        uint64_t w = mass_before;
-#pragma unroll 2
-        for (int j = 0; j < kEach; ++j) {
-            const int b = tid * kEach + j, more = tokens_in(slot(b));
-            const uint64_t mass = sh.mass_of(b, weight_in(slot(b)));
-            const uint64_t lo = by == By::kCount ? uint64_t(n) : by == By::kCut ? uint64_t(b) : w;
-            const uint64_t hi = by == By::kCount ? uint64_t(n + more) : by == By::kCut ? uint64_t(b + 1) : w + mass;
-            if (lo < reach && hi >= reach) {
-                sh.found = b;
-                sh.found_tokens = n;
-                sh.found_mass = w;
-            }
-            n += more;
-            w += mass;
-        }
-        __syncthreads();
-        Prefix q{scalar(sh.found), 0, 0, 0, 0, scalar(sh.found_mass), scalar(sh.found_tokens)};
-        if (q.bin < 0 || q.bin > kept.bin) continue;  // (not met within what is kept)
-        n = tokens_in(scalar(slot(q.bin)));
+        const uint64_t block_end = by == By::kCount ? uint64_t(tokens_end) : by == By::kCut ? uint64_t(64 * lane + 64) : mass_end;
+        const uint64_t block_size = by == By::kCount ? uint64_t(block_tokens) : by == By::kCut ? 64 : block_mass;
+        const uint64_t in = __ballot(block_end - block_size < reach && block_end >= reach);
+        if (in == 0) continue;  // (not met)
+        const int at = __builtin_ctzll(in), mine = 64 * at + lane;
+        const uint64_t own = slot(mine), m = sh.mass_of(mine, weight_in(own));
+        const int n_end = lane_of(tokens_end - block_tokens, at) + wave_up_to(tokens_in(own));
+        const uint64_t m_end = lane_of(mass_end - block_mass, at) + wave_up_to(m);
+        const uint64_t end = by == By::kCount ? uint64_t(n_end) : by == By::kCut ? uint64_t(mine) + 1 : m_end;
+        const int k = __builtin_ctzll(__ballot(end >= reach) | (uint64_t(1) << 63));
+        const int n = lane_of(tokens_in(own), k);
+        Prefix q{64 * at + k, 0, 0, 0, 0, lane_of(m_end - m, k), lane_of(n_end, k) - n};
+        if (q.bin > kept.bin) continue;  // (not met within what is kept)
         const double into = by == By::kReach || by == By::kAbove ? scalar(fmax(0.0, sh.inside(q.bin, target - double(q.mass)))) : 0.0;
         int index = -1;
         if (n > 0) index = bin.first(q, n, by, int(reach) - q.before, into, cut_key, q.bin == kept.bin ? kept.tokens : n);
@@ -918,15 +934,9 @@ __device__ __forceinline__ void uncount(Shared<E>& sh, const Row<__bf16, E>& row
 
 // Values in rank order: place q's logit, and how many tokens have it.
 __device__ __forceinline__ float value_at(int q) {
-    if (q == kValues) return 0.0f;
-    return __uint_as_float(q < kValues ? uint32_t(kTiny + kValues - q) << 16 : (uint32_t(kTiny + q - kValues) << 16) | 0x80000000u);
+    return __uint_as_float(q < kValues ? uint32_t(kTiny + kValues - q) << 16 : (uint32_t(kTiny + 1 + q - kValues) << 16) | 0x80000000u);
 }
-template <int E>
-__device__ __forceinline__ int count_at(const Shared<E>& sh, int q) {
-    if (q >= kRanked) return 0;
-    if (q == kValues) return int(sh.counts[0] + sh.counts[kSide]);
-    return int(sh.counts[q < kValues ? kValues - q : kSide + q - kValues]);
-}
+__device__ __forceinline__ int count_at(const Counts& sh, int q) { return int(sh.counts[q < kValues ? kValues - q : kSide + 1 + q - kValues]); }
 
 // A prefix of the ranks: all tokens of the values before q, and the first
 // `tokens` of that value.
@@ -935,64 +945,70 @@ struct ValuePrefix {
     uint64_t mass;  // of the values before, units of 2^-44 of the largest weight
 };
 
-// A row's answer from its counts; false: they do not tell.
+// A row's answer from its counts; false: they do not tell. Every wave looks for
+// the places by itself: it holds what lies before each block of 64 values (two a
+// lane), and looks at the block's values, one a lane.
 template <int E>
 __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& row, const SampleArgs& a, const Params& p, int64_t r) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    // the thread's values' counts, and the largest value
-    int own[kOwn], q0 = kRanked;
+    constexpr int kMine = kRanked / kThreads;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    // the thread's values (of block 8 j + wave the lane's), and the largest value
+    int own[kMine], q0 = kRanked;
 #pragma unroll
-    for (int j = kOwn - 1; j >= 0; --j) {
-        own[j] = count_at(sh, tid * kOwn + j);
-        if (own[j] > 0) q0 = tid * kOwn + j;
+    for (int j = 0; j < kMine; ++j) own[j] = count_at(sh, j * kThreads + tid);
+#pragma unroll
+    for (int j = kMine - 1; j >= 0; --j) {
+        const uint64_t some = __ballot(own[j] > 0);
+        if (some) q0 = j * kThreads + wave * 64 + __builtin_ctzll(some);
     }
-    if (tid == 0) sh.found = kRanked;
+    if (lane == 0) sh.block_tokens[wave] = q0;
     __syncthreads();
-    if (q0 < kRanked) atomicMin(&sh.found, q0);
-    __syncthreads();
-    q0 = scalar(sh.found);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) q0 = min(q0, sh.block_tokens[w]);
+    q0 = scalar(q0);
+    const int tiny = scalar(int(sh.counts[0] + sh.counts[kSide]));
+    if (q0 == kRanked || (tiny > 0 && q0 >= kValues) || sh.counts[kSide - 1] > 0) return false;
     const float top = value_at(q0);
-    if (q0 == kRanked || sh.counts[kSide - 1] > 0) return false;
     // (no weight below -2^8, or none is there)
     if (sh.counts[2 * kSide - 1] > 0 && !((double(top) + 0x1p8) * row.scale >= double(kBins))) return false;
     const double scale = row.scale;
     auto t_of = [&](float x) { return (double(top) - double(x)) * scale; };
-    // weight of a token: bin, and units of 2^-33 of its largest
-    auto token_weight = [&](double t, int* b) -> uint64_t {
-        *b = t < double(kBins) ? int(t) : 0;
-        return t < double(kBins) ? kOne - miss_at(t - double(*b)) : 0;
+    // a token's weight in units of 2^-44 of the largest
+    auto per_token = [&](double t) -> double {
+        const int b = t < double(kBins) ? int(t) : 0;
+        return t < double(kBins) ? sh.bin_weight(b) * (0x1p33 - double(miss_at(t - double(b)))) * 2048.0 : 0.0;
     };
-    auto mass_at = [&](int q, int n) -> uint64_t {
-        if (n == 0) return 0;
-        int b;
-        const uint64_t v = token_weight(t_of(value_at(q)), &b);
-        return sh.mass_of(b, uint64_t(n) * v);
-    };
-    uint64_t tokens = 0, mine = 0;
+    auto mass_of = [&](float x, int n) -> uint64_t { return uint64_t(__builtin_rint(double(n) * per_token(t_of(x)))); };
     double spread = 0.0;  // weights times t
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-        if (__ballot(own[j] > 0) == 0) continue;
-        const int q = tid * kOwn + j;
-        const uint64_t m = mass_at(q, own[j]);
-        tokens += own[j];
-        mine += m;
-        if (m > 0) spread += double(m) * t_of(value_at(q));
+    for (int j = 0; j < kMine; ++j) {
+        uint64_t m = 0;
+        if (__ballot(own[j] > 0) != 0) {
+            const float x = value_at(j * kThreads + tid);
+            m = mass_of(x, own[j]);
+            if (m > 0) spread += double(m) * t_of(x);
+        }
+        const uint64_t mass = wave_up_to(m);
+        const int tokens = wave_up_to(own[j]);
+        if (lane == 63) {
+            sh.block_mass[j * kWaves + wave] = mass;
+            sh.block_tokens[j * kWaves + wave] = tokens;
+        }
         if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
-    uint64_t before[2], all[2];
-    sums_before(sh, tokens, mine, before, all);
-    const int tokens_before = int(before[0]);
-    const uint64_t mass_before = before[1], all_tokens = all[0], all_mass = all[1];
+    __syncthreads();
+    // blocks 2 lane and 2 lane + 1, and what lies before them (the tiny ones before the lower half)
+    const uint64_t tiny_mass = tiny ? scalar(mass_of(0.0f, tiny)) : 0;
+    const int tokens0 = sh.block_tokens[2 * lane], tokens1 = sh.block_tokens[2 * lane + 1];
+    const uint64_t mass0 = sh.block_mass[2 * lane], mass1 = sh.block_mass[2 * lane + 1];
+    const int tokens_end = wave_up_to(tokens0 + tokens1) + (lane >= 32 ? tiny : 0);
+    const uint64_t mass_end = wave_up_to(mass0 + mass1) + (lane >= 32 ? tiny_mass : 0);
+    const int all_tokens = lane_of(tokens_end, 63);
+    const uint64_t all_mass = lane_of(mass_end, 63);
     // (what the tiny ones weigh may be off by 2^-24 of it)
-    if (mass_at(kValues, count_at(sh, kValues)) > all_mass / 512) return false;
-    ValuePrefix kept{kRanked, 0, int(all_tokens), all_mass};
-    auto per_token = [&](int q) -> double {
-        int b;
-        const uint64_t v = token_weight(t_of(value_at(q)), &b);
-        return sh.bin_weight(b) * double(v) * 2048.0;
-    };
-    auto all_of = [&](const ValuePrefix& x) -> uint64_t { return x.mass + (x.tokens ? mass_at(x.q, x.tokens) : 0); };
+    if (tiny_mass > all_mass / 512) return false;
+    ValuePrefix kept{kRanked, 0, all_tokens, all_mass};
     double unit = 0.0, weight = 0.0, second = 0.0;
     int drawn = 0, place = 0, drawn_tokens = 0;
     int cut_q = kRanked;  // min_p: the first value that is not kept
@@ -1006,6 +1022,7 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
             else hi = mid;
         }
         cut_q = scalar(hi);
+        if (cut_q == kValues && tiny > 0) return false;
     }
     enum Stage { kTopK, kTopP, kMinP, kDraw, kSecond, kStages };
 #pragma unroll 1
@@ -1014,17 +1031,26 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
         uint64_t reach = 0;
         double target = 0.0;
         if (stage == kTopK) {
-            if (p.top_k == 0 || p.top_k >= int(all_tokens)) continue;
+            if (p.top_k == 0 || p.top_k >= all_tokens) continue;
             reach = uint64_t(p.top_k);
-        } else if (stage == kTopP) {
-            if (!(p.top_p < 1.0f)) continue;
-            target = scalar(ceil(double(p.top_p) * double(all_of(kept))));
-            if (!(target > 0.0)) {
-                kept = ValuePrefix{q0, 1, 0, 0};
-                continue;
+        } else if (stage == kTopP || stage == kDraw) {
+            if (stage == kTopP && !(p.top_p < 1.0f)) continue;
+            const double M = double(scalar(kept.mass + (kept.tokens ? mass_of(value_at(kept.q), kept.tokens) : 0)));
+            if (stage == kTopP) {
+                target = scalar(ceil(double(p.top_p) * M));
+                if (!(target > 0.0)) {
+                    kept = ValuePrefix{q0, 1, 0, 0};
+                    continue;
+                }
+                by = By::kReach;
+                reach = uint64_t(target);
+            } else {
+                unit = scalar(0x1p44 / M);
+                const float u = p.temperature == 0.0f ? 0.0f : a.u[r];
+                target = scalar(fmin(u > 0.0f ? double(u) * M : 0.0, M - 1.0));
+                by = By::kAbove;
+                reach = uint64_t(target) + 1;
             }
-            by = By::kReach;
-            reach = uint64_t(target);
         } else if (stage == kMinP) {
             if (!(p.min_p > 0.0f)) continue;
             if (p.min_p > 1.0f) {
@@ -1034,47 +1060,34 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
             if (cut_q > kept.q) continue;
             by = By::kCut;
             reach = uint64_t(cut_q);
-        } else if (stage == kDraw) {
-            const uint64_t M = scalar(all_of(kept));
-            unit = scalar(0x1p44 / double(M));
-            const float u = p.temperature == 0.0f ? 0.0f : a.u[r];
-            target = scalar(fmin(u > 0.0f ? double(u) * double(M) : 0.0, double(M - 1)));
-            by = By::kAbove;
-            reach = uint64_t(target) + 1;
         } else {
             if (a.confidence != SANGAM_CONFIDENCE_MARGIN || kept.before + kept.tokens < 2) continue;
             reach = 2;
         }
-        // the thread whose values the place lies in, then the value: its end is the first at or above `reach`
-        __syncthreads();
-        if (tid == 0) sh.found = -1;
-        __syncthreads();
-        const uint64_t lo = by == By::kCount ? uint64_t(tokens_before) : by == By::kCut ? uint64_t(tid) * kOwn : mass_before;
-        const uint64_t more = by == By::kCount ? tokens : by == By::kCut ? uint64_t(kOwn) : mine;
-        if (lo < reach && lo + more >= reach) {
-            sh.found = tid;
-            sh.found_tokens = tokens_before;
-            sh.found_mass = mass_before;
-        }
-        __syncthreads();
-        const int owner = scalar(sh.found);
-        if (owner < 0) continue;
-        const int q = owner * kOwn + lane, n = lane < kOwn ? count_at(sh, q) : 0;
-        const uint64_t m = lane < kOwn ? mass_at(q, n) : 0;
-        const uint64_t n_end = uint64_t(scalar(sh.found_tokens)) + wave_up_to(uint64_t(n)), m_end = scalar(sh.found_mass) + wave_up_to(m);
-        const uint64_t end = by == By::kCount ? n_end : by == By::kCut ? uint64_t(q) + 1 : m_end;
-        const int at = __builtin_ctzll(__ballot(lane < kOwn && end >= reach) | (uint64_t(1) << 63));
-        ValuePrefix x{owner * kOwn + at, 0, int(scalar(int(__shfl(int(n_end), at) - __shfl(n, at)))), 0};
-        x.mass = scalar(uint64_t(__shfl(m_end, at) - __shfl(m, at)));
-        const int here = scalar(__shfl(n, at));
+        // the block in which the axis, counted in tokens, weight or values, first reaches `reach`
+        const uint64_t end1 = by == By::kCount ? uint64_t(tokens_end) : by == By::kCut ? uint64_t(128 * lane + 128) : mass_end;
+        const uint64_t size1 = by == By::kCount ? uint64_t(tokens1) : by == By::kCut ? 64 : mass1;
+        const uint64_t size0 = by == By::kCount ? uint64_t(tokens0) : by == By::kCut ? 64 : mass0;
+        const uint64_t in1 = __ballot(end1 - size1 < reach && end1 >= reach);
+        const uint64_t in0 = __ballot(end1 - size1 - size0 < reach && end1 - size1 >= reach);
+        if ((in0 | in1) == 0) return false;  // among the tiny ones
+        const int at = __builtin_ctzll(in0 | in1), block = 2 * at + (in1 != 0);
+        // then the value
+        const int q = 64 * block + lane, n = count_at(sh, q);
+        const uint64_t m = mass_of(value_at(q), n);
+        const int n_end = lane_of(tokens_end - tokens1 - (in1 ? 0 : tokens0), at) + wave_up_to(n);
+        const uint64_t m_end = lane_of(mass_end - mass1 - (in1 ? 0 : mass0), at) + wave_up_to(m);
+        const uint64_t end = by == By::kCount ? uint64_t(n_end) : by == By::kCut ? uint64_t(q) + 1 : m_end;
+        const int k = __builtin_ctzll(__ballot(end >= reach) | (uint64_t(1) << 63));
+        ValuePrefix x{64 * block + k, 0, lane_of(n_end - n, k), lane_of(m_end - m, k)};
+        const int here = lane_of(n, k);
         if (x.q > kept.q) continue;  // (not met within what is kept)
         const int most = x.q == kept.q ? kept.tokens : here;
-        const double each = scalar(per_token(x.q));
+        const double each = scalar(per_token(t_of(value_at(x.q))));
         x.tokens = here;
         if (by == By::kCount) x.tokens = int(reach) - x.before;
         if (by == By::kReach) x.tokens = scalar(max(1, min(here, int(ceil((target - double(x.mass)) / each)))));
         if (by == By::kAbove) x.tokens = scalar(max(1, min(most, int(floor((target - double(x.mass)) / each)) + 1)));
-        if (x.q == kValues && x.tokens > 0) return false;
         if (stage <= kMinP) {
             if (x.q < kept.q || x.tokens < kept.tokens) kept = x;
         } else if (stage == kDraw) {
@@ -1098,10 +1111,10 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
         });
         __syncthreads();
         if (tid < drawn_tokens) {
-            const uint64_t mine_ = sh.list[tid];
+            const uint64_t mine = sh.list[tid];
             int rank = 1;
-            for (int j = 0; j < drawn_tokens; ++j) rank += sh.list[j] < mine_;
-            if (rank == place) sh.index = int(mine_);
+            for (int j = 0; j < drawn_tokens; ++j) rank += sh.list[j] < mine;
+            if (rank == place) sh.index = int(mine);
         }
         __syncthreads();
         token = sh.index;
@@ -1117,13 +1130,14 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
         if (kept.q < kRanked) {
             spread = 0.0;
 #pragma unroll 1
-            for (int j = 0; j < kOwn && tid * kOwn + j <= kept.q; ++j) {
-                const int q = tid * kOwn + j;
-                const uint64_t m = mass_at(q, q < kept.q ? count_at(sh, q) : kept.tokens);
-                if (m > 0) spread += double(m) * t_of(value_at(q));
+            for (int q = tid; q <= kept.q; q += kThreads) {
+                const float y = value_at(q);
+                const uint64_t m = mass_of(y, q < kept.q ? count_at(sh, q) : kept.tokens);
+                if (m > 0) spread += double(m) * t_of(y);
             }
         }
         sum_all(sh, spread, none);
+        if (kept.q >= kValues && tiny > 0) spread += double(tiny_mass) * t_of(0.0f);
         c = -(spread * 0x1p-44 * unit * (0.69314718055994530942 / 64) - log(unit));
     }
     answer(a, r, token, c);
@@ -1275,8 +1289,7 @@ __global__ __launch_bounds__(kThreads) void sample_join_kernel(SampleArgs a, Spl
     const uint8_t* const at = s.workspace + r * s.row_bytes;
     typedef uint32_t U4 __attribute__((ext_vector_type(4)));
     const U4* const tops = reinterpret_cast<const U4*>(at + s.parts * s.record);
-    static_assert(offsetof(Shared<kPart>, tops) % 16 == 0, "tops are copied 16 bytes at a time");
-#pragma unroll 4
+    #pragma unroll 4
     for (int k = threadIdx.x; k < s.chunks * kThreads / 8; k += kThreads) reinterpret_cast<U4*>(sh.tops)[k] = tops[k];
     if constexpr (__is_same(T, __bf16)) {
         // eight counts at a time, of all the parts
@@ -1348,6 +1361,8 @@ __global__ __launch_bounds__(kThreads) void sample_join_kernel(SampleArgs a, Spl
 
 // Work-groups that the parts make if they can: three a CU.
 constexpr int64_t kGroups = 3 * 256;
+// Parts of a row at most: putting one more together takes longer than its share of the row.
+constexpr int kMostParts = 10;
 
 Split split_of(int64_t rows, int32_t vocab, int32_t dtype) {
     Split s{};
@@ -1358,7 +1373,7 @@ Split split_of(int64_t rows, int32_t vocab, int32_t dtype) {
         return s;
     }
     const int64_t wanted = std::max<int64_t>((kGroups + rows - 1) / rows, (s.chunks + kMostChunks - 1) / kMostChunks);
-    const int parts = int(std::min<int64_t>(wanted, s.chunks));
+    const int parts = int(std::min<int64_t>({wanted, s.chunks, std::max<int64_t>(kMostParts, (s.chunks + kMostChunks - 1) / kMostChunks)}));
     s.chunks_each = (s.chunks + parts - 1) / parts;
     s.parts = (s.chunks + s.chunks_each - 1) / s.chunks_each;
     s.record = dtype == SANGAM_DTYPE_BF16 ? kRecordValues : kRecordBins;
