@@ -130,8 +130,8 @@ struct Shared : Counts {
     };
     alignas(16) uint16_t tops[kTops];  // the largest logit of a thread's chunk (rounded up to 16 bits); entry chunk * kThreads + thread
     uint64_t part[2 * kWaves];
-    uint64_t block_mass[kRanked / 64];  // of 64 bins or values
-    int32_t block_tokens[kRanked / 64];
+    uint64_t block_mass[64];  // of a 64th of the bins or values
+    int32_t block_tokens[64];
     double sums[2 * kWaves];
     uint64_t found_mass, found_bin;
     int found, found_tokens, found_last, listed, queued;
@@ -195,6 +195,8 @@ __device__ __forceinline__ uint64_t from_lane(uint64_t x) {
     const int high = __builtin_amdgcn_update_dpp(0, int(x >> 32), CONTROL, ROWS, 0xF, false);
     return uint64_t(uint32_t(high)) << 32 | uint32_t(low);
 }
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CONTROL, ROWS, 0xF, false); }
 // Sum over the lanes up to this one: within rows of 16, then from row to row.
 __device__ __forceinline__ uint64_t wave_up_to(uint64_t x) {
     x += from_lane<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8
@@ -206,19 +208,34 @@ __device__ __forceinline__ uint64_t wave_up_to(uint64_t x) {
     return x;
 }
 
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ double from_lane(double x) {
+    return __builtin_bit_cast(double, from_lane<CONTROL, ROWS>(__builtin_bit_cast(uint64_t, x)));
+}
+__device__ __forceinline__ double wave_up_to(double x) {
+    x += from_lane<0x111, 0xF>(x);
+    x += from_lane<0x112, 0xF>(x);
+    x += from_lane<0x114, 0xF>(x);
+    x += from_lane<0x118, 0xF>(x);
+    x += from_lane<0x142, 0xA>(x);
+    x += from_lane<0x143, 0xC>(x);
+    return x;
+}
 __device__ __forceinline__ int wave_up_to(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    x += from_lane<0x111, 0xF>(x);
+    x += from_lane<0x112, 0xF>(x);
+    x += from_lane<0x114, 0xF>(x);
+    x += from_lane<0x118, 0xF>(x);
+    x += from_lane<0x142, 0xA>(x);
+    x += from_lane<0x143, 0xC>(x);
     return x;
 }
 __device__ __forceinline__ int lane_of(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 __device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
     return uint64_t(uint32_t(lane_of(int(x >> 32), lane))) << 32 | uint32_t(lane_of(int(x), lane));
 }
+
+__device__ __forceinline__ double lane_of(double x, int lane) { return __builtin_bit_cast(double, lane_of(__builtin_bit_cast(uint64_t, x), lane)); }
 
 // Sum over the threads before this one, and over all.
 template <int E>
@@ -605,7 +622,7 @@ struct Bin {
 
 // Parameters of a row, as the header defines them.
 struct Params {
-    float temperature, top_p, min_p;
+    float temperature, top_p, min_p, u;
     int top_k;
     bool none;  // the row's entry is outside: nothing is taken
 };
@@ -617,6 +634,7 @@ __device__ __forceinline__ Params params_of(const SampleArgs& a, int64_t r) {
     if (p.none) return p;
     p.temperature = a.temperatures ? a.temperatures[of] : a.temperature;
     if (!(p.temperature > 0.0f)) p.temperature = 0.0f;
+    p.u = a.u[r];
     p.top_k = a.top_ks ? a.top_ks[of] : a.top_k;
     if (p.top_k < 1 || p.top_k >= a.vocab) p.top_k = 0;
     p.top_p = a.top_ps ? a.top_ps[of] : a.top_p;
@@ -833,8 +851,7 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
         } else if (stage == kDraw) {
             const uint64_t M = scalar(kept.all(sh));
             unit = scalar(0x1p44 / double(M));
-            const float u = greedy ? 0.0f : a.u[r];
-            target = scalar(fmin(u > 0.0f ? double(u) * double(M) : 0.0, double(M - 1)));
+            target = scalar(fmin(!greedy && p.u > 0.0f ? double(p.u) * double(M) : 0.0, double(M - 1)));
             by = By::kAbove;
             reach = uint64_t(target) + 1;
         } else {
@@ -942,25 +959,31 @@ __device__ __forceinline__ int count_at(const Counts& sh, int q) { return int(sh
 // `tokens` of that value.
 struct ValuePrefix {
     int q, tokens, before;
-    uint64_t mass;  // of the values before, units of 2^-44 of the largest weight
+    double mass;  // of the values before, the largest weight being 1
 };
 
 // A row's answer from its counts; false: they do not tell. Every wave looks for
-// the places by itself: it holds what lies before each block of 64 values (two a
-// lane), and looks at the block's values, one a lane.
+// the places by itself: a lane holds what lies up to the end of a block of 128
+// values, and looks at two values of the block that a place lies in. Weights are
+// added up in 64 bits, in an order that is always the same.
 template <int E>
 __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& row, const SampleArgs& a, const Params& p, int64_t r) {
-    constexpr int kMine = kRanked / kThreads;
+    constexpr int kBlock = kRanked / 64, kSteps = 64 / kWaves;
+    static_assert(kBlock == 128, "two values a lane");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-    // the thread's values (of block 8 j + wave the lane's), and the largest value
-    int own[kMine], q0 = kRanked;
+    // the thread's values: two of each block kWaves i + wave, and the largest value
+    int own[kSteps][2], q0 = kRanked;
 #pragma unroll
-    for (int j = 0; j < kMine; ++j) own[j] = count_at(sh, j * kThreads + tid);
+    for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-    for (int j = kMine - 1; j >= 0; --j) {
-        const uint64_t some = __ballot(own[j] > 0);
-        if (some) q0 = j * kThreads + wave * 64 + __builtin_ctzll(some);
-    }
+        for (int h = 0; h < 2; ++h) own[i][h] = count_at(sh, (i * kWaves + wave) * kBlock + 64 * h + lane);
+#pragma unroll
+    for (int i = kSteps - 1; i >= 0; --i)
+#pragma unroll
+        for (int h = 1; h >= 0; --h) {
+            const uint64_t some = __ballot(own[i][h] > 0);
+            if (some) q0 = (i * kWaves + wave) * kBlock + 64 * h + __builtin_ctzll(some);
+        }
     if (lane == 0) sh.block_tokens[wave] = q0;
     __syncthreads();
 #pragma unroll
@@ -973,43 +996,49 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
     if (sh.counts[2 * kSide - 1] > 0 && !((double(top) + 0x1p8) * row.scale >= double(kBins))) return false;
     const double scale = row.scale;
     auto t_of = [&](float x) { return (double(top) - double(x)) * scale; };
-    // a token's weight in units of 2^-44 of the largest
-    auto per_token = [&](double t) -> double {
-        const int b = t < double(kBins) ? int(t) : 0;
-        return t < double(kBins) ? sh.bin_weight(b) * (0x1p33 - double(miss_at(t - double(b)))) * 2048.0 : 0.0;
+    // a token's weight, to 2^-33 of it as everywhere
+    auto weight_at = [&](double t) -> double {
+        const bool some = t >= 0.0 && t < double(kBins);  // (values above the largest logit are asked for too)
+        const double held = some ? t : 0.0, f = __builtin_amdgcn_fract(held);
+        const double w = sh.bin_weight(int(held)) * ((0x1p33 - double(miss_at(f))) * 0x1p-33);
+        return some ? w : 0.0;
     };
-    auto mass_of = [&](float x, int n) -> uint64_t { return uint64_t(__builtin_rint(double(n) * per_token(t_of(x)))); };
+    auto mass_of = [&](float x, int n) { return double(n) * weight_at(t_of(x)); };
     double spread = 0.0;  // weights times t
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-        uint64_t m = 0;
-        if (__ballot(own[j] > 0) != 0) {
-            const float x = value_at(j * kThreads + tid);
-            m = mass_of(x, own[j]);
-            if (m > 0) spread += double(m) * t_of(x);
+    for (int i = 0; i < kSteps; ++i) {
+        double mass = 0.0;
+        int tokens = 0;
+        if (__ballot((own[i][0] | own[i][1]) > 0) != 0) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const double t = t_of(value_at((i * kWaves + wave) * kBlock + 64 * h + lane));
+                const double m = double(own[i][h]) * weight_at(t);
+                mass += m;
+                spread += m > 0.0 ? m * t : 0.0;
+            }
+            mass = wave_up_to(mass);
+            tokens = wave_up_to(own[i][0] + own[i][1]);
         }
-        const uint64_t mass = wave_up_to(m);
-        const int tokens = wave_up_to(own[j]);
         if (lane == 63) {
-            sh.block_mass[j * kWaves + wave] = mass;
-            sh.block_tokens[j * kWaves + wave] = tokens;
+            sh.block_mass[i * kWaves + wave] = __builtin_bit_cast(uint64_t, mass);
+            sh.block_tokens[i * kWaves + wave] = tokens;
         }
-        if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
-    // blocks 2 lane and 2 lane + 1, and what lies before them (the tiny ones before the lower half)
-    const uint64_t tiny_mass = tiny ? scalar(mass_of(0.0f, tiny)) : 0;
-    const int tokens0 = sh.block_tokens[2 * lane], tokens1 = sh.block_tokens[2 * lane + 1];
-    const uint64_t mass0 = sh.block_mass[2 * lane], mass1 = sh.block_mass[2 * lane + 1];
-    const int tokens_end = wave_up_to(tokens0 + tokens1) + (lane >= 32 ? tiny : 0);
-    const uint64_t mass_end = wave_up_to(mass0 + mass1) + (lane >= 32 ? tiny_mass : 0);
+    // up to the end of the lane's block, and of the one before (the tiny ones lie before the lower half)
+    const double tiny_mass = tiny ? scalar(mass_of(0.0f, tiny)) : 0.0;
+    const int tokens_end = wave_up_to(sh.block_tokens[lane]) + (lane >= 32 ? tiny : 0);
+    const double mass_end = wave_up_to(__builtin_bit_cast(double, sh.block_mass[lane])) + (lane >= 32 ? tiny_mass : 0.0);
+    const int tokens_start = tokens_end - sh.block_tokens[lane];
+    const double mass_start = lane == 0 ? 0.0 : __shfl_up(mass_end, 1) + (lane == 32 ? tiny_mass : 0.0);
     const int all_tokens = lane_of(tokens_end, 63);
-    const uint64_t all_mass = lane_of(mass_end, 63);
+    const double all_mass = lane_of(mass_end, 63);
     // (what the tiny ones weigh may be off by 2^-24 of it)
     if (tiny_mass > all_mass / 512) return false;
     ValuePrefix kept{kRanked, 0, all_tokens, all_mass};
-    double unit = 0.0, weight = 0.0, second = 0.0;
+    double M = 0.0, weight = 0.0, second = 0.0;
     int drawn = 0, place = 0, drawn_tokens = 0;
     int cut_q = kRanked;  // min_p: the first value that is not kept
     if (p.min_p > 0.0f && p.min_p <= 1.0f) {
@@ -1027,78 +1056,87 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
     enum Stage { kTopK, kTopP, kMinP, kDraw, kSecond, kStages };
 #pragma unroll 1
     for (int stage = kTopK; stage < kStages; ++stage) {
+        // the place: the first token up to which there are `reach` tokens or values, at least `reach` of weight, or more
         By by = By::kCount;
-        uint64_t reach = 0;
-        double target = 0.0;
+        double reach = 0.0;
         if (stage == kTopK) {
             if (p.top_k == 0 || p.top_k >= all_tokens) continue;
-            reach = uint64_t(p.top_k);
+            reach = double(p.top_k);
         } else if (stage == kTopP || stage == kDraw) {
             if (stage == kTopP && !(p.top_p < 1.0f)) continue;
-            const double M = double(scalar(kept.mass + (kept.tokens ? mass_of(value_at(kept.q), kept.tokens) : 0)));
+            M = scalar(kept.mass + (kept.tokens ? mass_of(value_at(kept.q), kept.tokens) : 0.0));
             if (stage == kTopP) {
-                target = scalar(ceil(double(p.top_p) * M));
-                if (!(target > 0.0)) {
-                    kept = ValuePrefix{q0, 1, 0, 0};
+                reach = scalar(double(p.top_p) * M);
+                if (!(reach > 0.0)) {
+                    kept = ValuePrefix{q0, 1, 0, 0.0};
                     continue;
                 }
                 by = By::kReach;
-                reach = uint64_t(target);
             } else {
-                unit = scalar(0x1p44 / M);
-                const float u = p.temperature == 0.0f ? 0.0f : a.u[r];
-                target = scalar(fmin(u > 0.0f ? double(u) * M : 0.0, M - 1.0));
+                if (p.temperature == 0.0f) {
+                    drawn = q0;
+                    place = 1;
+                    drawn_tokens = scalar(count_at(sh, q0));
+                    weight = 1.0;
+                    continue;
+                }
+                reach = scalar(p.u > 0.0f ? fmin(double(p.u), 1.0) * M : 0.0);
                 by = By::kAbove;
-                reach = uint64_t(target) + 1;
             }
         } else if (stage == kMinP) {
             if (!(p.min_p > 0.0f)) continue;
             if (p.min_p > 1.0f) {
-                kept = ValuePrefix{q0, 1, 0, 0};
+                kept = ValuePrefix{q0, 1, 0, 0.0};
                 continue;
             }
             if (cut_q > kept.q) continue;
             by = By::kCut;
-            reach = uint64_t(cut_q);
+            reach = double(cut_q);
         } else {
             if (a.confidence != SANGAM_CONFIDENCE_MARGIN || kept.before + kept.tokens < 2) continue;
-            reach = 2;
+            reach = 2.0;
         }
-        // the block in which the axis, counted in tokens, weight or values, first reaches `reach`
-        const uint64_t end1 = by == By::kCount ? uint64_t(tokens_end) : by == By::kCut ? uint64_t(128 * lane + 128) : mass_end;
-        const uint64_t size1 = by == By::kCount ? uint64_t(tokens1) : by == By::kCut ? 64 : mass1;
-        const uint64_t size0 = by == By::kCount ? uint64_t(tokens0) : by == By::kCut ? 64 : mass0;
-        const uint64_t in1 = __ballot(end1 - size1 < reach && end1 >= reach);
-        const uint64_t in0 = __ballot(end1 - size1 - size0 < reach && end1 - size1 >= reach);
-        if ((in0 | in1) == 0) return false;  // among the tiny ones
-        const int at = __builtin_ctzll(in0 | in1), block = 2 * at + (in1 != 0);
+        auto met = [&](double end) { return by == By::kAbove ? end > reach : end >= reach; };
+        // the block: the first that has tokens and ends at the place or behind it (or, as sums are rounded, the last with any)
+        const bool some = by == By::kCut || tokens_end > tokens_start;
+        const double block_end = by == By::kCount ? double(tokens_end) : by == By::kCut ? double(kBlock * lane + kBlock) : mass_end;
+        const uint64_t in = __ballot(some && met(block_end)), any = __ballot(some && (by == By::kCount || by == By::kCut || mass_end > mass_start));
+        const int at = in ? __builtin_ctzll(in) : 63 - __builtin_clzll(any);
+        const double block_start = by == By::kCount ? double(tokens_start) : by == By::kCut ? double(kBlock * lane) : mass_start;
+        if (tiny > 0 && at >= 32 && __ballot(lane == at && met(block_start)) != 0) return false;  // among the tiny ones
         // then the value
-        const int q = 64 * block + lane, n = count_at(sh, q);
-        const uint64_t m = mass_of(value_at(q), n);
-        const int n_end = lane_of(tokens_end - tokens1 - (in1 ? 0 : tokens0), at) + wave_up_to(n);
-        const uint64_t m_end = lane_of(mass_end - mass1 - (in1 ? 0 : mass0), at) + wave_up_to(m);
-        const uint64_t end = by == By::kCount ? uint64_t(n_end) : by == By::kCut ? uint64_t(q) + 1 : m_end;
-        const int k = __builtin_ctzll(__ballot(end >= reach) | (uint64_t(1) << 63));
-        ValuePrefix x{64 * block + k, 0, lane_of(n_end - n, k), lane_of(m_end - m, k)};
-        const int here = lane_of(n, k);
+        const int q = kBlock * at + lane, n0 = count_at(sh, q), n1 = count_at(sh, q + 64);
+        const double m0 = mass_of(value_at(q), n0), m1 = mass_of(value_at(q + 64), n1);
+        const int n_end0 = lane_of(tokens_start, at) + wave_up_to(n0), n_end1 = lane_of(n_end0, 63) + wave_up_to(n1);
+        const double m_end0 = lane_of(mass_start, at) + wave_up_to(m0), m_end1 = lane_of(m_end0, 63) + wave_up_to(m1);
+        const double end0 = by == By::kCount ? double(n_end0) : by == By::kCut ? double(q + 1) : m_end0;
+        const double end1 = by == By::kCount ? double(n_end1) : by == By::kCut ? double(q + 65) : m_end1;
+        const bool none = by == By::kCut;
+        const uint64_t in0 = __ballot((none || n0 > 0) && met(end0)), in1 = __ballot((none || n1 > 0) && met(end1));
+        const uint64_t with0 = __ballot(m0 > 0.0), with1 = __ballot(m1 > 0.0);
+        const int k = in0 ? __builtin_ctzll(in0) : in1 ? 64 + __builtin_ctzll(in1) : with1 ? 127 - __builtin_clzll(with1) : 63 - __builtin_clzll(with0 | 1);
+        const int here = k < 64 ? lane_of(n0, k) : lane_of(n1, k - 64);
+        ValuePrefix x{kBlock * at + k, here, k < 64 ? lane_of(n_end0 - n0, k) : lane_of(n_end1 - n1, k - 64), 0.0};
+        // (what lies before: the end of the one before, the very number that was compared)
+        x.mass = k == 0 ? lane_of(mass_start, at) : k <= 64 ? lane_of(m_end0, k - 1) : lane_of(m_end1, k - 65);
         if (x.q > kept.q) continue;  // (not met within what is kept)
         const int most = x.q == kept.q ? kept.tokens : here;
-        const double each = scalar(per_token(t_of(value_at(x.q))));
-        x.tokens = here;
+        const double each = scalar(weight_at(t_of(value_at(x.q))));
         if (by == By::kCount) x.tokens = int(reach) - x.before;
-        if (by == By::kReach) x.tokens = scalar(max(1, min(here, int(ceil((target - double(x.mass)) / each)))));
-        if (by == By::kAbove) x.tokens = scalar(max(1, min(most, int(floor((target - double(x.mass)) / each)) + 1)));
+        if (by == By::kReach) x.tokens = scalar(max(1, min(here, int(ceil(fmin((reach - x.mass) / each, 0x1p30))))));
+        if (by == By::kAbove) x.tokens = scalar(max(1, min(most, int(floor(fmin((reach - x.mass) / each, 0x1p30))) + 1)));
         if (stage <= kMinP) {
             if (x.q < kept.q || x.tokens < kept.tokens) kept = x;
         } else if (stage == kDraw) {
             drawn = x.q;
             place = x.tokens;
             drawn_tokens = here;
-            weight = scalar(each * 0x1p-44);
+            weight = each;
         } else {
-            second = scalar(each * 0x1p-44);
+            second = each;
         }
     }
+    const double unit = scalar(1.0 / M);
     // the token: the place-th by index among those with its logit
     const float x = value_at(drawn);
     int token;
@@ -1131,14 +1169,13 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
             spread = 0.0;
 #pragma unroll 1
             for (int q = tid; q <= kept.q; q += kThreads) {
-                const float y = value_at(q);
-                const uint64_t m = mass_of(y, q < kept.q ? count_at(sh, q) : kept.tokens);
-                if (m > 0) spread += double(m) * t_of(y);
+                const double t = t_of(value_at(q)), m = double(q < kept.q ? count_at(sh, q) : kept.tokens) * weight_at(t);
+                if (m > 0.0) spread += m * t;
             }
         }
         sum_all(sh, spread, none);
-        if (kept.q >= kValues && tiny > 0) spread += double(tiny_mass) * t_of(0.0f);
-        c = -(spread * 0x1p-44 * unit * (0.69314718055994530942 / 64) - log(unit));
+        if (kept.q >= kValues && tiny > 0) spread += tiny_mass * t_of(0.0f);
+        c = -(spread * unit * (0.69314718055994530942 / 64) - log(unit));
     }
     answer(a, r, token, c);
     return true;
@@ -1289,25 +1326,35 @@ __global__ __launch_bounds__(kThreads) void sample_join_kernel(SampleArgs a, Spl
     const uint8_t* const at = s.workspace + r * s.row_bytes;
     typedef uint32_t U4 __attribute__((ext_vector_type(4)));
     const U4* const tops = reinterpret_cast<const U4*>(at + s.parts * s.record);
-    #pragma unroll 4
-    for (int k = threadIdx.x; k < s.chunks * kThreads / 8; k += kThreads) reinterpret_cast<U4*>(sh.tops)[k] = tops[k];
+        constexpr int kTopPieces = Shared<kPart>::kTops / 8 / kThreads;
+#pragma unroll
+    for (int j = 0; j < kTopPieces; ++j)
+        if (int(threadIdx.x) + j * kThreads < s.chunks * kThreads / 8)
+            reinterpret_cast<U4*>(sh.tops)[int(threadIdx.x) + j * kThreads] = tops[int(threadIdx.x) + j * kThreads];
     if constexpr (__is_same(T, __bf16)) {
         // eight counts at a time, of all the parts
         constexpr int kPieces = kRecordValues / 16, kMine = (kPieces + kThreads - 1) / kThreads;
+        constexpr int kAtOnce = 5;
         uint32_t sums[kMine][8] = {};
-#pragma unroll 4
-        for (int part = 0; part < s.parts; ++part) {
-            const U4* const piece = reinterpret_cast<const U4*>(at + part * s.record);
-            U4 w[kMine];
+#pragma unroll 1
+        for (int part0 = 0; part0 < s.parts; part0 += kAtOnce) {
+            U4 w[kAtOnce][kMine];
 #pragma unroll
-            for (int j = 0; j < kMine; ++j) w[j] = piece[min(int(threadIdx.x) + j * kThreads, kPieces - 1)];
+            for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
-            for (int j = 0; j < kMine; ++j)
+                for (int j = 0; j < kMine; ++j)
+                    if (part0 + i < s.parts && int(threadIdx.x) + j * kThreads < kPieces)
+                        w[i][j] = reinterpret_cast<const U4*>(at + (part0 + i) * s.record)[int(threadIdx.x) + j * kThreads];
+                    else w[i][j] = U4{0, 0, 0, 0};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sums[j][2 * e] += w[j][e] & 0xFFFFu;
-                    sums[j][2 * e + 1] += w[j][e] >> 16;
-                }
+            for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        sums[j][2 * e] += w[i][j][e] & 0xFFFFu;
+                        sums[j][2 * e + 1] += w[i][j][e] >> 16;
+                    }
         }
 #pragma unroll
         for (int j = 0; j < kMine; ++j)
@@ -1359,6 +1406,8 @@ __global__ __launch_bounds__(kThreads) void sample_join_kernel(SampleArgs a, Spl
     from_logits(sh, row, a, p, r);
 }
 
+// Rows from which a work-group takes a whole one.
+constexpr int64_t kWholeRows = 256;
 // Work-groups that the parts make if they can: three a CU.
 constexpr int64_t kGroups = 3 * 256;
 // Parts of a row at most: putting one more together takes longer than its share of the row.
@@ -1368,7 +1417,7 @@ Split split_of(int64_t rows, int32_t vocab, int32_t dtype) {
     Split s{};
     constexpr int chunk = kThreads * kPart;
     s.chunks = (vocab + chunk - 1) / chunk;
-    if (rows < 1 || rows >= kGroups) {
+    if (rows < 1 || rows >= kWholeRows) {
         s.parts = 1;
         return s;
     }
