@@ -391,9 +391,9 @@ struct Row {
     // threads hold any, these are listed, and the vectors in them dealt over all
     // threads, so that they come in one or two rounds of loads (a thread that walked
     // its own chunks took one after the other: 18 us for a bin of a row of 152,064).
-    template <typename F>
-    __device__ __forceinline__ void each_within(Shared<E>& sh, float low, float high, F f) const {
-        constexpr int kRound = 2;
+    // f(vectors on their way together, which of the row each is, or `vectors`)
+    template <int AT_ONCE, typename F>
+    __device__ __forceinline__ void each_reaching(Shared<E>& sh, float low, F f) const {
         __syncthreads();
         if (threadIdx.x == 0) sh.queued = 0;
         __syncthreads();
@@ -410,11 +410,11 @@ struct Row {
         const int items = all ? vectors : queued * kLoads;
         const Vec* const v = body();
 #pragma unroll 1
-        for (int k0 = threadIdx.x; k0 < items; k0 += kRound * kThreads) {
-            Vec w[kRound];
-            int k[kRound];
+        for (int k0 = threadIdx.x; k0 < items; k0 += AT_ONCE * kThreads) {
+            Vec w[AT_ONCE];
+            int k[AT_ONCE];
 #pragma unroll
-            for (int j = 0; j < kRound; ++j) {
+            for (int j = 0; j < AT_ONCE; ++j) {
                 const int item = k0 + j * kThreads;
                 k[j] = vectors;
                 if (item < items) {
@@ -423,8 +423,14 @@ struct Row {
                 }
                 if (k[j] < vectors) w[j] = v[k[j]];
             }
+            f(w, k);
+        }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each_within(Shared<E>& sh, float low, float high, F f) const {
+        each_reaching<2>(sh, low, [&](const Vec(&w)[2], const int(&k)[2]) {
 #pragma unroll
-            for (int j = 0; j < kRound; ++j) {
+            for (int j = 0; j < 2; ++j) {
                 if (k[j] >= vectors) continue;
                 float x[V];
                 unpack(w[j], head + k[j] * V, x);
@@ -434,7 +440,7 @@ struct Row {
                     __builtin_amdgcn_sched_barrier(0);  // (side by side they take twice the registers)
                 }
             }
-        }
+        });
         each_edge([&](int i, float x) {
             if (x >= low && x <= high) f(i, x);
         });
@@ -940,6 +946,33 @@ __device__ __forceinline__ void count(Counts& sh, const Row<__bf16, E>& row, uin
     }
 }
 
+// f(index) of all logits equal to x (not 0): two at a time, by what the bits differ in.
+template <int E, typename F>
+__device__ __forceinline__ void each_equal(Shared<E>& sh, const Row<__bf16, E>& row, float x, F f) {
+    typedef uint16_t Halves __attribute__((ext_vector_type(8)));
+    typedef uint16_t Two __attribute__((ext_vector_type(2)));
+    const uint16_t bits = uint16_t(__float_as_uint(x) >> 16);
+    auto found = [&](int i) {
+        if (i != row.forbid) f(i);
+    };
+    constexpr int kAtOnce = 8;
+    row.template each_reaching<kAtOnce>(sh, x, [&](const auto& w, const int(&k)[kAtOnce]) {
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (k[j] >= row.vectors) continue;
+            const Halves off = __builtin_bit_cast(Halves, w[j]) ^ bits;
+            const Two least = __builtin_elementwise_min(__builtin_elementwise_min(off.s01, off.s23), __builtin_elementwise_min(off.s45, off.s67));
+            if (least.x != 0 && least.y != 0) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (off[e] == 0) found(row.head + k[j] * 8 + e);
+        }
+    });
+    row.each_edge([&](int i, float y) {
+        if (y == x) found(i);
+    });
+}
+
 // Takes the forbidden token out of the counts again.
 template <int E>
 __device__ __forceinline__ void uncount(Shared<E>& sh, const Row<__bf16, E>& row) {
@@ -1043,14 +1076,10 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
     int cut_q = kRanked;  // min_p: the first value that is not kept
     if (p.min_p > 0.0f && p.min_p <= 1.0f) {
         const double T_ = p.temperature == 0.0f ? 1.0 : double(p.temperature), low = log(double(p.min_p));
-        int lo = q0, hi = kRanked;  // (kept at lo)
-#pragma unroll 1
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if ((double(value_at(mid)) - double(top)) / T_ >= low) lo = mid;
-            else hi = mid;
-        }
-        cut_q = scalar(hi);
+        // (those that are kept come first: blocks by their last value, then values)
+        auto keeps = [&](int q) { return __builtin_popcountll(__ballot((double(value_at(q)) - double(top)) / T_ >= low)); };
+        const int blocks = keeps(kBlock * lane + kBlock - 1);
+        if (blocks < 64) cut_q = kBlock * blocks + keeps(kBlock * blocks + lane) + keeps(kBlock * blocks + 64 + lane);
         if (cut_q == kValues && tiny > 0) return false;
     }
     enum Stage { kTopK, kTopP, kMinP, kDraw, kSecond, kStages };
@@ -1143,7 +1172,7 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
     if (drawn_tokens <= kList) {
         __syncthreads();
         if (tid == 0) sh.listed = 0;
-        row.each_within(sh, x, x, [&](int i, float) {
+        each_equal(sh, row, x, [&](int i) {
             const int k = atomicAdd(&sh.listed, 1);
             if (k < kList) sh.list[k] = uint32_t(i);
         });
