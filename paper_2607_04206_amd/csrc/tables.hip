@@ -12,6 +12,7 @@
 
 #include "../../include/sangam_tables.h"
 #include "entry.h"
+#include "wave_sum.h"
 
 namespace sangam {
 void set_error(const std::string& msg);
@@ -29,22 +30,11 @@ constexpr int kItemsInLds = 1024;
 
 __device__ __forceinline__ int pages_of(int len) { return len <= 0 ? 0 : (len - 1) / kPage + 1; }
 
-// Inclusive sum over the lanes up to this one.
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    return x;
-}
-
 // Sum over the threads before this one; *total over all. `part`: an entry per wave.
 template <int THREADS>
 __device__ int64_t sum_before(int64_t x, int64_t* part, int64_t* total) {
     const int wave = threadIdx.x / 64;
-    const int64_t up_to = wave_sum(x);
+    const int64_t up_to = int64_t(wave_up_to(uint64_t(x)));
     __syncthreads();
     if ((threadIdx.x & 63) == 63) part[wave] = up_to;
     __syncthreads();
@@ -70,30 +60,49 @@ struct ResizeArgs {
     int32_t requests, max_pages, free_cap;
 };
 
-// One work-group: what a request takes depends on all before it. A wave moves a
-// request's pages, 64 at a time.
+// One work-group: what a request takes depends on all before it. The pages that
+// move are dealt over the threads one by one, each finds its request by its number:
+// 12,800 pages of 100 requests among 1024 in 9 us, by a wave a request 27.
 __global__ __launch_bounds__(kResizeThreads) void tables_resize_kernel(ResizeArgs a) {
     __shared__ int64_t part[kResizeThreads / 64];
-    __shared__ int64_t at[kResizeThreads];  // of a request's first page that moves, in the order of the moves
-    __shared__ int32_t first[kResizeThreads], moved[kResizeThreads];
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
+    __shared__ int64_t at[kResizeThreads];  // moves before a request's
+    __shared__ int32_t first[kResizeThreads];
+    const int tid = threadIdx.x;
     const int64_t had = min(max(a.num_free[0], 0), a.free_cap);
-    auto size = [&](int r, int& held, int& need) {
+    int held, need;
+    auto look = [&](int r) {
         held = r < a.requests ? min(max(a.held[r], 0), a.max_pages) : 0;
         need = r < a.requests ? pages_of(a.lengths[r]) : 0;
     };
-    auto each_request = [&](int r0, auto move) {
-        for (int i = wave; i < kResizeThreads && r0 + i < a.requests; i += kResizeThreads / 64) {
-            const int n = moved[i];
-            int32_t* row = a.pages + int64_t(r0 + i) * a.row_stride + first[i];
-            for (int j = lane; j < n; j += 64) move(row[j], at[i] + j);
+    const bool one = a.requests <= kResizeThreads;  // (then a look is enough)
+    look(tid);
+    // the `moves` of requests [r0, r0 + kResizeThreads), numbered from `before`: take(entry of the table, number) gives a
+    // page, which put(entry, number, page) moves; some are on their way together
+    auto each_move = [&](int r0, int64_t before, int64_t moves, auto take, auto put) {
+        constexpr int kTogether = 4;
+        for (int64_t k0 = tid; k0 < moves; k0 += kTogether * kResizeThreads) {
+            int32_t *entry[kTogether], page[kTogether];
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) {
+                const int64_t k = k0 + j * kResizeThreads;
+                entry[j] = nullptr;
+                if (k >= moves) continue;
+                int i = 0;  // the last request whose moves begin at or before this one
+#pragma unroll
+                for (int step = kResizeThreads / 2; step > 0; step /= 2)
+                    if (at[i + step] <= before + k) i += step;
+                entry[j] = a.pages + int64_t(r0 + i) * a.row_stride + first[i] + (before + k - at[i]);
+                page[j] = take(entry[j], before + k);
+            }
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j)
+                if (entry[j]) put(entry[j], before + k0 + j * kResizeThreads, page[j]);
         }
     };
     // the pages that come back: how many, then where they go
     int64_t given = 0, total;
     for (int r0 = 0; r0 < a.requests; r0 += kResizeThreads) {
-        int held, need;
-        size(r0 + tid, held, need);
+        if (!one) look(r0 + tid);
         sum_before<kResizeThreads>(max(held - need, 0), part, &total);
         given += total;
     }
@@ -101,20 +110,18 @@ __global__ __launch_bounds__(kResizeThreads) void tables_resize_kernel(ResizeArg
     if (given > 0) {
         int64_t before = 0;
         for (int r0 = 0; r0 < a.requests; r0 += kResizeThreads) {
-            int held, need;
-            size(r0 + tid, held, need);
+            if (!one) look(r0 + tid);
             const int gives = max(held - need, 0);
             at[tid] = before + sum_before<kResizeThreads>(gives, part, &total);
             first[tid] = need;
-            moved[tid] = gives;
-            before += total;
             __syncthreads();
-            each_request(r0, [&](int32_t& entry, int64_t k) {
+            each_move(r0, before, total, [](const int32_t* entry, int64_t) { return *entry; }, [&](int32_t* entry, int64_t k, int32_t page) {
                 const int64_t place = many - 1 - k;
-                if (place < a.free_cap) a.free_pages[place] = entry;
-                entry = -1;
+                if (place < a.free_cap) a.free_pages[place] = page;
+                *entry = -1;
             });
-            if (gives > 0) a.held[r0 + tid] = need;
+            before += total;
+            if (gives > 0) a.held[r0 + tid] = held = need;
             __syncthreads();
         }
     }
@@ -122,22 +129,24 @@ __global__ __launch_bounds__(kResizeThreads) void tables_resize_kernel(ResizeArg
     const int64_t top = min(many, int64_t(a.free_cap));
     int64_t before = 0, taken = 0, short_of = 0;
     for (int r0 = 0; r0 < a.requests; r0 += kResizeThreads) {
-        int held, need;
-        size(r0 + tid, held, need);
+        if (!one) look(r0 + tid);
         const int wants = need <= a.max_pages ? max(need - held, 0) : 0;
         const int64_t mine = before + sum_before<kResizeThreads>(wants, part, &total);
         const bool fits = mine + wants <= top;
-        at[tid] = mine;
-        first[tid] = held;
-        moved[tid] = fits ? wants : 0;
         before += total;
+        // (those that fit come first, so their moves are numbered on without a gap)
+        constexpr int64_t kShort = int64_t(1) << 48;
+        int64_t sums;
+        const bool none = (!fits && wants > 0) || need > a.max_pages;
+        sum_before<kResizeThreads>((fits ? wants : 0) + (none ? kShort : 0), part, &sums);
+        at[tid] = fits ? mine : taken + sums % kShort;
+        first[tid] = held;
         __syncthreads();
-        each_request(r0, [&](int32_t& entry, int64_t k) { entry = a.free_pages[top - 1 - k]; });
+        each_move(r0, taken, sums % kShort, [&](const int32_t*, int64_t k) { return a.free_pages[top - 1 - k]; },
+                  [](int32_t* entry, int64_t, int32_t page) { *entry = page; });
         if (fits && wants > 0) a.held[r0 + tid] = need;
-        sum_before<kResizeThreads>(fits ? wants : 0, part, &total);
-        taken += total;
-        sum_before<kResizeThreads>((!fits && wants > 0) || need > a.max_pages, part, &total);
-        short_of += total;
+        taken += sums % kShort;
+        short_of += sums / kShort;
     }
     if (tid == 0) {
         a.num_free[0] = int32_t(top - taken);

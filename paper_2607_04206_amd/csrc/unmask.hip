@@ -241,6 +241,7 @@ __global__ __launch_bounds__(kThreads) void unmask_kernel(UnmaskArgs a) {
         if (n > 64 * kKeys) large = true;
         else if (w != wave) continue;
         else if (n <= 64) by_wave<1>(a, b, r0, int(n), count_of(b), threshold_of(b));
+        else if (n <= 256) by_wave<4>(a, b, r0, int(n), count_of(b), threshold_of(b));
         else by_wave<kKeys>(a, b, r0, int(n), count_of(b), threshold_of(b));
     }
     if (large)

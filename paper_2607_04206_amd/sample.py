@@ -22,9 +22,7 @@ MAX_VOCAB = 1 << 18
 def _each(x, name: str, dtype, dev, entries: Optional[int], lowest, highest):
     """A parameter as (address or None, value, entries): a tensor [entries] on dev, or a number."""
     if isinstance(x, torch.Tensor):
-        if x.dim() != 1 or (entries is not None and x.shape[0] != entries):
-            raise ValueError(f"{name} must be a contiguous tensor [{'n' if entries is None else entries}], as the other parameters")
-        return _ints(x, name, dev, tuple(x.shape), dtype), 0, x.shape[0]
+        return _ints(x, name, dev, entries, dtype), 0, x.numel()
     if not lowest <= x <= highest:
         raise ValueError(f"{name} must be {lowest} to {highest}, got {x}")
     return None, x, entries
@@ -57,7 +55,7 @@ def tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: Union[float, t
         raise ValueError("the logits of a row must be consecutive")
     if not -1 <= forbid < vocab:
         raise ValueError(f"forbid must be -1 or a token, got {forbid}")
-    of = None if params_of is None else _ints(params_of, "params_of", dev, (rows,))
+    of = None if params_of is None else _ints(params_of, "params_of", dev, rows)
     entries = rows if params_of is None else None
     t, t_all, entries = _each(temperature, "temperature", torch.float32, dev, entries, 0.0, math.inf)
     k, k_all, entries = _each(top_k, "top_k", torch.int32, dev, entries, 0, 2 ** 31 - 1)
@@ -73,10 +71,10 @@ def tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: Union[float, t
         workspace = _new((need,), torch.uint8, dev, stream)
     elif workspace is not None and (not workspace.is_contiguous() or workspace.device != dev):
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
-    d = SampleDesc(logits.data_ptr(), rows, logits.stride(0) if rows > 1 else 0, vocab, dtype, _ints(u, "u", dev, (rows,), torch.float32), of,
+    d = SampleDesc(logits.data_ptr(), rows, logits.stride(0) if rows > 1 else 0, vocab, dtype, _ints(u, "u", dev, rows, torch.float32), of,
                    2 ** 31 if entries is None else entries, t, k, p, m, t_all, k_all, p_all, m_all, CONFIDENCES[confidence], forbid)
-    _launch(dev, lib.sangam_sample_tokens, ctypes.byref(d), _ints(out, "out", dev, (rows,)),
-            _ints(confidence_out, "confidence_out", dev, (rows,), torch.float32), workspace.data_ptr() if workspace is not None else None,
+    _launch(dev, lib.sangam_sample_tokens, ctypes.byref(d), _ints(out, "out", dev, rows),
+            _ints(confidence_out, "confidence_out", dev, rows, torch.float32), workspace.data_ptr() if workspace is not None else None,
             workspace.numel() * workspace.element_size() if workspace is not None else 0, s)
     return out, confidence_out
 
@@ -108,9 +106,9 @@ def unmask(tokens: torch.Tensor, confidence: torch.Tensor, ids: torch.Tensor, ro
         out = _new((rows,), torch.int32, dev, stream)
     if left is None:
         left = _new((blocks,), torch.int32, dev, stream)
-    d = UnmaskDesc(tokens.data_ptr() if tokens.is_contiguous() else _ints(tokens, "tokens", dev, (rows,)),
-                   _ints(confidence, "confidence", dev, (rows,), torch.float32), _ints(ids, "ids", dev, (rows,) if slots is None else None),
-                   None if slots is None else _ints(slots, "slots", dev, (rows,), torch.int64), indptr, n, c, rows, ids.shape[0], blocks,
+    d = UnmaskDesc(_ints(tokens, "tokens", dev, rows),
+                   _ints(confidence, "confidence", dev, rows, torch.float32), _ints(ids, "ids", dev, rows if slots is None else None),
+                   None if slots is None else _ints(slots, "slots", dev, rows, torch.int64), indptr, n, c, rows, ids.shape[0], blocks,
                    mask_id, n_all, c_all)
-    _launch(dev, lib.sangam_sample_unmask, ctypes.byref(d), _ints(out, "out", dev, (rows,)), _ints(left, "left", dev, (blocks,)), s)
+    _launch(dev, lib.sangam_sample_unmask, ctypes.byref(d), _ints(out, "out", dev, rows), _ints(left, "left", dev, blocks), s)
     return out, left

@@ -27,14 +27,14 @@ class Tables:
     items: torch.Tensor
 
 
-def _ints(t, name: str, dev, shape=None, dtype=torch.int32) -> int:
-    """Address of a contiguous tensor [n] (or of that shape) of whole numbers on dev."""
+def _ints(t, name: str, dev, entries: Optional[int] = None, dtype=torch.int32) -> int:
+    """Address of a contiguous tensor [entries] (None: of any) of that dtype on dev."""
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
         raise TypeError(f"{name} must be a torch.Tensor of {dtype}")
-    if t.device != dev:
+    if t.get_device() != dev.index:
         raise ValueError(f"{name} must be on {dev}, got {t.device}")
-    if not t.is_contiguous() or (t.dim() != 1 if shape is None else t.shape != shape):
-        raise ValueError(f"{name} must be a contiguous tensor [n]" if shape is None else f"{name} must be a contiguous tensor {list(shape)}")
+    if t.dim() != 1 or not t.is_contiguous() or (entries is not None and t.numel() != entries):
+        raise ValueError(f"{name} must be a contiguous tensor [{'n' if entries is None else entries}], got {list(t.shape)}")
     return t.data_ptr()
 
 
@@ -57,13 +57,13 @@ def resize(table: torch.Tensor, held: torch.Tensor, lengths: torch.Tensor, free:
     c_table = _table(table)
     dev = table.device
     s = _stream(dev, stream)
-    h = _ints(held, "held", dev, (c_table.requests,))
-    n = _ints(lengths, "lengths", dev, (c_table.requests,))
+    h = _ints(held, "held", dev, c_table.requests)
+    n = _ints(lengths, "lengths", dev, c_table.requests)
     f = _ints(free, "free", dev)
-    m = _ints(num_free, "num_free", dev, (1,))
+    m = _ints(num_free, "num_free", dev, 1)
     if short is None:
         short = _new((1,), torch.int32, dev, stream)
-    _launch(dev, lib.sangam_tables_resize, ctypes.byref(c_table), h, n, f, free.numel(), m, _ints(short, "short", dev, (1,)), s)
+    _launch(dev, lib.sangam_tables_resize, ctypes.byref(c_table), h, n, f, free.numel(), m, _ints(short, "short", dev, 1), s)
     return short
 
 
@@ -84,14 +84,16 @@ def build(table: torch.Tensor, request: Optional[torch.Tensor], kv_len: torch.Te
         raise ValueError("rows and pages must not be negative")
     k = _ints(kv_len, "kv_len", dev)
     items = kv_len.numel()
-    batch = TablesBatch(items, 0, None if request is None else _ints(request, "request", dev, (items,)), k,
-                        _ints(q_indptr, "q_indptr", dev, (items + 1,)), _ints(q_offset, "q_offset", dev, (items,)),
-                        None if q_pos is None else _ints(q_pos, "q_pos", dev, (rows,)))
+    batch = TablesBatch(items, 0, None if request is None else _ints(request, "request", dev, items), k,
+                        _ints(q_indptr, "q_indptr", dev, items + 1), _ints(q_offset, "q_offset", dev, items),
+                        None if q_pos is None else _ints(q_pos, "q_pos", dev, rows))
     if out is None:
-        out = Tables(_new((items + 1,), torch.int32, dev, stream), _new((pages,), torch.int32, dev, stream),
-                     _new((rows,), torch.int32, dev, stream), _new((rows,), torch.int64, dev, stream), _new((rows,), torch.int32, dev, stream))
+        # (one allocation: each costs about as much as the launch's own work here)
+        sizes = [2 * rows, rows, rows, items + 1, pages]
+        slots, positions, row_items, page_indptr, page_ids = _new((4 * rows + items + 1 + pages,), torch.int32, dev, stream).split(sizes)
+        out = Tables(page_indptr, page_ids, positions, slots.view(torch.int64), row_items)
     _launch(dev, lib.sangam_tables_build, ctypes.byref(c_table), ctypes.byref(batch),
-            _ints(out.page_indptr, "out.page_indptr", dev, (items + 1,)), _ints(out.page_ids, "out.page_ids", dev, (pages,)), pages,
-            _ints(out.positions, "out.positions", dev, (rows,)), _ints(out.slots, "out.slots", dev, (rows,), torch.int64),
-            _ints(out.items, "out.items", dev, (rows,)), rows, s)
+            _ints(out.page_indptr, "out.page_indptr", dev, items + 1), _ints(out.page_ids, "out.page_ids", dev, pages), pages,
+            _ints(out.positions, "out.positions", dev, rows), _ints(out.slots, "out.slots", dev, rows, torch.int64),
+            _ints(out.items, "out.items", dev, rows), rows, s)
     return out
