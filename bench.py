@@ -285,7 +285,8 @@ def serve_trace(args):
     dev = torch.device("cuda:0")
     reqs = workloads.serving_trace(args.seed, args.trace_iters, args.trace_rate)
     loop = ServingLoop(reqs, hq=28, hkv=4, d=128, tau=args.tau, device=dev, seed=args.seed,
-                       kv_format=args.kv_format, rotary={} if args.rotary else None)
+                       kv_format=args.kv_format, rotary={} if args.rotary else None,
+                       sampling={"vocab": args.sampling_vocab} if args.sampling_vocab else None)
     log = loop.run(args.trace_iters * 8)
     torch.cuda.synchronize()
     ms = np.asarray([r.events[0].elapsed_time(r.events[1]) for r in log])
@@ -319,6 +320,8 @@ def serve_trace(args):
         res["kv_format"] = args.kv_format
     if args.rotary:
         res["rotary"] = True
+    if args.sampling_vocab:
+        res["sampling_vocab"] = args.sampling_vocab
     print(json.dumps(res), flush=True)
 
 
@@ -451,6 +454,8 @@ def main():
                     help="quantised KV cache instead of bf16 (--serve-trace)")
     ap.add_argument("--rotary", action="store_true",
                     help="rotate q and k at their positions before each call (--serve-trace)")
+    ap.add_argument("--sampling-vocab", type=int, default=0,
+                    help="sample a token of so many for each decode row and unmask the confident ones (--serve-trace)")
     ap.add_argument("--trace-iters", type=int, default=600, help="iterations (--serve-trace)")
     ap.add_argument("--trace-rate", type=float, default=0.3, help="requests per iteration (--serve-trace)")
     ap.add_argument("--kv-transfer", action="store_true",

@@ -5,11 +5,16 @@ refreshes the cache at the block boundary; Sec. 2.2, Sec. 4.3), each
 iteration's microbatch is composed by the deficit token-budget rule
 (Sec. 4.1, Alg. 1) and served by one sangam_attn_forward call over a paged KV
 pool (Sec. 5), or by one sangam_kvq_forward call over a quantised pool. With
-rotary positions, q and k are rotated at their rows' positions before it.
+rotary positions, q and k are rotated at their rows' positions before it. The
+block table lies on the device and follows the requests' lengths (tables.resize),
+and each batch's page list, positions and slots are built there (tables.build).
+With sampling, each decode row takes a token from logits (sample.tokens), and the
+most confident rows of each block keep theirs (sample.unmask), which decides how
+many steps a block takes.
 
 Only one attention layer is run per iteration (the model around it is out of
-scope), with synthetic Q / K / V values: the loop exercises batch composition,
-planning and the kernels on real mixed batches."""
+scope), with synthetic Q / K / V values and logits: the loop exercises batch
+composition, planning and the kernels on real mixed batches."""
 from __future__ import annotations
 
 import dataclasses
@@ -19,7 +24,7 @@ from typing import List, Optional
 import numpy as np
 import torch
 
-from . import attn, kv, kvq, rope, sched
+from . import attn, kv, kvq, rope, sample, sched, tables
 
 BLOCK = 32
 PAGE = 16
@@ -53,6 +58,7 @@ class _State:
     steps_left: int = 0
     phase: str = "waiting"      # waiting (for a prefill), decoding, done
     queued_at: int = 0
+    fresh: bool = False         # its response has no ids yet
 
     @property
     def L(self) -> int:
@@ -75,6 +81,7 @@ class Iteration:
     queue_waits: List[int] = dataclasses.field(default_factory=list)
     captured: Optional[dict] = None
     batch: Optional[list] = None  # (request id, kind) of each item, in batch order
+    left: Optional[List[int]] = None  # with sampling: rows of each decode's block that are still masked
 
 
 class ServingLoop:
@@ -82,11 +89,15 @@ class ServingLoop:
 
     kv_format: None for a bf16 cache, or a format of kvq.FORMATS.
     rotary: None, or the arguments of rope.plan (rot_dim is the head dim unless
-    they say otherwise)."""
+    they say otherwise).
+    sampling: None (blocks take the trace's steps), or vocab, and any of
+    temperature, top_k, top_p, min_p and confidence of sample.tokens and of count
+    and threshold (0.9, the paper's) of sample.unmask: a block is done when no row
+    of it is masked. Token vocab is the mask."""
 
     def __init__(self, requests, *, hq: int, hkv: int, d: int, tau: int, device,
                  num_pool_pages: Optional[int] = None, max_rows: int = 1 << 15, seed: int = 0,
-                 kv_format: Optional[str] = None, rotary: Optional[dict] = None):
+                 kv_format: Optional[str] = None, rotary: Optional[dict] = None, sampling: Optional[dict] = None):
         if kv_format is not None and kv_format not in kvq.FORMATS:
             raise ValueError(f"kv_format must be None or one of {sorted(kvq.FORMATS)}, got {kv_format!r}")
         self.reqs = [_State(r) for r in sorted(requests, key=lambda r: (r.arrival, r.rid))]
@@ -111,10 +122,38 @@ class ServingLoop:
                 self.q_rot, self.k_rot = torch.empty_like(self.q), torch.empty_like(self.k_new)
             self.out = torch.empty((max_rows, hq, d), dtype=torch.bfloat16, device=device)
             self.lse = torch.empty((max_rows, hq), dtype=torch.float32, device=device)
+            # the block table follows the requests' lengths (0 before the first prefill and after the end)
+            self._rows = {id(s): i for i, s in enumerate(self.reqs)}
+            self.table = torch.full((len(self.reqs), max([-(-s.L // PAGE) for s in self.reqs], default=0)), -1, dtype=torch.int32, device=device)
+            self.held = torch.zeros(len(self.reqs), dtype=torch.int32, device=device)
+            self.free_pages = torch.tensor(self.pool._free, dtype=torch.int32, device=device)
+            self.num_free = torch.tensor([self.pool.free], dtype=torch.int32, device=device)
+            self._lengths = np.zeros(len(self.reqs), np.int32)
+            self._resized = True
+        self.sampling = None
+        if sampling is not None:
+            self._set_sampling(device, seed, **sampling)
         self.deficit = 0
         self.next_arrival = 0
         self.waiting: List[_State] = []  # arrival order of the requests (re-prefills keep their place)
         self.sm_scale = float(np.float32(1.0 / np.sqrt(d)))
+
+    def _set_sampling(self, device, seed, *, vocab: int, count: int = 1, threshold: float = 0.9, **how) -> None:
+        if not 1 <= vocab < sample.MAX_VOCAB:
+            raise ValueError(f"vocab must be 1 to {sample.MAX_VOCAB - 1}, got {vocab}")
+        if count < 1:
+            raise ValueError("count must be 1 at least: a block of no confident row would not end")
+        unknown = set(how) - {"temperature", "top_k", "top_p", "min_p", "confidence"}
+        if unknown:
+            raise ValueError(f"sampling does not take {sorted(unknown)}")
+        self.sampling, self.mask_id = {"temperature": 0.0, **how}, vocab
+        self.count, self.threshold = count, threshold
+        if device is None:
+            return
+        self._gen = torch.Generator(device=device).manual_seed(seed)
+        # one token id a slot of the pool, and a step's logits, the mask's own included (that no row takes)
+        self.ids = torch.full((PAGE * self.pool.num_pages,), -1, dtype=torch.int32, device=device)
+        self.logits = torch.empty((0, vocab + 1), dtype=torch.bfloat16, device=device)
 
     def _page_rows(self, page_ids: np.ndarray) -> kv.KvPlan:
         """A plan of all rows of some pages."""
@@ -162,6 +201,8 @@ class ServingLoop:
         for s in admitted:
             if s.pages is None:  # a request's pages live from its first prefill to its end
                 s.pages = self.pool.take(-(-s.L // PAGE))
+                s.fresh = True
+                self._resize(s, s.L)
         items = decodes + admitted
         nd = len(decodes)
         n = [BLOCK] * nd + [s.L for s in admitted]
@@ -185,9 +226,9 @@ class ServingLoop:
             timed = capture = False
         else:
             self._nd = nd
-            self._positions = np.concatenate([np.arange(a, a + b, dtype=np.int32) for a, b in zip(o, n)]) if self.rope else None
             self._desc = (q_indptr, np.asarray(o, np.int32), kv_len, page_indptr)
-            self._run(p, page_ids, rows, timed, capture)
+            self._left = None
+            self._run(p, page_ids, rows, timed, capture, items)
         rec = Iteration(t=t, decodes=len(decodes), prefills=len(admitted),
                         prefill_tokens=int(sum(s.L for s in admitted)), waiting_after=len(self.waiting),
                         deficit=self.deficit, plan_ms=plan_ms, events=self._ev if timed else None,
@@ -195,24 +236,69 @@ class ServingLoop:
                         queue_waits=[t - s.queued_at for s in admitted])
         rec.captured = self._snap if capture else None
         rec.batch = [(s.req.rid, "decode" if k < nd else "prefill") for k, s in enumerate(items)]
-        self._advance(t, decodes, admitted)
+        if self.dev is not None and self.sampling is not None:
+            rec.left = self._left if self._left is not None else []
+        self._advance(t, decodes, admitted, rec.left)
         return rec
 
-    def _run(self, p, page_ids, rows, timed, capture):
-        pid = torch.from_numpy(page_ids).to(self.dev, non_blocking=True)
+    def _resize(self, s: _State, length: int) -> None:
+        """A request's length in the block table, from the next batch on."""
+        if self.dev is not None:
+            self._lengths[self._rows[id(s)]] = length
+            self._resized = True
+
+    def _batch_tables(self, items, rows: int, pages: int) -> tables.Tables:
+        """The block table after this iteration's requests, and what the batch's
+        calls read of it: the host sends lengths and offsets."""
+        if self._resized:
+            tables.resize(self.table, self.held, torch.from_numpy(self._lengths.copy()).to(self.dev, non_blocking=True), self.free_pages, self.num_free)
+            self._resized = False
+        q_indptr, q_offset, kv_len, _ = self._desc
+        n = len(items)
+        sent = torch.from_numpy(np.concatenate([np.asarray([self._rows[id(s)] for s in items], np.int32), kv_len, q_offset, q_indptr])).to(self.dev, non_blocking=True)
+        return tables.build(self.table, sent[:n], sent[n:2 * n], sent[3 * n:], sent[2 * n:3 * n], rows=rows, pages=pages)
+
+    def _sample(self, b: tables.Tables, items) -> None:
+        """A token for every row of the decodes' blocks, and the rows that keep
+        theirs; the responses of fresh prefills are masked first."""
+        q_indptr = self._desc[0]
+        for k, s in enumerate(items[self._nd:], self._nd):
+            if s.fresh:
+                self.ids[b.slots[int(q_indptr[k]):int(q_indptr[k + 1])][s.req.prompt:]] = self.mask_id
+                s.fresh = False
+        rows = BLOCK * self._nd
+        if rows == 0:
+            return
+        if self.logits.shape[0] < rows:  # as a language model's: a broad bulk, and in each row one token that stands out
+            self.logits = (2.2 * torch.randn((rows, self.mask_id + 1), generator=self._gen, device=self.dev)).to(torch.bfloat16)
+            high = 10.0 + 15.0 * torch.rand((rows, 1), generator=self._gen, device=self.dev)
+            self.logits.scatter_(1, torch.randint(0, self.mask_id, (rows, 1), generator=self._gen, device=self.dev), high.to(torch.bfloat16))
+        u = torch.rand((rows,), generator=self._gen, device=self.dev)
+        tokens, confidence = sample.tokens(self.logits[:rows], u, forbid=self.mask_id, **self.sampling)
+        out, left = sample.unmask(tokens, confidence, self.ids, self._indptr(self._nd), mask_id=self.mask_id, count=self.count, threshold=self.threshold,
+                                  slots=b.slots[:rows])
+        self.sampled = (tokens, confidence, out)
+        self._left = left.tolist()  # (the host waits here: the blocks that are done leave the next batch)
+
+    def _indptr(self, blocks: int) -> torch.Tensor:
+        return torch.arange(0, BLOCK * blocks + 1, BLOCK, dtype=torch.int32, device=self.dev)
+
+    def _run(self, p, page_ids, rows, timed, capture, items):
+        b = self._batch_tables(items, rows, len(page_ids))
+        pid = b.page_ids
         stream = torch.cuda.current_stream(self.dev)
         snap = None
         nd = self._nd
         q, k_new, v_new = self.q[:rows], self.k_new[:rows], self.v_new[:rows]
         if self.rope is not None:
-            positions = torch.from_numpy(self._positions).to(self.dev, non_blocking=True)
-            q, k_new = rope.rotate(self.rope, q, k_new, positions, q_out=self.q_rot[:rows], k_out=self.k_rot[:rows])
+            q, k_new = rope.rotate(self.rope, q, k_new, b.positions, q_out=self.q_rot[:rows], k_out=self.k_rot[:rows])
         if capture:
             q_indptr, q_offset, kv_len, page_indptr = self._desc
             snap = dict(q_indptr=q_indptr, q_offset=q_offset, kv_len=kv_len,
                         page_indptr=page_indptr, page_ids=page_ids, sm_scale=self.sm_scale,
                         q=q.clone(), k_new=k_new.clone(), v_new=v_new.clone(), decodes=nd)
             snap["k_pages"], snap["v_pages"] = self._pages(page_ids, pid)
+            snap["tables"] = b
         ev = lev = used = None
         if timed:
             ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True))
@@ -230,29 +316,35 @@ class ServingLoop:
         if timed:
             ev[1].record(stream)
             lev = [(lev[2 * k], lev[2 * k + 1]) for k in range(3) if used[k]]
+        if self.sampling is not None:
+            self._sample(b, items)
         if capture:
             snap["out"] = self.out[:rows].clone()
             snap["lse"] = self.lse[:rows].clone()
         self._ev, self._lev, self._snap = ev, lev, snap
 
-    def _advance(self, t, decodes, admitted):
+    def _advance(self, t, decodes, admitted, left=None):
         # advance: a prefill starts (or resumes at) its block; a decode step
         # may resolve the block, which sends the request back for a re-prefill
+        done = []
         for s in admitted:
             s.phase = "decoding"
             s.steps_left = s.req.steps[s.block]
-        for s in decodes:
-            s.steps_left -= 1
+        for k, s in enumerate(decodes):
+            s.steps_left = s.steps_left - 1 if left is None else left[k]
             if s.steps_left == 0:
                 s.block += 1
                 if s.block == len(s.req.steps):
                     s.phase = "done"
-                    self.pool.give(s.pages)
-                    s.pages = None
+                    done.append(s)
                 else:
                     s.phase = "waiting"
                     s.queued_at = t + 1
                     self.waiting.append(s)
+        for s in reversed(done):  # in the order of the block table: the first one's pages are taken first
+            self.pool.give(s.pages)
+            s.pages = None
+            self._resize(s, 0)
         self.waiting.sort(key=lambda s: (s.req.arrival, s.req.rid))
 
     def run(self, max_iterations: int, timed: bool = True) -> List[Iteration]:

@@ -1,0 +1,98 @@
+"""The serving loop with its block table on the device and with sampling
+(paper_2607_04206_amd/serve.py): page lists, positions and slots of every batch
+against the host's, tokens and confidences against their definition, the ids of
+the pool step by step until every response is resolved; quantised and rotated as
+a worker runs them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import workloads
+from paper_2607_04206_amd.serve import PAGE, ServingLoop
+from tests.test_sample import check
+from tests.test_unmask import definition
+
+
+def test_arguments():
+    reqs = workloads.serving_trace(0, 10, 0.4, median=100)
+    make = lambda **kw: ServingLoop(reqs, hq=8, hkv=2, d=64, tau=1024, device=None, sampling=kw)  # noqa: E731
+    for bad in (dict(vocab=0), dict(vocab=1 << 18), dict(vocab=100, count=0), dict(vocab=100, heat=1.0)):
+        with pytest.raises(ValueError):
+            make(**bad)
+    loop = make(vocab=100, temperature=0.5, confidence="margin")
+    loop.run(200)  # the host alone: the trace's steps
+    assert all(s.phase == "done" for s in loop.reqs)
+
+
+@pytest.mark.gpu
+def test_block_table_follows_the_pool():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    reqs = workloads.serving_trace(5, 60, 0.8, median=120)
+    loop = ServingLoop(reqs, hq=8, hkv=2, d=64, tau=2048, device=torch.device("cuda:0"), rotary={})
+    batches = 0
+    for t in range(600):
+        if not loop.busy():
+            break
+        rec = loop.step(t, timed=False, capture=True)
+        if rec is None:
+            continue
+        c = rec.captured
+        b = c["tables"]
+        assert np.array_equal(b.page_ids.cpu().numpy(), c["page_ids"]) and np.array_equal(b.page_indptr.cpu().numpy(), c["page_indptr"])
+        n = np.diff(c["q_indptr"])
+        positions = np.concatenate([o + np.arange(k) for o, k in zip(c["q_offset"], n)])
+        items = np.repeat(np.arange(len(n)), n)
+        page = c["page_ids"][c["page_indptr"][items] + positions // PAGE].astype(np.int64)
+        assert np.array_equal(b.positions.cpu().numpy(), positions) and np.array_equal(b.items.cpu().numpy(), items)
+        assert np.array_equal(b.slots.cpu().numpy(), page * PAGE + positions % PAGE)
+        batches += 1
+    assert batches > 50 and all(s.phase == "done" for s in loop.reqs)
+    assert loop.pool.free == loop.pool.num_pages
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("how,threshold,loop_kw", [
+    (dict(), 0.9, dict()), (dict(temperature=0.8, top_p=0.95), 0.5, dict(kv_format="e4m3", rotary={})),
+    (dict(temperature=1.0, top_k=50, confidence="margin"), math.inf, dict()), (dict(confidence="entropy"), -2.0, dict(rotary={}))])
+def test_sampling(how, threshold, loop_kw):
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    reqs = workloads.serving_trace(7, 12, 0.5, median=100, resp=64)
+    vocab = 1999
+    loop = ServingLoop(reqs, hq=8, hkv=2, d=64, tau=1024, device=torch.device("cuda:0"), sampling=dict(vocab=vocab, count=3, threshold=threshold, **how), **loop_kw)
+    params = {"temperature": 0.0, "top_k": 0, "top_p": 1.0, **how}
+    kind = params.pop("confidence", "probability")
+    steps = 0
+    for t in range(2000):
+        if not loop.busy():
+            break
+        before = loop.ids.cpu().numpy()
+        rec = loop.step(t, timed=False, capture=True)
+        if rec is None:
+            continue
+        nd, c = rec.decodes, rec.captured
+        slots = c["tables"].slots.cpu().numpy()
+        after = loop.ids.cpu().numpy()
+        expect = before.copy()
+        for k in range(nd, len(c["kv_len"])):  # prefills: only fresh ones mask their response
+            rid = rec.batch[k][0]
+            state = next(s for s in loop.reqs if s.req.rid == rid)
+            if state.block == 0:
+                expect[slots[c["q_indptr"][k] + state.req.prompt:c["q_indptr"][k + 1]]] = vocab
+        if nd:
+            rows = 32 * nd
+            tokens, confidence, out = (x.cpu().numpy() for x in loop.sampled)
+            if steps % 5 == 0 and params["temperature"] == 0:
+                for r in range(0, rows, 7):
+                    check(loop.logits[r].double().cpu().numpy(), int(tokens[r]), float(confidence[r]), 0.0, params["temperature"], kind, params["top_k"],
+                          float(np.float32(params["top_p"])), forbid=vocab)
+            assert (tokens >= 0).all() and (tokens < vocab).all()
+            want, left = definition(tokens, confidence, expect[slots[:rows]], np.arange(0, rows + 1, 32), vocab, [3] * nd, [np.float32(threshold)] * nd)
+            assert np.array_equal(out, want) and rec.left == left.tolist()
+            expect[slots[:rows]] = want
+            steps += 1
+        assert np.array_equal(after, expect), f"iteration {t}"
+    assert steps > 5 and all(s.phase == "done" for s in loop.reqs) and loop.pool.free == loop.pool.num_pages
