@@ -112,6 +112,8 @@ struct Counts {
         uint32_t counts[2 * kSide];
     };
     float wave_top[2][kWaves];
+    double wave_sums[2 * kWaves];
+    int32_t first_token;
 };
 
 // E: logits of a thread in a chunk.
@@ -589,6 +591,7 @@ struct Params {
     float temperature, top_p, min_p, u;
     int top_k;
     bool none;  // the row's entry is outside: nothing is taken
+    __device__ bool whole() const { return temperature == 0.0f && top_k == 0 && top_p >= 1.0f && min_p <= 0.0f; }
 };
 
 __device__ __forceinline__ Params params_of(const SampleArgs& a, int64_t r) {
@@ -1168,6 +1171,159 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
     return true;
 }
 
+// ---------------------------------------------------------------- the first token, of everything
+
+// Where nothing filters and the first token is taken, no ranks are needed: one
+// look sums weights in 32 bits, eight at a time, and those sums in 64. A weight is
+// 2^(c x - shift) with shift the lane's largest c x so far; c in two parts, so that
+// weights are off by 2^-23 (1 + |c x - shift|) at most and by chance.
+struct Whole {
+    double s, st;   // weights, and weights times their exponent
+    float shift;    // of both
+    float best, next;
+    int32_t token;  // the first with the largest logit
+    int32_t fine;   // there are weights, and all are numbers
+};
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2eRest = float(1.4426950408889634074 - double(kLog2e));
+constexpr float kLowestBest = -1e38f;
+
+// Sums of two ranges as one.
+__device__ __forceinline__ void join(double& s, double& st, float& shift, double s2, double st2, float shift2) {
+    const float top = fmaxf(shift, shift2);
+    const double d = double(shift) - double(top), d2 = double(shift2) - double(top), f = exp2(d), f2 = exp2(d2);
+    st = f * (st + s * d) + f2 * (st2 + s2 * d2);
+    s = f * s + f2 * s2;
+    shift = top;
+}
+
+// The product as 32 bits hold it, wherever it is used (and not fused with what it is subtracted from).
+__device__ __forceinline__ float shift_of(float best) {
+    float shift = best * kLog2e;
+    asm("" : "+v"(shift));
+    return shift;
+}
+__device__ __forceinline__ float exponent_of(float x, float shift) { return __builtin_fmaf(x, kLog2eRest, __builtin_fmaf(x, kLog2e, -shift)); }
+
+template <int KIND, typename T, int E>
+__device__ __forceinline__ Whole look_once(Counts& sh, const Row<T, E>& row) {
+    constexpr int V = Row<T, E>::V, kBatch = 8 / V;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    double s = 0.0, st = 0.0;
+    float best = kLowestBest, next = -INFINITY, shift = shift_of(kLowestBest);
+    int at = INT32_MAX;
+    auto add = [&](auto& x, int n) {  // n logits, of which best takes note already
+        const float to = shift_of(best);
+        const float r = __builtin_amdgcn_exp2f(shift - to);
+        float part = 0.0f, part_t = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e >= n) break;
+            const float t = exponent_of(x[e], to), w = __builtin_amdgcn_exp2f(t);
+            part += w;
+            if (KIND == SANGAM_CONFIDENCE_ENTROPY) part_t += w > 0.0f ? w * t : 0.0f;
+        }
+        if (KIND == SANGAM_CONFIDENCE_ENTROPY) st = double(r) * (st + s * double(shift - to)) + double(part_t);
+        s = double(r) * s + double(part);
+        shift = to;
+    };
+    auto note = [&](float m, int i) {
+        if (m > best) at = i;
+        best = fmaxf(best, m);
+    };
+    row.each_chunk([&](int, int v0, const auto& w) {
+#pragma unroll
+        for (int j = 0; j < Row<T, E>::kLoads; j += kBatch) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int k = v0 + (j + i) * kThreads + tid;
+                float y[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = -INFINITY;
+                if (k < row.last) row.unpack(w[j + i], row.head + k * V, y);
+                float m = y[0];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    if (e > 0) m = fmaxf(m, y[e]);
+                    x[i * V + e] = y[e];
+                }
+                if (KIND == SANGAM_CONFIDENCE_MARGIN) {
+                    float most = best;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        next = fmaxf(next, fminf(most, y[e]));
+                        most = fmaxf(most, y[e]);
+                    }
+                }
+                note(m, row.head + k * V);
+            }
+            add(x, 8);
+            __builtin_amdgcn_sched_barrier(0);  // (side by side batches take all registers)
+        }
+    });
+    row.each_edge([&](int i, float x) {
+        if (KIND == SANGAM_CONFIDENCE_MARGIN) next = fmaxf(next, fminf(best, x));
+        if (x == best && i < at) at = i;
+        note(x, i);
+        const float one[8] = {x};
+        add(one, 1);
+    });
+    // all lanes', then all waves'
+    float top = wave_max(best);
+    if (lane == 0) sh.wave_top[0][wave] = top;
+    __syncthreads();
+    if (tid == 0) sh.first_token = INT32_MAX;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.wave_top[0][w]);
+    const int holders = __syncthreads_count(best == top);
+    const float mine = wave_max(best == top && holders == 1 ? next : best);
+    if (best == top && at < row.vocab)
+        for (int e = 0; e < V && at + e < row.vocab; ++e)
+            if (row.at(at + e) == top) {
+                atomicMin(&sh.first_token, at + e);
+                break;
+            }
+    const float to = shift_of(top);
+    const double d = double(shift) - double(to), f = exp2(d);
+    st = f * (st + s * d);
+    s = f * s;
+#pragma unroll
+    for (int k = 32; k > 0; k /= 2) {
+        s += __shfl_xor(s, k);
+        st += __shfl_xor(st, k);
+    }
+    if (lane == 0) {
+        sh.wave_top[1][wave] = mine;
+        sh.wave_sums[wave] = s;
+        sh.wave_sums[kWaves + wave] = st;
+    }
+    __syncthreads();
+    Whole all{0.0, 0.0, to, top, -INFINITY, sh.first_token, 0};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        all.s += sh.wave_sums[w];
+        all.st += sh.wave_sums[kWaves + w];
+        all.next = fmaxf(all.next, sh.wave_top[1][w]);
+    }
+    all.fine = all.s > 0.0 && all.s < 1e30 && top > kLowestBest && all.token < row.vocab;  // (no number fails)
+    return all;
+}
+
+template <typename T, int E>
+__device__ __forceinline__ Whole look_once(Counts& sh, const Row<T, E>& row, int kind) {
+    return kind == SANGAM_CONFIDENCE_ENTROPY  ? look_once<SANGAM_CONFIDENCE_ENTROPY>(sh, row)
+           : kind == SANGAM_CONFIDENCE_MARGIN ? look_once<SANGAM_CONFIDENCE_MARGIN>(sh, row)
+                                              : look_once<SANGAM_CONFIDENCE_PROBABILITY>(sh, row);
+}
+
+__device__ __forceinline__ void answer(const SampleArgs& a, int64_t r, const Whole& all) {
+    double c = exp2(double(exponent_of(all.best, all.shift))) / all.s;
+    if (a.confidence == SANGAM_CONFIDENCE_MARGIN) c -= exp2(double(exponent_of(all.next, all.shift))) / all.s;
+    if (a.confidence == SANGAM_CONFIDENCE_ENTROPY) c = 0.69314718055994530942 * (all.st / all.s) - log(all.s);
+    answer(a, r, all.token, c);
+}
+
 template <typename T, int E>
 __device__ __forceinline__ Row<T, E> row_of(const SampleArgs& a, int64_t r, const Params& p) {
     Row<T, E> row;
@@ -1201,7 +1357,7 @@ __device__ __forceinline__ void start(Shared<E>& sh) {
     if (threadIdx.x < 64) sh.powers[threadIdx.x] = exp2(threadIdx.x * (-1.0 / 64));
 }
 
-constexpr int kPending = -2;  // the token of a row that its values did not tell
+constexpr int kPending = -2;  // the token of a row that the launch before did not tell
 
 // A work-group takes a row of bf16. (What sample_kernel takes more registers for
 // is left to it: three work-groups fit a CU.)
@@ -1225,34 +1381,55 @@ __global__ __launch_bounds__(kThreads, 6) void sample_values_kernel(SampleArgs a
     if (!choose_by_value(sh, row, a, p, r)) answer(a, r, kPending, 0.0);
 }
 
-// A work-group takes a row, or the pending ones of some rows.
+// A work-group takes a row of which the first token is wanted, of everything.
+template <typename T, int KIND>
+__global__ __launch_bounds__(kThreads) void sample_whole_kernel(SampleArgs a) {
+    __shared__ Counts sh;
+    const int64_t r = blockIdx.x;
+    const Params p = params_of(a, r);
+    if (p.none) {
+        answer(a, r, -1, 0.0);
+        return;
+    }
+    if (p.whole()) {
+        const Whole all = look_once<KIND>(sh, row_of<T, kWhole<T>>(a, r, p));
+        if (all.fine) {
+            answer(a, r, all);
+            return;
+        }
+    }
+    answer(a, r, kPending, 0.0);
+}
+
+// A work-group takes a row, or its row if it is pending.
 template <typename T, bool PENDING>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, int64_t rows) {
+__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     constexpr int E = kWhole<T>;
     __shared__ Shared<E> sh;
-    const int64_t step = gridDim.x;
-    start(sh);
-    for (int64_t r0 = blockIdx.x; r0 < rows; r0 += 64 * step) {
-        uint64_t todo = 1;
-        if (PENDING) {
-            const int64_t mine = r0 + (threadIdx.x & 63) * step;
-            todo = __ballot(mine < rows && a.tokens[mine] == kPending);
-            __syncthreads();  // (all waves have looked before a row gets its token)
-        }
-        while (todo) {
-            const int64_t r = r0 + __builtin_ctzll(todo) * step;
-            todo &= todo - 1;
-            const Params p = params_of(a, r);
-            if (p.none) {
-                answer(a, r, -1, 0.0);
-                continue;
-            }
-            Row<T, E> row = row_of<T, E>(a, r, p);
-            __syncthreads();
-            from_logits(sh, row, a, p, r);
-        }
-        if (!PENDING) break;
+    const int64_t r = blockIdx.x;
+    if (PENDING && a.tokens[r] != kPending) return;
+    const Params p = params_of(a, r);
+    if (p.none) {
+        answer(a, r, -1, 0.0);
+        return;
     }
+    Row<T, E> row = row_of<T, E>(a, r, p);
+    start(sh);
+    __syncthreads();  // (and all waves have looked before the row gets its token)
+    from_logits(sh, row, a, p, r);
+}
+
+// The kernels of a type.
+template <typename T>
+const void* whole_kernel(int kind) {
+    return kind == SANGAM_CONFIDENCE_ENTROPY  ? reinterpret_cast<const void*>(&sample_whole_kernel<T, SANGAM_CONFIDENCE_ENTROPY>)
+           : kind == SANGAM_CONFIDENCE_MARGIN ? reinterpret_cast<const void*>(&sample_whole_kernel<T, SANGAM_CONFIDENCE_MARGIN>)
+                                              : reinterpret_cast<const void*>(&sample_whole_kernel<T, SANGAM_CONFIDENCE_PROBABILITY>);
+}
+template <typename T>
+const void* row_kernel(bool pending) {
+    if (__is_same(T, __bf16) || pending) return reinterpret_cast<const void*>(&sample_kernel<T, true>);
+    return reinterpret_cast<const void*>(&sample_kernel<T, __is_same(T, __bf16)>);
 }
 
 // Few rows are cut into parts, of some chunks each: a work-group counts a part, and
@@ -1291,6 +1468,9 @@ __global__ __launch_bounds__(kThreads) void sample_part_kernel(SampleArgs a, Spl
         __syncthreads();
         for (int k = threadIdx.x; k < kSide; k += kThreads)
             reinterpret_cast<uint32_t*>(record)[k] = sh.counts[2 * k] | (sh.counts[2 * k + 1] << 16);
+    } else if (p.whole()) {
+        const Whole all = look_once(sh, row, a.confidence);
+        if (threadIdx.x == 0) *reinterpret_cast<Whole*>(record) = all;
     } else {
         float top;
         const Filled filled = fill(sh, row, top, tops);
@@ -1354,6 +1534,23 @@ __global__ __launch_bounds__(kThreads) void sample_join_kernel(SampleArgs a, Spl
         uncount(sh, row);
         __syncthreads();
         if (choose_by_value(sh, row, a, p, r)) return;
+    } else if (p.whole()) {
+        Whole all{0.0, 0.0, shift_of(kLowestBest), -INFINITY, -INFINITY, INT32_MAX, 1};
+        for (int part = 0; part < s.parts; ++part) {
+            const Whole w = *reinterpret_cast<const Whole*>(at + part * s.record);
+            // (a part without weight has no say; one with what is no number is not summed up)
+            if (!w.fine && w.s == 0.0 && w.best == kLowestBest) continue;
+            all.fine = all.fine && w.fine;
+            join(all.s, all.st, all.shift, w.s, w.st, w.shift);
+            all.next = fmaxf(fmaxf(all.next, w.next), fminf(all.best, w.best));
+            if (w.best > all.best) all.token = w.token;  // (parts come in order)
+            if (w.best == all.best) all.token = min(all.token, w.token);
+            all.best = fmaxf(all.best, w.best);
+        }
+        if (all.fine && all.s > 0.0) {
+            answer(a, r, all);
+            return;
+        }
     } else {
         float top = -INFINITY;
         bool far = false, any = false;
@@ -1473,6 +1670,7 @@ sangam_status sample(const sangam_sample_desc* d, int32_t* tokens, float* confid
         if (const sangam_status e = launch(part, d->rows * split.parts, kargs)) return e;
         return launch(join, d->rows, kargs);
     }
+    const bool maybe_whole = d->temperatures || d->temperature == 0.0f;  // rows whose first token of everything is wanted
     // a grid's threads are counted in 32 bits
     const int64_t step = (int64_t(1) << 32) / kThreads - 1;
     for (int64_t row = 0; row < d->rows; row += step) {
@@ -1482,15 +1680,16 @@ sangam_status sample(const sangam_sample_desc* d, int32_t* tokens, float* confid
         if (some.params_of) some.params_of += row;
         some.tokens += row;
         if (some.conf) some.conf += row;
-        int64_t rows = std::min(step, d->rows - row);
-        void* kargs[] = {&some, &rows};
-        if (bf16) {
-            if (const sangam_status e = launch(reinterpret_cast<const void*>(&sample_values_kernel), rows, kargs)) return e;
-            if (const sangam_status e = launch(reinterpret_cast<const void*>(&sample_kernel<__bf16, true>), std::min<int64_t>(rows, 256), kargs)) return e;
-        } else if (const sangam_status e = launch(fp32 ? reinterpret_cast<const void*>(&sample_kernel<float, false>)
-                                                       : reinterpret_cast<const void*>(&sample_kernel<_Float16, false>), rows, kargs)) {
-            return e;
-        }
+        const int64_t rows = std::min(step, d->rows - row);
+        void* kargs[] = {&some};
+        const bool pending = bf16 || maybe_whole;
+        if (pending)
+            if (const sangam_status e = launch(bf16   ? reinterpret_cast<const void*>(&sample_values_kernel)
+                                               : fp32 ? whole_kernel<float>(d->confidence)
+                                                      : whole_kernel<_Float16>(d->confidence), rows, kargs))
+                return e;
+        const void* fn = bf16 ? row_kernel<__bf16>(pending) : fp32 ? row_kernel<float>(pending) : row_kernel<_Float16>(pending);
+        if (const sangam_status e = launch(fn, rows, kargs)) return e;
     }
     return SANGAM_OK;
 }

@@ -28,6 +28,14 @@ def _each(x, name: str, dtype, dev, entries: Optional[int], lowest, highest):
     return None, x, entries
 
 
+def _result(t: Optional[torch.Tensor], name: str, entries: int, dtype, dev, stream) -> Tuple[torch.Tensor, int]:
+    """The tensor that a result goes to, made here if none was passed, and its address."""
+    if t is None:
+        t = _new((entries,), dtype, dev, stream)
+        return t, t.data_ptr()
+    return t, _ints(t, name, dev, entries, dtype)
+
+
 def tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: Union[float, torch.Tensor] = 1.0, top_k: Union[int, torch.Tensor] = 0,
            top_p: Union[float, torch.Tensor] = 1.0, min_p: Union[float, torch.Tensor] = 0.0, params_of: Optional[torch.Tensor] = None,
            confidence: str = "probability", forbid: int = -1, out: Optional[torch.Tensor] = None, confidence_out: Optional[torch.Tensor] = None,
@@ -61,10 +69,8 @@ def tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: Union[float, t
     k, k_all, entries = _each(top_k, "top_k", torch.int32, dev, entries, 0, 2 ** 31 - 1)
     p, p_all, entries = _each(top_p, "top_p", torch.float32, dev, entries, 0.0, 1.0)
     m, m_all, entries = _each(min_p, "min_p", torch.float32, dev, entries, 0.0, 1.0)
-    if out is None:
-        out = _new((rows,), torch.int32, dev, stream)
-    if confidence_out is None:
-        confidence_out = _new((rows,), torch.float32, dev, stream)
+    out, to = _result(out, "out", rows, torch.int32, dev, stream)
+    confidence_out, c_to = _result(confidence_out, "confidence_out", rows, torch.float32, dev, stream)
     dtype = DTYPES[logits.dtype]
     need = lib.sangam_sample_workspace_bytes(rows, vocab, dtype)
     if workspace is None and need > 0:
@@ -73,8 +79,7 @@ def tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: Union[float, t
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
     d = SampleDesc(logits.data_ptr(), rows, logits.stride(0) if rows > 1 else 0, vocab, dtype, _ints(u, "u", dev, rows, torch.float32), of,
                    2 ** 31 if entries is None else entries, t, k, p, m, t_all, k_all, p_all, m_all, CONFIDENCES[confidence], forbid)
-    _launch(dev, lib.sangam_sample_tokens, ctypes.byref(d), _ints(out, "out", dev, rows),
-            _ints(confidence_out, "confidence_out", dev, rows, torch.float32), workspace.data_ptr() if workspace is not None else None,
+    _launch(dev, lib.sangam_sample_tokens, ctypes.byref(d), to, c_to, workspace.data_ptr() if workspace is not None else None,
             workspace.numel() * workspace.element_size() if workspace is not None else 0, s)
     return out, confidence_out
 
@@ -102,13 +107,11 @@ def unmask(tokens: torch.Tensor, confidence: torch.Tensor, ids: torch.Tensor, ro
         raise ValueError("row_indptr must hold an entry more than blocks")
     n, n_all, _ = _each(count, "count", torch.int32, dev, blocks, 0, 2 ** 31 - 1)
     c, c_all, _ = _each(threshold, "threshold", torch.float32, dev, blocks, -math.inf, math.inf)
-    if out is None:
-        out = _new((rows,), torch.int32, dev, stream)
-    if left is None:
-        left = _new((blocks,), torch.int32, dev, stream)
+    out, to = _result(out, "out", rows, torch.int32, dev, stream)
+    left, l_to = _result(left, "left", blocks, torch.int32, dev, stream)
     d = UnmaskDesc(_ints(tokens, "tokens", dev, rows),
                    _ints(confidence, "confidence", dev, rows, torch.float32), _ints(ids, "ids", dev, rows if slots is None else None),
                    None if slots is None else _ints(slots, "slots", dev, rows, torch.int64), indptr, n, c, rows, ids.shape[0], blocks,
                    mask_id, n_all, c_all)
-    _launch(dev, lib.sangam_sample_unmask, ctypes.byref(d), _ints(out, "out", dev, rows), _ints(left, "left", dev, blocks), s)
+    _launch(dev, lib.sangam_sample_unmask, ctypes.byref(d), to, l_to, s)
     return out, left

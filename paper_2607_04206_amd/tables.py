@@ -63,7 +63,10 @@ def resize(table: torch.Tensor, held: torch.Tensor, lengths: torch.Tensor, free:
     m = _ints(num_free, "num_free", dev, 1)
     if short is None:
         short = _new((1,), torch.int32, dev, stream)
-    _launch(dev, lib.sangam_tables_resize, ctypes.byref(c_table), h, n, f, free.numel(), m, _ints(short, "short", dev, 1), s)
+        left = short.data_ptr()
+    else:
+        left = _ints(short, "short", dev, 1)
+    _launch(dev, lib.sangam_tables_resize, ctypes.byref(c_table), h, n, f, free.numel(), m, left, s)
     return short
 
 
@@ -88,12 +91,15 @@ def build(table: torch.Tensor, request: Optional[torch.Tensor], kv_len: torch.Te
                         _ints(q_indptr, "q_indptr", dev, items + 1), _ints(q_offset, "q_offset", dev, items),
                         None if q_pos is None else _ints(q_pos, "q_pos", dev, rows))
     if out is None:
-        # (one allocation: each costs about as much as the launch's own work here)
+        # (one allocation and no checks of it: each costs about as much as the launch's own work here)
         sizes = [2 * rows, rows, rows, items + 1, pages]
-        slots, positions, row_items, page_indptr, page_ids = _new((4 * rows + items + 1 + pages,), torch.int32, dev, stream).split(sizes)
+        memory = _new((sum(sizes),), torch.int32, dev, stream)
+        slots, positions, row_items, page_indptr, page_ids = memory.split(sizes)
         out = Tables(page_indptr, page_ids, positions, slots.view(torch.int64), row_items)
-    _launch(dev, lib.sangam_tables_build, ctypes.byref(c_table), ctypes.byref(batch),
-            _ints(out.page_indptr, "out.page_indptr", dev, items + 1), _ints(out.page_ids, "out.page_ids", dev, pages), pages,
-            _ints(out.positions, "out.positions", dev, rows), _ints(out.slots, "out.slots", dev, rows, torch.int64),
-            _ints(out.items, "out.items", dev, rows), rows, s)
+        at = memory.data_ptr()
+        to = at + 16 * rows, at + 16 * rows + 4 * (items + 1), at + 8 * rows, at, at + 12 * rows
+    else:
+        to = (_ints(out.page_indptr, "out.page_indptr", dev, items + 1), _ints(out.page_ids, "out.page_ids", dev, pages),
+              _ints(out.positions, "out.positions", dev, rows), _ints(out.slots, "out.slots", dev, rows, torch.int64), _ints(out.items, "out.items", dev, rows))
+    _launch(dev, lib.sangam_tables_build, ctypes.byref(c_table), ctypes.byref(batch), to[0], to[1], pages, to[2], to[3], to[4], rows, s)
     return out
