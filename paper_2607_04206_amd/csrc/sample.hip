@@ -338,15 +338,15 @@ struct Row {
             f(i, at(i));
         }
     }
-    // A little under all logits of the row's first n bins, and a little above those behind the first n.
-    __device__ __forceinline__ float lowest(int n) const {
+    // A little under all logits of the row's first n bins, and a little above those behind the first n. The little: a part of the
+    // border, rounded to 32 bits, and what t is rounded by (2^-33 around kOrigin, else 2^-52 of the numbers it is made of), which
+    // alone counts at a border near 0: logits of +-1e-20 have the t of 0.
+    __device__ __forceinline__ double border(int n, double side) const {
         const double x = wide ? top - n / scale : (kOrigin - double(base + n)) / scale;
-        return scale > 0.0 ? scalar(float(fmax(x - fabs(x) * 0x1p-22, -3.5e38))) : -INFINITY;
+        return x + side * (fabs(x) * 0x1p-22 + (wide ? (fabs(top) + n / scale) * 0x1p-48 : 0x1p-30 / scale));
     }
-    __device__ __forceinline__ float highest(int n) const {
-        const double x = wide ? top - n / scale : (kOrigin - double(base + n)) / scale;
-        return scale > 0.0 ? scalar(float(x + fabs(x) * 0x1p-22)) : INFINITY;
-    }
+    __device__ __forceinline__ float lowest(int n) const { return scale > 0.0 ? scalar(float(fmax(border(n, -1.0), -3.5e38))) : -INFINITY; }
+    __device__ __forceinline__ float highest(int n) const { return scale > 0.0 ? scalar(float(border(n, 1.0))) : INFINITY; }
     // All logits of the row from `low` to `high`. Where tops says that few chunks of
     // threads hold any, these are listed, and the vectors in them dealt over all
     // threads, so that they come in one or two rounds of loads (a thread that walked
@@ -1023,9 +1023,11 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
     __syncthreads();
     // up to the end of the lane's block, and of the one before (the tiny ones lie before the lower half)
     const double tiny_mass = tiny ? scalar(mass_of(0.0f, tiny)) : 0.0;
-    const int tokens_end = wave_up_to(sh.block_tokens[lane]) + (lane >= 32 ? tiny : 0);
-    const double mass_end = wave_up_to(__builtin_bit_cast(double, sh.block_mass[lane])) + (lane >= 32 ? tiny_mass : 0.0);
-    const int tokens_start = tokens_end - sh.block_tokens[lane];
+    const int block_tokens = sh.block_tokens[lane];
+    const double block_mass = __builtin_bit_cast(double, sh.block_mass[lane]);
+    const int tokens_end = wave_up_to(block_tokens) + (lane >= 32 ? tiny : 0);
+    const double mass_end = wave_up_to(block_mass) + (lane >= 32 ? tiny_mass : 0.0);
+    const int tokens_start = tokens_end - block_tokens;
     const double mass_start = lane == 0 ? 0.0 : __shfl_up(mass_end, 1) + (lane == 32 ? tiny_mass : 0.0);
     const int all_tokens = lane_of(tokens_end, 63);
     const double all_mass = lane_of(mass_end, 63);
@@ -1071,7 +1073,7 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
                     continue;
                 }
                 reach = scalar(p.u > 0.0f ? fmin(double(p.u), 1.0) * M : 0.0);
-                by = By::kAbove;
+                by = p.u < 1.0f || !(p.u == p.u) ? By::kAbove : By::kReach;  // (from 1 on the last of any weight)
             }
         } else if (stage == kMinP) {
             if (!(p.min_p > 0.0f)) continue;
@@ -1086,11 +1088,15 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
             if (a.confidence != SANGAM_CONFIDENCE_MARGIN || kept.before + kept.tokens < 2) continue;
             reach = 2.0;
         }
+    again:
         auto met = [&](double end) { return by == By::kAbove ? end > reach : end >= reach; };
-        // the block: the first that has tokens and ends at the place or behind it (or, as sums are rounded, the last with any)
-        const bool some = by == By::kCut || tokens_end > tokens_start;
+        // the block: the first that has tokens, or weight, and ends at the place or behind it (or, as sums are rounded, the last with
+        // any; rounded sums of nothing may grow as well, so that what has no weight is no place by weight)
+        const bool by_mass = by == By::kReach || by == By::kAbove;
+        const bool some = by == By::kCut || (by_mass ? block_mass > 0.0 : block_tokens > 0);
         const double block_end = by == By::kCount ? double(tokens_end) : by == By::kCut ? double(kBlock * lane + kBlock) : mass_end;
-        const uint64_t in = __ballot(some && met(block_end)), any = __ballot(some && (by == By::kCount || by == By::kCut || mass_end > mass_start));
+        const uint64_t in = __ballot(some && met(block_end)), any = __ballot(some);
+        if (in == 0 && tiny > 0) return false;
         const int at = in ? __builtin_ctzll(in) : 63 - __builtin_clzll(any);
         const double block_start = by == By::kCount ? double(tokens_start) : by == By::kCut ? double(kBlock * lane) : mass_start;
         if (tiny > 0 && at >= 32 && __ballot(lane == at && met(block_start)) != 0) return false;  // among the tiny ones
@@ -1102,18 +1108,24 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
         const double end0 = by == By::kCount ? double(n_end0) : by == By::kCut ? double(q + 1) : m_end0;
         const double end1 = by == By::kCount ? double(n_end1) : by == By::kCut ? double(q + 65) : m_end1;
         const bool none = by == By::kCut;
-        const uint64_t in0 = __ballot((none || n0 > 0) && met(end0)), in1 = __ballot((none || n1 > 0) && met(end1));
+        const uint64_t in0 = __ballot((none || (by_mass ? m0 > 0.0 : n0 > 0)) && met(end0)), in1 = __ballot((none || (by_mass ? m1 > 0.0 : n1 > 0)) && met(end1));
         const uint64_t with0 = __ballot(m0 > 0.0), with1 = __ballot(m1 > 0.0);
         const int k = in0 ? __builtin_ctzll(in0) : in1 ? 64 + __builtin_ctzll(in1) : with1 ? 127 - __builtin_clzll(with1) : 63 - __builtin_clzll(with0 | 1);
         const int here = k < 64 ? lane_of(n0, k) : lane_of(n1, k - 64);
         ValuePrefix x{kBlock * at + k, here, k < 64 ? lane_of(n_end0 - n0, k) : lane_of(n_end1 - n1, k - 64), 0.0};
         // (what lies before: the end of the one before, the very number that was compared)
         x.mass = k == 0 ? lane_of(mass_start, at) : k <= 64 ? lane_of(m_end0, k - 1) : lane_of(m_end1, k - 65);
-        if (x.q > kept.q) continue;  // (not met within what is kept)
+        if (x.q > kept.q) {  // not met within what is kept
+            if (stage != kDraw) continue;
+            if (by == By::kCount) return false;  // (counts are exact: the second time it is)
+            by = By::kCount;  // rounded sums: the last that is kept
+            reach = double(kept.before + kept.tokens);
+            goto again;
+        }
         const int most = x.q == kept.q ? kept.tokens : here;
         const double each = scalar(weight_at(t_of(value_at(x.q))));
         if (by == By::kCount) x.tokens = int(reach) - x.before;
-        if (by == By::kReach) x.tokens = scalar(max(1, min(here, int(ceil(fmin((reach - x.mass) / each, 0x1p30))))));
+        if (by == By::kReach) x.tokens = scalar(max(1, min(most, int(ceil(fmin((reach - x.mass) / each, 0x1p30))))));
         if (by == By::kAbove) x.tokens = scalar(max(1, min(most, int(floor(fmin((reach - x.mass) / each, 0x1p30))) + 1)));
         if (stage <= kMinP) {
             if (x.q < kept.q || x.tokens < kept.tokens) kept = x;
@@ -1493,7 +1505,7 @@ __global__ __launch_bounds__(kThreads) void sample_join_kernel(SampleArgs a, Spl
     const uint8_t* const at = s.workspace + r * s.row_bytes;
     typedef uint32_t U4 __attribute__((ext_vector_type(4)));
     const U4* const tops = reinterpret_cast<const U4*>(at + s.parts * s.record);
-        constexpr int kTopPieces = Shared<kPart>::kTops / 8 / kThreads;
+    constexpr int kTopPieces = Shared<kPart>::kTops / 8 / kThreads;
 #pragma unroll
     for (int j = 0; j < kTopPieces; ++j)
         if (int(threadIdx.x) + j * kThreads < s.chunks * kThreads / 8)
@@ -1677,7 +1689,14 @@ sangam_status sample(const sangam_sample_desc* d, int32_t* tokens, float* confid
         SampleArgs some = args;
         some.logits = static_cast<const uint8_t*>(d->logits) + row * d->row_stride * int64_t(size);
         some.u += row;
-        if (some.params_of) some.params_of += row;
+        if (some.params_of) {
+            some.params_of += row;
+        } else if (arrays) {
+            some.num_params -= row;
+            for (const float** x : {&some.temperatures, &some.top_ps, &some.min_ps})
+                if (*x) *x += row;
+            if (some.top_ks) some.top_ks += row;
+        }
         some.tokens += row;
         if (some.conf) some.conf += row;
         const int64_t rows = std::min(step, d->rows - row);

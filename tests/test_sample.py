@@ -187,29 +187,76 @@ def test_strides(dev, dtype, pad, offset):
 
 
 @pytest.mark.gpu
-def test_uniform_numbers(dev):
+@pytest.mark.parametrize("filters", [dict(top_p=0.9), dict(), dict(top_k=13), dict(min_p=0.01), dict(top_k=300, top_p=0.5, min_p=0.1)])
+@pytest.mark.parametrize("vocab", [777, 20000])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_ends_of_the_uniform_numbers(dev, dtype, vocab, filters):
     """The ends of u, and numbers that are none of it."""
     gen = torch.Generator().manual_seed(3)
-    logits = make((8, 777), "normal", torch.float32, gen)
+    logits = make((8, vocab), "normal", DTYPES[dtype], gen)
     u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, 7.0, -1.0, math.nan, 2.0 ** -149, 0.5])
-    tokens, _ = sample.tokens(logits.to(dev), u.to(dev), temperature=1.0, top_p=0.9)
+    tokens, _ = sample.tokens(logits.to(dev), u.to(dev), temperature=1.0, **filters)
     tokens = tokens.cpu()
     for r in range(8):
-        order, w, _ = ranked(logits[r].numpy(), 1.0, top_p=float(np.float32(0.9)))
+        order, w, _ = ranked(logits[r].double().numpy(), 1.0, **{k: v if k == "top_k" else float(np.float32(v)) for k, v in filters.items()})
         last = order[int((w > 0).sum()) - 1]
         if r in (0, 4, 5, 6):
             assert tokens[r] == order[0]
-        elif r in (1, 2, 3):
+        elif r in (2, 3):
             assert tokens[r] == last
-    # halves to the last bit: six equal tokens, u M = 3 exactly
-    equal = torch.full((4, 6), 2.5, device=dev)
+        elif r == 1:  # up to 2^-24 short of the last weight
+            assert order.tolist().index(int(tokens[r])) == min(int(np.searchsorted(np.cumsum(w), float(u[1]) * w.sum(), side="right")), int((w > 0).sum()) - 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_halves_to_the_last_bit(dev, dtype):
+    # six equal tokens, u M = 3 exactly
+    equal = torch.full((4, 6), 2.5, dtype=DTYPES[dtype], device=dev)
     tokens, conf = sample.tokens(equal, torch.tensor([0.0, 0.5, 0.5 - 2.0 ** -25, 1.0], device=dev), temperature=0.7)
     assert tokens.tolist() == [0, 3, 2, 5] and conf.tolist() == [float(np.float32(1 / 6))] * 4
     tokens, conf = sample.tokens(equal, torch.full((4,), 0.99, device=dev), temperature=0.7, top_p=0.5)
     assert tokens.tolist() == [2] * 4 and conf.tolist() == [float(np.float32(1 / 3))] * 4
-    many = torch.zeros((2, 4096), device=dev)  # more of them than are sorted
+    many = torch.zeros((2, 4096), dtype=DTYPES[dtype], device=dev)  # more of them than are sorted
     tokens, conf = sample.tokens(many, torch.tensor([0.5, 0.25], device=dev), temperature=1.0, top_p=0.5)
     assert tokens.tolist() == [1024, 512] and conf.tolist() == [1 / 2048] * 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_zeros_and_far_values_among_others(dev, dtype):
+    """Zeros, tiny and huge logits last, first and in the middle of the ranks, where bf16 has no counts of its own for them."""
+    gen = torch.Generator().manual_seed(21)
+    rows = []
+    for other in (torch.rand(700, generator=gen) + 0.1, -torch.rand(700, generator=gen) - 0.1, torch.randn(700, generator=gen)):
+        for few in (torch.zeros(40), torch.full((40,), 1e-20), torch.full((40,), -3e-9), torch.full((1,), 300.0), torch.full((40,), -300.0),
+                    torch.cat([torch.zeros(20), -torch.zeros(20)])):
+            x = torch.cat([other, few, few.flip(0)[:5], torch.full((100 - len(few) - min(5, len(few)),), -INF)])
+            rows.append(x[torch.randperm(len(x), generator=gen)])
+    logits = torch.stack(rows).to(DTYPES[dtype])
+    n = len(rows)
+    for params in (dict(temperature=2.0), dict(temperature=30.0), dict(temperature=1.0, top_k=720), dict(temperature=5.0, top_p=0.97), dict(temperature=3.0, min_p=0.6),
+                   dict(temperature=0.0), dict(temperature=200.0, top_k=710, min_p=0.3)):
+        for u in (torch.rand(n, generator=gen), 1 - 2.0 ** -10 * torch.rand(n, generator=gen), 2.0 ** -10 * torch.rand(n, generator=gen)):
+            for kind in sample.CONFIDENCES:
+                run_rows(logits, u, params, kind, dev)
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_launch_takes(dev):
+    """Rows beyond those of the first launch, with parameters a row."""
+    rows = (1 << 23) + 700
+    logits = torch.zeros((rows, 2), dtype=torch.float32, device=dev)
+    logits[:, 1] = (torch.arange(rows, device=dev) % 3 - 1).float()
+    temperature = (torch.arange(rows, device=dev) % 2).float()
+    top_k = (torch.arange(rows, device=dev) % 5 == 0).int()
+    tokens, conf = sample.tokens(logits, torch.full((rows,), 0.999999, device=dev), temperature=temperature, top_k=top_k)
+    first = (logits[:, 1] > 0).int()
+    last = torch.where((temperature > 0) & (top_k == 0), 1 - first, first)
+    assert torch.equal(tokens, last)
+    e = torch.exp(-logits[:, 1].double().abs())
+    want = torch.where(top_k > 0, 1.0, torch.where(tokens == first, 1.0, e) / (1.0 + e))
+    assert (conf.double() - want).abs().max() <= 2.0 ** -19
 
 
 @pytest.mark.gpu
@@ -285,6 +332,117 @@ def test_streams_outputs_and_graphs(dev):
         b = sample.unmask(*a, ids0, indptr, mask_id=3001, count=2)
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(a + b, g + h))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_logits_next_to_zero(dev, dtype):
+    """Logits so near 0 that their weights are that of 0, as the largest, among others and around the last that is kept."""
+    gen = torch.Generator().manual_seed(22)
+    for scale, rest in ((1e-20, -1.0), (1e-20, 1.0), (1e-30, 0.0), (1e-12, -40.0), (1e-38, 1e-12)):
+        x = torch.full((6, 3001), rest) * (1 + torch.rand((6, 3001), generator=gen))
+        x[:, ::7] = scale * torch.randn((6, 429), generator=gen)
+        for params in (PARAMS[0], PARAMS[1], dict(temperature=0.9, top_k=200), dict(temperature=0.9, top_k=429), dict(temperature=30.0, top_p=0.1), dict(temperature=1e-15)):
+            for kind in sample.CONFIDENCES:
+                run_rows(x.to(DTYPES[dtype]), torch.rand(6, generator=gen), params, kind, dev)
+
+
+# rows that are split over work-groups (fewer than 256 of a long vocabulary), and rows of which a work-group takes a whole one
+LONG = 20011
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [0, 1, 2, 5, 9, 11])
+@pytest.mark.parametrize("how", ["peaked", "ties", "equal", "near", "zeros", "wide", "masked", "holes", "rising"])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_long_rows(dev, dtype, how, which):
+    gen = torch.Generator().manual_seed(71 + which)
+    for kind in sample.CONFIDENCES:
+        run_rows(make((6, LONG), how, DTYPES[dtype], gen), torch.rand(6, generator=gen), PARAMS[which], kind, dev)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", list(sample.CONFIDENCES))
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_rows_alone_and_among_many(dev, dtype, kind):
+    """255, 256 and 300 rows against the definition, here and there, and each against itself in a call of few rows."""
+    gen = torch.Generator().manual_seed(72)
+    logits = make((300, LONG), "normal", DTYPES[dtype], gen)
+    logits[7], logits[255] = -INF, math.nan
+    logits[11, 100], logits[256, :9000] = INF, -INF
+    u = torch.rand(300, generator=gen)
+    temperature = torch.where(torch.arange(300) % 3 == 0, 0.0, torch.rand(300, generator=gen) + 0.3)
+    top_k = torch.where(torch.arange(300) % 4 == 0, 0, torch.randint(1, 500, (300,), generator=gen)).int()
+    there = logits.to(dev)
+    at = torch.tensor([0, 3, 7, 11, 12, 100, 254, 255, 256, 299])
+    for params in (dict(temperature=temperature, top_k=top_k), dict(temperature=0.0), dict(temperature=0.8, top_p=0.9)):
+        of = lambda n: {k: v[n].to(dev) if torch.is_tensor(v) else v for k, v in params.items()}  # noqa: E731
+        few, few_conf = run_rows(logits[at], u[at], {k: v[at] if torch.is_tensor(v) else v for k, v in params.items()}, kind, dev)
+        for rows in (255, 256, 300):
+            tokens, conf = sample.tokens(there[:rows], u[:rows].to(dev), confidence=kind, **of(slice(rows)))
+            here = at < rows
+            for r, token, c in zip(at[here].tolist(), tokens.cpu()[at[here]], conf.cpu()[at[here]]):
+                one = {k: (v[r].item() if torch.is_tensor(v) else float(np.float32(v))) for k, v in params.items()}
+                check(logits[r].double().numpy(), int(token), float(c), float(u[r]), kind=kind, **one)
+            # (weights of bf16 rows are summed alike; places of others are whole numbers)
+            assert torch.equal(tokens[at[here].to(dev)], few[here.to(dev)])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_graphs_of_long_rows(dev, dtype):
+    """Two captured calls with parts of rows, replayed in turn and with eager calls between them."""
+    gen = torch.Generator().manual_seed(73)
+    x, y = (make((5, LONG), how, DTYPES[dtype], gen).to(dev) for how in ("peaked", "normal"))
+    u = torch.rand(5, generator=gen).to(dev)
+    greedy, drawn = dict(temperature=0.0, confidence="entropy"), dict(temperature=0.9, top_p=0.95, confidence="margin")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        sample.tokens(x, u, **greedy)
+        sample.tokens(y, u, **drawn)
+    torch.cuda.synchronize()
+    one, two = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(one):
+        a = sample.tokens(x, u, **greedy)
+    with torch.cuda.graph(two):
+        b = sample.tokens(y, u, **drawn)
+    for k in range(5):
+        u.copy_(torch.rand(5, generator=gen))
+        x.copy_(make((5, LONG), ("normal", "ties", "masked", "holes", "peaked")[k], DTYPES[dtype], gen))
+        y.copy_(make((5, LONG), ("near", "masked", "peaked", "equal", "holes")[k], DTYPES[dtype], gen))
+        one.replay()
+        two.replay()
+        want = sample.tokens(x, u, **greedy) + sample.tokens(y, u, **drawn)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(a + b, want))
+
+
+@pytest.mark.gpu
+def test_rows_past_32_bits(dev):
+    """Rows whose offsets in elements and bytes do not fit in 32 bits."""
+    stride = (1 << 31) + 13
+    gen = torch.Generator().manual_seed(74)
+    for vocab in (LONG, 999):
+        buffer = torch.empty(2 * stride + vocab, dtype=torch.bfloat16, device=dev)
+        view = torch.as_strided(buffer, (3, vocab), (stride, 1), 0)
+        view.copy_(make((3, vocab), "normal", torch.bfloat16, gen))
+        for params in (PARAMS[0], PARAMS[5]):
+            run_rows(view, torch.rand(3, generator=gen), params, "probability", dev)
+
+
+def test_workspace():
+    """Parts of rows need memory; too little of it, or at an odd address, is refused before any HIP call."""
+    lib, bytes_of = _lib.lib, _lib.lib.sangam_sample_workspace_bytes
+    assert bytes_of(4, 100, 0) == bytes_of(256, LONG, 0) == bytes_of(0, LONG, 0) == bytes_of(-1, LONG, 0) == bytes_of(4, LONG, 7) == bytes_of(4, 0, 0) == 0
+    assert bytes_of(4, 2 ** 18 + 1, 0) == bytes_of(2 ** 31, LONG, 0) == 0
+    for dtype in range(3):
+        need = bytes_of(4, LONG, dtype)
+        assert need > 0
+        desc = c_desc(vocab=LONG, row_stride=LONG, dtype=dtype)
+        assert lib.sangam_sample_tokens(ctypes.byref(desc), 4096, 4096, None, need, None) == -5
+        assert lib.sangam_sample_tokens(ctypes.byref(desc), 4096, 4096, 4096, need - 1, None) == -5
+        assert lib.sangam_sample_tokens(ctypes.byref(desc), 4096, 4096, 4096 + 128, need, None) == -6
 
 
 @pytest.mark.gpu
