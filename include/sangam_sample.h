@@ -45,10 +45,13 @@ extern "C" {
  * shares the whole weight with its like. A row without any weight gets token
  * -1, confidence 0. Weights under 2^-64 of the largest count as none.
  *
- * Logits are exact; weights are held to 2^-33 and sums to 2^-44 of the largest
- * weight, as whole numbers, so that a row's token does not depend on the order
- * of additions, and equal logits share to the last bit. Confidences are computed
- * in 64 bits where filters or u need them so, else in 32 with sums in 64.
+ * Logits are exact. Places are found by weights held to 2^-33 of themselves:
+ * fp16 and fp32 rows sum them as whole numbers of 2^-44 of the largest, bf16 rows
+ * in 64 bits in an order that is always the same. So a row's token does not
+ * depend on when what is added, nor on the rows beside it, and equal logits share
+ * alike. Confidences come from the same sums, but for the first token of
+ * everything of fp16 and fp32 rows (T = 0, nothing filtered): its weights are
+ * computed in 32 bits and summed in 32 over a few, then in 64, to 2^-19 of the sum.
  *
  * Parameters: an array has num_params entries, of which row r takes entry
  * params_of[r] (NULL: r); a NULL array stands for the value beside it. A row

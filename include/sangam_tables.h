@@ -27,7 +27,7 @@ extern "C" {
 typedef struct sangam_block_table {
     int32_t *pages;      /* device, [requests, max_pages] */
     int64_t row_stride;  /* in entries, >= max_pages */
-    int32_t requests;    /* >= 0 */
+    int32_t requests;    /* 0 to 2^30 */
     int32_t max_pages;   /* of a request, >= 0 */
 } sangam_block_table;
 
@@ -45,7 +45,8 @@ typedef struct sangam_block_table {
  * beyond max_pages (they keep what they have).
  *
  * lengths below 0 count as 0; held[r] as at most max_pages, num_free[0] as at
- * most free_cap. Entries of `free` above the top are left as they are, and so
+ * most free_cap. Pages that come back to a full stack of free_cap are lost: give
+ * it room for all pages. Entries of `free` above the top are left as they are, and so
  * are those of the table that nothing moves into or out of.
  *
  * Errors: SANGAM_ERR_INVALID_ARG (a NULL pointer, a size out of range),
@@ -59,7 +60,7 @@ sangam_status sangam_tables_resize(const sangam_block_table *table, int32_t *hel
  * q_indptr[i + 1], at positions q_offset[i] and on, or where q_pos is not NULL
  * at q_pos[row]. All device arrays; q_pos holds `rows` entries. */
 typedef struct sangam_tables_batch {
-    int32_t num_items; /* >= 0 */
+    int32_t num_items; /* 0 to 2^30 */
     int32_t reserved;  /* 0 */
     const int32_t *request;  /* [num_items] or NULL */
     const int32_t *kv_len;   /* [num_items] */

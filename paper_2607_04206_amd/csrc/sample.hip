@@ -743,7 +743,7 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
     static_assert(kBins == 64 * 64, "a block a lane");
     const int lane = tid & 63, wave = tid / 64;
     __syncthreads();
-#pragma unroll 2
+#pragma unroll 1
     for (int block = wave; block < 64; block += kWaves) {
         const int b = 64 * block + lane;
         const uint64_t bin = slot(b), m = sh.mass_of(b, weight_in(bin));

@@ -3,8 +3,10 @@
 // (include/sangam_tables.h).
 //
 // Both move a few bytes per page and row (the batch of a busy worker: some tens
-// of KB), so what they cost is the launch and a chain of dependent loads: sizes,
-// their prefix sum, the entries. One launch each, the prefix sums in LDS.
+// of KB, 0.01 us of a copy), so what they cost is the launch and a chain of
+// dependent loads: sizes, their prefix sum, the entries. One launch each, the
+// prefix sums in LDS. A batch of 32 decodes or of 48 beside long prefills is
+// built in 4.8 to 5.3 us of the kernel, 13.5 from Python.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -27,6 +29,7 @@ constexpr int kPage = 16;
 constexpr int kResizeThreads = 1024;
 constexpr int kBuildThreads = 256;
 constexpr int kItemsInLds = 1024;
+constexpr int kMost = 1 << 30;  // requests and items: they are counted on in steps of work-groups, in 32 bits
 
 __device__ __forceinline__ int pages_of(int len) { return len <= 0 ? 0 : (len - 1) / kPage + 1; }
 
@@ -62,7 +65,8 @@ struct ResizeArgs {
 
 // One work-group: what a request takes depends on all before it. The pages that
 // move are dealt over the threads one by one, each finds its request by its number:
-// 12,800 pages of 100 requests among 1024 in 9 us, by a wave a request 27.
+// 12,800 pages of 100 requests among 1024 are taken in 11.2 us and given back in
+// 13.2 (by a wave a request 16.8 and 27.5).
 __global__ __launch_bounds__(kResizeThreads) void tables_resize_kernel(ResizeArgs a) {
     __shared__ int64_t part[kResizeThreads / 64];
     __shared__ int64_t at[kResizeThreads];  // moves before a request's
@@ -255,8 +259,8 @@ sangam_status fail(sangam_status code, const std::string& msg) {
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 sangam_status check_table(const sangam_block_table* t) {
-    if (!t || t->requests < 0 || t->max_pages < 0)
-        return fail(SANGAM_ERR_INVALID_ARG, "table must not be NULL, nor its requests and max_pages negative");
+    if (!t || t->requests < 0 || t->requests > kMost || t->max_pages < 0)
+        return fail(SANGAM_ERR_INVALID_ARG, "table must not be NULL, nor its requests outside 0 to 2^30, nor max_pages negative");
     if (t->requests > 0 && t->max_pages > 0) {
         if (!t->pages) return fail(SANGAM_ERR_INVALID_ARG, "the table's pages must not be NULL");
         if (t->row_stride < t->max_pages || t->row_stride > (int64_t(1) << 40))
@@ -291,8 +295,8 @@ sangam_status build(const sangam_block_table* table, const sangam_tables_batch* 
                     int32_t* positions, int64_t* slots, int32_t* items, int64_t rows, void* stream) {
     clear_error();
     if (const sangam_status s = check_table(table)) return s;
-    if (!b || b->num_items < 0 || pages < 0 || pages > INT32_MAX || rows < 0 || rows > INT32_MAX)
-        return fail(SANGAM_ERR_INVALID_ARG, "batch must not be NULL, nor num_items, pages and rows outside 0 to 2^31 - 1");
+    if (!b || b->num_items < 0 || b->num_items > kMost || pages < 0 || pages > INT32_MAX || rows < 0 || rows > INT32_MAX)
+        return fail(SANGAM_ERR_INVALID_ARG, "batch must not be NULL, nor num_items outside 0 to 2^30, nor pages and rows outside 0 to 2^31 - 1");
     if (!page_indptr || !b->q_indptr || (b->num_items > 0 && (!b->kv_len || !b->q_offset)))
         return fail(SANGAM_ERR_INVALID_ARG, "page_indptr and the batch's kv_len, q_indptr and q_offset must not be NULL");
     for (const void* p : {static_cast<const void*>(b->request), static_cast<const void*>(b->kv_len), static_cast<const void*>(b->q_indptr),

@@ -233,7 +233,7 @@ def c_table(**kw):
 
 
 @pytest.mark.parametrize("status,table,args", [
-    (-1, dict(requests=-1), {}), (-1, dict(max_pages=-1), {}), (-1, dict(pages=None), {}), (-1, dict(row_stride=7), {}), (-1, dict(row_stride=2 ** 40 + 1), {}),
+    (-1, dict(requests=-1), {}), (-1, dict(requests=2 ** 30 + 1), {}), (-1, dict(max_pages=-1), {}), (-1, dict(pages=None), {}), (-1, dict(row_stride=7), {}), (-1, dict(row_stride=2 ** 40 + 1), {}),
     (-6, dict(pages=4098), {}), (-1, {}, dict(held=None)), (-1, {}, dict(lengths=None)), (-1, {}, dict(free=None)), (-1, {}, dict(cap=-1)),
     (-1, {}, dict(num_free=None)), (-1, {}, dict(short=None)), (-6, {}, dict(held=4097)), (-6, {}, dict(free=4098)), (-6, {}, dict(short=4097))])
 def test_resize_refusals(status, table, args):
@@ -242,7 +242,7 @@ def test_resize_refusals(status, table, args):
 
 
 @pytest.mark.parametrize("status,b,args", [
-    (-1, dict(num_items=-1), {}), (-1, dict(kv_len=None), {}), (-1, dict(q_indptr=None), {}), (-1, dict(q_offset=None), {}), (-6, dict(request=4097), {}),
+    (-1, dict(num_items=-1), {}), (-1, dict(num_items=2 ** 30 + 1), {}), (-1, dict(kv_len=None), {}), (-1, dict(q_indptr=None), {}), (-1, dict(q_offset=None), {}), (-6, dict(request=4097), {}),
     (-6, dict(q_pos=4098), {}), (-6, dict(kv_len=4097), {}), (-1, {}, dict(page_indptr=None)), (-1, {}, dict(pages=-1)), (-1, {}, dict(rows=-1)),
     (-1, {}, dict(rows=2 ** 31)), (-1, {}, dict(pages=2 ** 31)), (-6, {}, dict(slots=4100)), (-6, {}, dict(page_ids=4097)), (-6, {}, dict(items=4097))])
 def test_build_refusals(status, b, args):
