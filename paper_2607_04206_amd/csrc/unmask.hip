@@ -4,10 +4,12 @@
 // The `count` most confident candidates are those above a border key, and of
 // those equal to it the lowest rows. The border is found bit by bit: with the
 // confidences as whole numbers of their order, the largest key that at least
-// `count` of them reach. A block is a wave's, its keys in registers (up to 16 a
+// `count` of them reach. A block is a wave's, its keys in registers (up to 4 a
 // lane), a bit of the border one ballot a register; larger blocks are a
-// work-group's, by digits of 8 bits counted in LDS. A launch moves 16 bytes a
-// row and is bound by its own latency.
+// work-group's, by digits of 8 bits counted in LDS, up to 4096 rows with their
+// keys there, too. A launch moves 16 bytes a row and is bound by its own
+// latency: one block of 32 rows takes 2.8 us, 4096 of them 5.3, 64 of 256 rows
+// 5.4, 120 of 1024 8.0, 120 of 2048 11.4; 4097 rows 40.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -16,6 +18,7 @@
 
 #include "../../include/sangam_sample.h"
 #include "entry.h"
+#include "wave_sum.h"
 
 namespace sangam {
 void set_error(const std::string& msg);
@@ -28,7 +31,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kKeys = 16;  // of a lane: blocks of up to 1024 rows are a wave's
+constexpr int kKeys = 4;     // of a lane: blocks of up to 256 rows are a wave's (1024 take 15.1 us by a wave, 7.5 by a work-group)
+constexpr int kHeld = 4096;  // keys of a work-group: blocks of up to so many rows are looked at once
 
 struct UnmaskArgs {
     const int32_t* tokens;
@@ -42,6 +46,7 @@ struct UnmaskArgs {
     int32_t num_blocks, mask_id, count;
     float threshold;
     int32_t *out, *left;
+    int32_t each;  // blocks of a work-group, up to one a wave
 };
 
 // A row's id before the step, and where it lies (nullptr: nowhere to be written).
@@ -145,50 +150,125 @@ __device__ __forceinline__ void by_wave(const UnmaskArgs& a, int block, int64_t 
     if (a.left && lane == 0) a.left[block] = masked - taken;
 }
 
-// A block of any size, by a whole work-group.
-__device__ void by_group(const UnmaskArgs& a, int block, int64_t r0, int64_t n, int count, float threshold) {
-    __shared__ int bins[256], part[kWaves];
-    __shared__ uint32_t digit;
-    __shared__ int behind;
+struct Groups {
+    int bins[256];
+    int part[kWaves];
+    uint32_t key[kHeld];
+};
+
+// Sum over the work-group.
+__device__ __forceinline__ int sum_all(Groups& sh, int x) {
+    x = wave_up_to(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) sh.part[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) x += sh.part[w];
+    return x;
+}
+
+// The `count`-th largest key, and how many of those equal to it are among the `count` largest; each(f) calls f with every
+// key, 0 < count <= number of keys above 0. Every wave finds a digit by itself, a lane holding four bins from the top.
+template <typename F>
+__device__ __forceinline__ uint32_t border_of(Groups& sh, int count, int& ties, F each) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    uint32_t known = 0;
+    int wanted = count;  // among the keys that begin as the border does
+#pragma unroll 1
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        __syncthreads();
+        sh.bins[tid] = 0;
+        __syncthreads();
+        each([&](uint32_t key) {
+            if (key > 0 && (uint64_t(key) >> (shift + 8)) == (uint64_t(known) >> (shift + 8))) atomicAdd(&sh.bins[(key >> shift) & 255], 1);
+        });
+        __syncthreads();
+        int n[4], up_to = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) up_to += n[k] = sh.bins[255 - 4 * lane - k];
+        const int mine = up_to;
+        up_to = wave_up_to(up_to);
+        const uint64_t in = __ballot(up_to >= wanted);
+        const int at = in ? __builtin_ctzll(in) : 63;
+        int above = up_to - mine, digit = 255 - 4 * lane;
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (digit == 255 - 4 * lane - k && above + n[k] < wanted) {
+                above += n[k];
+                digit -= 1;
+            }
+        known |= uint32_t(__builtin_amdgcn_readlane(digit, at)) << shift;
+        wanted -= __builtin_amdgcn_readlane(above, at);
+    }
+    ties = wanted;
+    return known;
+}
+
+// A block of up to kHeld rows, by a whole work-group: a wave's rows follow one another. (Keys in registers take 104 of them and
+// spill the ballots of 16 a lane: 4096 blocks of 32 rows then take 11.2 us beside them.)
+__device__ __forceinline__ void by_group_held(Groups& sh, const UnmaskArgs& a, int block, int64_t r0, int n, int count, float threshold) {
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    const int first = (n + kThreads - 1) / kThreads * 64 * wave + lane, end = min(first - lane + (n + kThreads - 1) / kThreads * 64, n);
+    uint32_t sure = 0;
+    int candidates = 0, masked = 0;
+#pragma unroll 4
+    for (int i = first; i < end; i += 64) {
+        const Row x = row_at(a, r0 + i, threshold);
+        sh.key[i] = x.key;
+        sure = sure << 1 | uint32_t(x.sure);
+        candidates += x.key > 0;
+        masked += x.id == a.mask_id;
+    }
+    sure = __brev(sure) >> ((32 - (first < end ? (end - first + 63) / 64 : 0)) & 31);  // the first one's bit lowest again
+    candidates = sum_all(sh, candidates);
+    uint32_t border = count <= 0 ? 0xFFFFFFFFu : 1;
+    int ties = count <= 0 ? 0 : n;
+    if (count > 0 && count < candidates)
+        border = border_of(sh, count, ties, [&](auto f) {
+#pragma unroll 4
+            for (int i = first; i < end; i += 64) f(sh.key[i]);
+        });
+    // those equal to the border before this wave's
+    int own = 0;
+    for (int i = first; i < end; i += 64) own += border > 0 && sh.key[i] == border;
+    own = wave_up_to(own);
+    __syncthreads();
+    if (lane == 63) sh.part[wave] = own;
+    __syncthreads();
+    int equal = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+        if (w < wave) equal += sh.part[w];
+    for (int i0 = first - lane; i0 < end; i0 += 64) {
+        const int i = i0 + lane;
+        const uint32_t key = i < end ? sh.key[i] : 0;
+        const uint64_t same = __ballot(key > 0 && key == border);
+        const int mine = equal + ones(same & ((uint64_t(1) << lane) - 1));
+        equal += ones(same);
+        const bool takes = key > 0 && ((sure & 1) || key > border || (key == border && mine < ties));
+        sure >>= 1;
+        masked -= takes;
+        if (i < end) put(a, r0 + i, takes);
+    }
+    masked = sum_all(sh, masked);
+    if (a.left && threadIdx.x == 0) a.left[block] = masked;
+}
+
+// A block of any size, by a whole work-group, which looks at it six times.
+__device__ __forceinline__ void by_group(Groups& sh, const UnmaskArgs& a, int block, int64_t r0, int64_t n, int count, float threshold) {
     const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
-    uint32_t border = 1;
-    int64_t ties = n;
     int candidates = 0;
     for (int64_t i = tid; i < n; i += kThreads) candidates += row_at(a, r0 + i, threshold).key > 0;
-    // (a wave's sum, then the work-group's)
-    for (int d = 32; d > 0; d /= 2) candidates += __shfl_xor(candidates, d);
-    __syncthreads();
-    if (lane == 0) part[wave] = candidates;
-    __syncthreads();
-    candidates = 0;
-    for (int w = 0; w < kWaves; ++w) candidates += part[w];
-    if (count <= 0) {
-        border = 0xFFFFFFFFu;
-        ties = 0;
-    } else if (count < candidates) {
-        uint32_t known = 0;
-        int wanted = count;  // among the keys that begin as the border does
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            bins[tid] = 0;
-            __syncthreads();
-            for (int64_t i = tid; i < n; i += kThreads) {
-                const uint32_t key = row_at(a, r0 + i, threshold).key;
-                if (key > 0 && (uint64_t(key) >> (shift + 8)) == (uint64_t(known) >> (shift + 8))) atomicAdd(&bins[(key >> shift) & 255], 1);
-            }
-            __syncthreads();
-            if (tid == 0) {
-                int d = 255, above = 0;
-                while (d > 0 && above + bins[d] < wanted) above += bins[d--];
-                digit = uint32_t(d);
-                behind = wanted - above;
-            }
-            __syncthreads();
-            known |= digit << shift;
-            wanted = behind;
-            __syncthreads();
-        }
-        border = known;
-        ties = wanted;
+    candidates = sum_all(sh, candidates);
+    uint32_t border = count <= 0 ? 0xFFFFFFFFu : 1;
+    int64_t ties = count <= 0 ? 0 : n;
+    if (count > 0 && count < candidates) {
+        int among = 0;
+        border = border_of(sh, count, among, [&](auto f) {
+            for (int64_t i = tid; i < n; i += kThreads) f(row_at(a, r0 + i, threshold).key);
+        });
+        ties = among;
     }
     // rows in order, so that the lowest of equal ones are taken
     int64_t equal = 0;
@@ -199,12 +279,12 @@ __device__ void by_group(const UnmaskArgs& a, int block, int64_t r0, int64_t n, 
         if (i < n) x = row_at(a, r0 + i, threshold);
         const uint64_t same = __ballot(x.key > 0 && x.key == border);
         __syncthreads();
-        if (lane == 0) part[wave] = ones(same);
+        if (lane == 0) sh.part[wave] = ones(same);
         __syncthreads();
         int64_t mine = equal + ones(same & ((uint64_t(1) << lane) - 1));
         for (int w = 0; w < kWaves; ++w) {
-            if (w < wave) mine += part[w];
-            equal += part[w];
+            if (w < wave) mine += sh.part[w];
+            equal += sh.part[w];
         }
         const bool takes = x.key > 0 && (x.sure || x.key > border || (x.key == border && mine < ties));
         if (i < n) {
@@ -212,19 +292,14 @@ __device__ void by_group(const UnmaskArgs& a, int block, int64_t r0, int64_t n, 
             masked += x.id == a.mask_id && !takes;
         }
     }
-    for (int d = 32; d > 0; d /= 2) masked += __shfl_xor(masked, d);
-    __syncthreads();
-    if (lane == 0) part[wave] = masked;
-    __syncthreads();
-    if (a.left && tid == 0) {
-        for (int w = 1; w < kWaves; ++w) masked += part[w];
-        a.left[block] = masked;
-    }
+    masked = sum_all(sh, masked);
+    if (a.left && tid == 0) a.left[block] = masked;
 }
 
-// Work-group g: blocks kWaves g to kWaves g + 3, a wave each, then those of them
-// that are larger; the rows outside all blocks are dealt over the work-groups.
+// Work-group g: blocks each g and on, a wave each, then those of them that are
+// larger; the rows outside all blocks are dealt over the work-groups.
 __global__ __launch_bounds__(kThreads) void unmask_kernel(UnmaskArgs a) {
+    __shared__ Groups sh;
     const int wave = threadIdx.x / 64;
     auto block_at = [&](int b, int64_t& r0, int64_t& n) {
         r0 = min(max(int64_t(a.row_indptr[b]), int64_t(0)), a.rows);
@@ -233,24 +308,24 @@ __global__ __launch_bounds__(kThreads) void unmask_kernel(UnmaskArgs a) {
     auto count_of = [&](int b) { return a.counts ? a.counts[b] : a.count; };
     auto threshold_of = [&](int b) { return a.thresholds ? a.thresholds[b] : a.threshold; };
     bool large = false;
-    for (int w = 0; w < kWaves; ++w) {
-        const int b = blockIdx.x * kWaves + w;
+    for (int w = 0; w < a.each; ++w) {
+        const int b = blockIdx.x * a.each + w;
         if (b >= a.num_blocks) break;
         int64_t r0, n;
         block_at(b, r0, n);
         if (n > 64 * kKeys) large = true;
         else if (w != wave) continue;
         else if (n <= 64) by_wave<1>(a, b, r0, int(n), count_of(b), threshold_of(b));
-        else if (n <= 256) by_wave<4>(a, b, r0, int(n), count_of(b), threshold_of(b));
         else by_wave<kKeys>(a, b, r0, int(n), count_of(b), threshold_of(b));
     }
     if (large)
-        for (int w = 0; w < kWaves; ++w) {
-            const int b = blockIdx.x * kWaves + w;
+        for (int w = 0; w < a.each; ++w) {
+            const int b = blockIdx.x * a.each + w;
             if (b >= a.num_blocks) break;
             int64_t r0, n;
             block_at(b, r0, n);
-            if (n > 64 * kKeys) by_group(a, b, r0, n, count_of(b), threshold_of(b));
+            if (n > 64 * kKeys && n <= kHeld) by_group_held(sh, a, b, r0, int(n), count_of(b), threshold_of(b));
+            if (n > kHeld) by_group(sh, a, b, r0, n, count_of(b), threshold_of(b));
         }
     const int64_t before = min(max(int64_t(a.row_indptr[0]), int64_t(0)), a.rows);
     const int64_t behind = max(min(max(int64_t(a.row_indptr[a.num_blocks]), int64_t(0)), a.rows), before);
@@ -283,10 +358,12 @@ sangam_status unmask(const sangam_unmask_desc* d, int32_t* out, int32_t* left, v
         if (reinterpret_cast<uintptr_t>(p) % 4) return fail(SANGAM_ERR_ALIGN, "the arrays must be 4-byte aligned");
     if (reinterpret_cast<uintptr_t>(d->slots) % 8) return fail(SANGAM_ERR_ALIGN, "slots must be 8-byte aligned");
     if (d->rows == 0 && (d->num_blocks == 0 || !left)) return SANGAM_OK;
+    // blocks of over 128 rows on average have a work-group to themselves, so that large ones do not wait for one another
+    const int32_t each = d->rows > int64_t(d->num_blocks) * (kThreads / 2) ? 1 : kWaves;
     UnmaskArgs args{d->tokens, d->confidence, d->ids, d->slots, d->row_indptr, d->counts, d->thresholds, d->rows, d->num_ids,
-                    d->num_blocks, d->mask_id, d->count, d->threshold, out, left};
+                    d->num_blocks, d->mask_id, d->count, d->threshold, out, left, each};
     void* kargs[] = {&args};
-    const int64_t groups = std::max<int64_t>((int64_t(d->num_blocks) + kWaves - 1) / kWaves, std::min<int64_t>((d->rows + kThreads - 1) / kThreads, 64));
+    const int64_t groups = std::max<int64_t>((int64_t(d->num_blocks) + args.each - 1) / args.each, std::min<int64_t>((d->rows + kThreads - 1) / kThreads, 64));
     if (groups > (int64_t(1) << 24) - 1) return fail(SANGAM_ERR_INVALID_ARG, "too many blocks");
     const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&unmask_kernel), dim3(unsigned(std::max<int64_t>(groups, 1))), dim3(kThreads), kargs, 0,
                                          static_cast<hipStream_t>(stream));

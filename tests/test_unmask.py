@@ -54,7 +54,7 @@ def put(dev, *arrays):
 
 
 SIZES = {"one": [1], "block": [32], "wave": [64, 65, 63, 0, 1, 128], "many": [32] * 301, "ragged": [0, 5, 0, 0, 100, 1, 31, 700, 64, 2], "limit": [1024, 1025, 3],
-         "large": [5000, 32, 2049, 0, 1030]}
+         "large": [5000, 32, 2049, 0, 1030], "held": [4096, 4097, 0, 2048, 1025, 1, 4095, 257], "spread": [1100, 1536, 700, 1, 0] * 5}
 
 
 @pytest.mark.gpu
