@@ -818,9 +818,9 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
         } else if (stage == kDraw) {
             const uint64_t M = scalar(kept.all(sh));
             unit = scalar(0x1p44 / double(M));
-            target = scalar(fmin(!greedy && p.u > 0.0f ? double(p.u) * double(M) : 0.0, double(M - 1)));
+            target = scalar(!greedy && p.u > 0.0f ? fmin(double(p.u), 1.0) * double(M) : 0.0);
             by = By::kAbove;
-            reach = uint64_t(target) + 1;
+            reach = scalar(min(uint64_t(target) + 1, M));  // (the sums of long flat rows are beyond 2^53: a target may round up to M)
         } else {
             if (a.confidence != SANGAM_CONFIDENCE_MARGIN || kept.before + kept.tokens < 2) continue;
             reach = 2;
@@ -840,7 +840,10 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
         if (q.bin > kept.bin) continue;  // (not met within what is kept)
         const double into = by == By::kReach || by == By::kAbove ? scalar(fmax(0.0, sh.inside(q.bin, target - double(q.mass)))) : 0.0;
         int index = -1;
-        if (n > 0) index = bin.first(q, n, by, int(reach) - q.before, into, cut_key, q.bin == kept.bin ? kept.tokens : n);
+        // (a draw at the end of what is kept of this bin is given by the number of its tokens, or it would fall on the one behind)
+        const bool at_end = stage == kDraw && q.bin == kept.bin && into >= double(kept.weight);
+        if (n > 0)
+            index = bin.first(q, n, at_end ? By::kCount : by, at_end ? kept.tokens : int(reach) - q.before, into, cut_key, q.bin == kept.bin ? kept.tokens : n);
         if (stage <= kMinP) {
             if (q.bin < kept.bin || q.tokens < kept.tokens) kept = q;
         } else if (stage == kDraw) {
@@ -1028,7 +1031,8 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
     const int tokens_end = wave_up_to(block_tokens) + (lane >= 32 ? tiny : 0);
     const double mass_end = wave_up_to(block_mass) + (lane >= 32 ? tiny_mass : 0.0);
     const int tokens_start = tokens_end - block_tokens;
-    const double mass_start = lane == 0 ? 0.0 : __shfl_up(mass_end, 1) + (lane == 32 ? tiny_mass : 0.0);
+    const double mass_before = __shfl_up(mass_end, 1);  // (by all lanes: the second one's comes from the first)
+    const double mass_start = lane == 0 ? 0.0 : mass_before + (lane == 32 ? tiny_mass : 0.0);
     const int all_tokens = lane_of(tokens_end, 63);
     const double all_mass = lane_of(mass_end, 63);
     // (what the tiny ones weigh may be off by 2^-24 of it)

@@ -209,6 +209,27 @@ def test_ends_of_the_uniform_numbers(dev, dtype, vocab, filters):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows", [5, 256])
+@pytest.mark.parametrize("how", ["equal", "near", "zeros"])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_last_token_of_flat_rows(dev, dtype, how, rows):
+    """Draws at the end of long rows whose weights are beyond 2^53 in units of 2^-44."""
+    gen = torch.Generator().manual_seed(24)
+    logits = make((5, 50257), how, DTYPES[dtype], gen)
+    u = torch.tensor([1.0, 1.0 - 2.0 ** -24, INF, 2.0, 0.9999])
+    for params in (dict(temperature=1.0), dict(temperature=2.0, top_k=30000), dict(temperature=1.0, top_p=0.9), dict(temperature=1.0, min_p=0.9)):
+        tokens, _ = sample.tokens(logits.to(dev).repeat(rows // 5 + 1, 1)[:rows], u.to(dev).repeat(rows // 5 + 1)[:rows], **params)
+        for r in range(5):
+            order, w, _ = ranked(logits[r].double().numpy(), params["temperature"], **{k: v if k == "top_k" else float(np.float32(v)) for k, v in params.items() if k != "temperature"})
+            place, last = int(np.flatnonzero(order == int(tokens[r]))[0]), int((w > 0).sum()) - 1
+            if r in (0, 2, 3):
+                assert place == last
+            else:  # (weights are held to 2^-33 of themselves)
+                assert 0 <= place <= last and abs(w[:place + 1].sum() - float(u[r]) * w.sum()) <= w[place] + 1e-9 * w.sum()
+        assert (tokens.view(-1)[:5] == tokens[rows // 5 * 5 - 5:rows // 5 * 5]).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", list(DTYPES))
 def test_halves_to_the_last_bit(dev, dtype):
     # six equal tokens, u M = 3 exactly
@@ -345,6 +366,22 @@ def test_logits_next_to_zero(dev, dtype):
         for params in (PARAMS[0], PARAMS[1], dict(temperature=0.9, top_k=200), dict(temperature=0.9, top_k=429), dict(temperature=30.0, top_p=0.1), dict(temperature=1e-15)):
             for kind in sample.CONFIDENCES:
                 run_rows(x.to(DTYPES[dtype]), torch.rand(6, generator=gen), params, kind, dev)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", list(sample.CONFIDENCES))
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_powers_of_two_among_the_largest(dev, dtype, kind):
+    """The largest logits on both sides of each power of two, where the sums of bf16's values begin anew."""
+    gen = torch.Generator().manual_seed(25)
+    for high in (256.0, 128.0, 64.0, 2.0, 0.5, 2.0 ** -10, -2.0 ** -10, -1.0, -64.0, -128.0):
+        x = high * (1 + 0.03 * torch.rand((5, 1111), generator=gen))
+        x[:, ::3] = high * (1 - 0.02 * torch.rand((5, 371), generator=gen))
+        x[0, 5:] = high * 0.98
+        x[1, 5:] = -300.0
+        for params in (dict(temperature=0.0, top_k=2), dict(temperature=1.0, top_k=17), dict(temperature=1.0, min_p=1e-5), dict(temperature=0.5 * abs(high), top_p=0.6),
+                       dict(temperature=3.0, top_k=134, min_p=0.006), dict(temperature=1.0)):
+            run_rows(x.to(DTYPES[dtype]), torch.rand(5, generator=gen), params, kind, dev)
 
 
 # rows that are split over work-groups (fewer than 256 of a long vocabulary), and rows of which a work-group takes a whole one
