@@ -43,7 +43,8 @@ extern "C" {
  *
  * A logit that is -inf or no number has no weight and is never taken; +inf
  * shares the whole weight with its like. A row without any weight gets token
- * -1, confidence 0. Weights under 2^-64 of the largest count as none.
+ * -1, confidence 0. Weights under 2^-64 of the largest count as none; of fp16 and
+ * fp32 rows, those up to 2^-63.9 of it may.
  *
  * Logits are exact. Places are found by weights held to 2^-33 of themselves:
  * fp16 and fp32 rows sum them as whole numbers of 2^-44 of the largest, bf16 rows

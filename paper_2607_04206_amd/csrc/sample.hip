@@ -818,9 +818,13 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
         } else if (stage == kDraw) {
             const uint64_t M = scalar(kept.all(sh));
             unit = scalar(0x1p44 / double(M));
-            target = scalar(!greedy && p.u > 0.0f ? fmin(double(p.u), 1.0) * double(M) : 0.0);
-            by = By::kAbove;
-            reach = scalar(min(uint64_t(target) + 1, M));  // (the sums of long flat rows are beyond 2^53: a target may round up to M)
+            if (!greedy && p.u >= 1.0f) {  // the last that is kept, by its number: M may be reached before it, by less than a unit of 2^-44
+                reach = uint64_t(kept.before + kept.tokens);
+            } else {
+                target = scalar(!greedy && p.u > 0.0f ? double(p.u) * double(M) : 0.0);
+                by = By::kAbove;
+                reach = scalar(min(uint64_t(target) + 1, M));  // (the sums of long flat rows are beyond 2^53: a target may round up to M)
+            }
         } else {
             if (a.confidence != SANGAM_CONFIDENCE_MARGIN || kept.before + kept.tokens < 2) continue;
             reach = 2;
@@ -1076,8 +1080,22 @@ __device__ __forceinline__ bool choose_by_value(Shared<E>& sh, Row<__bf16, E>& r
                     weight = 1.0;
                     continue;
                 }
-                reach = scalar(p.u > 0.0f ? fmin(double(p.u), 1.0) * M : 0.0);
-                by = p.u < 1.0f || !(p.u == p.u) ? By::kAbove : By::kReach;  // (from 1 on the last of any weight)
+                if (p.u >= 1.0f) {
+                    // the last that is kept and has any weight, by its number: sums may not tell it from those before. Values with
+                    // a weight come first: whole blocks of them, then some of a block
+                    auto weighs = [&](int q) { return t_of(value_at(q)) < double(kBins); };
+                    const int blocks = __builtin_popcountll(__ballot(weighs(kBlock * lane + kBlock - 1)));
+                    int tokens = all_tokens;
+                    if (blocks < 64) {
+                        const int q = kBlock * blocks + lane;
+                        const int more = wave_up_to((weighs(q) ? count_at(sh, q) : 0) + (weighs(q + 64) ? count_at(sh, q + 64) : 0));
+                        tokens = lane_of(tokens_start, blocks) + lane_of(more, 63);
+                    }
+                    reach = double(min(tokens, kept.before + kept.tokens));
+                } else {
+                    reach = scalar(p.u > 0.0f ? double(p.u) * M : 0.0);
+                    by = By::kAbove;
+                }
             }
         } else if (stage == kMinP) {
             if (!(p.min_p > 0.0f)) continue;

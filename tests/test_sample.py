@@ -468,6 +468,52 @@ def test_rows_past_32_bits(dev):
             run_rows(view, torch.rand(3, generator=gen), params, "probability", dev)
 
 
+# ------------------------------------------------------------------ far tails
+def tails(vocab, T, others):
+    """Rows whose last tokens of any weight are some tens of powers of two under the largest, in any dtype, and none within 0.2 of
+    the 64th. All others have no weight: they are masked, or 69 powers of two under the largest."""
+    fixed = [[30.0] + [-10.0] * 5,                                  # 2^-57.7
+             [30.0, 29.0, 29.0, 3.0] + [-8.0] * 700 + [-12.0] * 3,  # 2^-54.8, more equal ones than are sorted, 2^-60.6
+             [30.0, 12.0] + [-13.0] * 600,                          # 2^-62.0
+             [40.0, 39.0] + [0.0, -0.0] * 30,                       # 2^-57.7
+             [42.0, 7.0, 0.0, 0.0, -0.5, -0.5, -2.0],               # 2^-60.6, -61.3, -63.5
+             [300.0, 290.0, 258.0, 258.0, 268.0],                   # 2^-60.6, beyond what bf16 counts
+             [-2.0] * 9 + [-40.0] * 2 + [-45.0],                    # 2^-54.8, -62.0
+             [20.0] * 40 + [-4.5, -5.0, -20.0]]                     # 2^-35.3, -36.1, -57.7
+    gen = torch.Generator().manual_seed(vocab)
+    x = torch.empty((len(fixed), vocab))
+    for r, values in enumerate(fixed):
+        x[r] = -INF if others == "masked" else (values[0] - 48.0) * T
+        x[r, torch.randperm(vocab, generator=gen)[:len(values)]] = torch.tensor(values) * T
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("others", ["masked", "weightless"])
+@pytest.mark.parametrize("rows,vocab", [(8, 1500), (8, 20011), (264, 20011)])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_last_token_of_any_weight(dev, dtype, rows, vocab, others):
+    """u from 1 on takes the last kept token of any weight (2^-64 of the largest at least), also where it is under what sums
+    hold. Confidences: one rounding to 32 bits, and 2^-33 of the weight and of the sum."""
+    for T in (1.0, 0.5, 4.0):
+        x = tails(vocab, T, others).to(DTYPES[dtype])
+        n = x.shape[0]
+        u = torch.tensor([1.0, 2.0, INF, 1.0, 1.0, 3.0, 1.0, 1.0])
+        for params in (dict(), dict(top_k=vocab - 1), dict(top_k=300), dict(top_k=6), dict(top_k=2), dict(min_p=1e-18), dict(min_p=1e-30), dict(top_p=1.0 - 2.0 ** -24),
+                       dict(top_k=700, min_p=1e-17, top_p=0.99)):
+            tokens, conf = sample.tokens(x.to(dev).repeat(rows // n, 1), u.to(dev).repeat(rows // n), temperature=T, **params)
+            tokens, conf = tokens.cpu().view(-1, n), conf.cpu().view(-1, n)
+            assert (tokens == tokens[0]).all() and (conf == conf[0]).all()
+            for r in range(n):
+                order, w, z = ranked(x[r].double().numpy(), T, **{k: v if k == "top_k" else float(np.float32(v)) for k, v in params.items()})
+                bits = z / math.log(2.0)
+                assert not ((w > 0) & (abs(bits + 64) < 0.2)).any()
+                last = int(((w > 0) & (bits > -64)).sum()) - 1
+                assert int(tokens[0, r]) == order[last], (T, params, r)
+                ref = w[last] / w.sum()
+                assert abs(float(conf[0, r]) - ref) <= (2.0 ** -24 * (1 + 2.0 ** -6) + 2.0 ** -32) * ref, (T, params, r)
+
+
 def test_workspace():
     """Parts of rows need memory; too little of it, or at an odd address, is refused before any HIP call."""
     lib, bytes_of = _lib.lib, _lib.lib.sangam_sample_workspace_bytes
