@@ -773,7 +773,7 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
     if (p.min_p > 0.0f && p.min_p <= 1.0f) {
         const double T_ = greedy ? 1.0 : double(p.temperature), low = log(double(p.min_p));
         auto keeps = [&](float x) { return (double(x) - double(top)) / T_ >= low; };
-        float cut = float(fmax(double(top) + T_ * low, -3.4e38));
+        float cut = float(fmax(double(top) + T_ * low, -0x1.fffffep127));  // (the lowest number has weight, too, under a large T)
 #pragma unroll 1
         for (int k = 0; k < 4 && !keeps(cut); ++k) cut = nextafterf(cut, INFINITY);
 #pragma unroll 1

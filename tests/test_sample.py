@@ -514,6 +514,27 @@ def test_last_token_of_any_weight(dev, dtype, rows, vocab, others):
                 assert abs(float(conf[0, r]) - ref) <= (2.0 ** -24 * (1 + 2.0 ** -6) + 2.0 ** -32) * ref, (T, params, r)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [6, 260])
+def test_lowest_numbers_under_large_temperatures(dev, rows):
+    """Logits of the type's lowest value have weight, and min-p keeps them, where the temperature is that large."""
+    gen = torch.Generator().manual_seed(26)
+    for dtype in DTYPES.values():
+        x = torch.randn((rows, 20011), generator=gen).to(dtype)
+        x[:, ::3] = torch.finfo(dtype).min
+        x[0, 1:] = torch.finfo(dtype).min
+        x[1, 7] = torch.finfo(dtype).max
+        u = torch.rand(rows, generator=gen)
+        u[2:4] = torch.tensor([1.0, 1.0 - 2.0 ** -24])
+        for T in (INF, 1e38, 3e38):
+            for params in (dict(min_p=0.5), dict(min_p=0.02), dict(min_p=0.02, top_k=15000), dict(top_p=0.9, min_p=1e-4), dict()):
+                for kind in sample.CONFIDENCES:
+                    there, of = x.to(dev), dict(temperature=T, **params)
+                    tokens, conf = sample.tokens(there, u.to(dev), confidence=kind, **of)
+                    for r in range(6):
+                        check(x[r].double().numpy(), int(tokens[r]), float(conf[r]), float(u[r]), kind=kind, **{k: v if k == "top_k" else float(np.float32(v)) for k, v in of.items()})
+
+
 def test_workspace():
     """Parts of rows need memory; too little of it, or at an odd address, is refused before any HIP call."""
     lib, bytes_of = _lib.lib, _lib.lib.sangam_sample_workspace_bytes
