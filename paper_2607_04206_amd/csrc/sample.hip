@@ -30,6 +30,7 @@
 
 #include "../../include/sangam_sample.h"
 #include "entry.h"
+#include "exact_sum.h"
 #include "wave_sum.h"
 
 namespace sangam {
@@ -861,13 +862,15 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
     if (a.confidence == SANGAM_CONFIDENCE_MARGIN) {
         c = (double(top_weight) * 0x1p-33 - second) * unit;
     } else if (a.confidence == SANGAM_CONFIDENCE_ENTROPY) {
-        double s = 0.0, none = 0.0;
+        ExactSum sum{};  // (which thread gets which logits hangs on the order of LDS atomics)
         auto part = [&](double t) { return sh.bin_weight(int(t)) * double(kOne - miss_at(t - int(t))) * 0x1p-33 * t; };
         row.each_within(sh, row.lowest(min(kept.bin + 1, kBins)), INFINITY, [&](int, float x) {
             const double t = bin.place(x, 0);
-            if (t < double(kept.bin) || (kept.tokens > 0 && t < double(kept.bin + 1) && key_of(x) < kept.key)) s += part(t);
+            if (t < double(kept.bin) || (kept.tokens > 0 && t < double(kept.bin + 1) && key_of(x) < kept.key)) sum.add(part(t));  // (under 34)
         });
-        sum_all(sh, s, none);
+        uint64_t before[2], all[2];
+        sums_before(sh, sum.high, sum.low, before, all);
+        double s = ExactSum{all[0], all[1]}.value();
         if (kept.tokens > 0 && kept.ties > 0) s += kept.ties * part(bin.place(logit_of(kept.key), 0));
         c = -(s * unit * (0.69314718055994530942 / 64) - log(unit));
     }

@@ -4,6 +4,9 @@ ties, masked and infinite logits, odd sizes and strides, parameters a row or a
 request, refusals."""
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -533,6 +536,47 @@ def test_lowest_numbers_under_large_temperatures(dev, rows):
                     tokens, conf = sample.tokens(there, u.to(dev), confidence=kind, **of)
                     for r in range(6):
                         check(x[r].double().numpy(), int(tokens[r]), float(conf[r]), float(u[r]), kind=kind, **{k: v if k == "top_k" else float(np.float32(v)) for k, v in of.items()})
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_entropies_in_any_order(dev, dtype):
+    """The entropy of what is kept is the same to the last bit every time, in few and in many rows, and for every order of the
+    row's tokens: which thread adds what changes nothing."""
+    gen = torch.Generator().manual_seed(27)
+    for how in ("normal", "peaked", "rising", "near", "holes"):
+        x = make((9, LONG), how, DTYPES[dtype], gen).to(dev)
+        u = torch.rand(9, generator=gen).to(dev)
+        for params in (dict(temperature=1.0), dict(temperature=0.7, top_k=2000), dict(temperature=1.2, top_p=0.9), dict(temperature=0.0, min_p=1e-4)):
+            one = lambda t, n=1: sample.tokens(t.repeat(n, 1), u.repeat(n), confidence="entropy", **params)[1]  # noqa: E731
+            want = one(x)
+            for _ in range(5):
+                assert torch.equal(one(x), want)
+                assert torch.equal(one(x[:, torch.randperm(LONG, generator=gen).to(dev)]), want)
+            assert torch.equal(one(x, 30).view(30, 9), want.expand(30, 9))
+
+
+def test_exact_sums(tmp_path):
+    """The sum that these entropies take, on the host: the same bits in every order, of up to 2^18 numbers, each added to 2^-84."""
+    if not shutil.which("g++"):
+        pytest.skip("needs g++")
+    exe = str(tmp_path / "driver")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-fsanitize=undefined", "-fno-sanitize-recover=all",
+                    os.path.join(os.path.dirname(os.path.abspath(__file__)), "sanitize", "exact_sum_driver.cpp"), "-o", exe], check=True)
+    rng = np.random.default_rng(6)
+    cases = [rng.random(1000), 34 * 2.0 ** -rng.uniform(0, 66, 5000), np.full(1 << 18, 34.0), np.full(1 << 18, np.nextafter(64.0, 0.0)), 2.0 ** -rng.uniform(30, 90, 3000),
+             np.array([0.0, 2.0 ** -38, 1.5 * 2.0 ** -38, 2.0 ** -39, 33.999]), np.zeros(0)]
+    for x in cases:
+        text, orders = "", 3 if len(x) < 10000 else 1
+        for k in range(orders):
+            text += " ".join([str(len(x))] + [float(v).hex() for v in (rng.permutation(x) if k else x)]) + "\n"
+        out = [line.split() for line in subprocess.run([exe], input=text, capture_output=True, text=True, check=True).stdout.splitlines()]
+        assert len(out) == orders and all(o == out[0] for o in out)
+        want = math.fsum(x)
+        assert abs(float.fromhex(out[0][2]) - want) <= len(x) * 2.0 ** -84 + 2.0 ** -52 * want
+    # a sum of doubles does hang on the order
+    x = cases[1]
+    assert len({float(np.cumsum(rng.permutation(x))[-1]) for _ in range(20)}) > 1
 
 
 def test_workspace():
