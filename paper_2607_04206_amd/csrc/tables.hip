@@ -14,6 +14,7 @@
 
 #include "../../include/sangam_tables.h"
 #include "entry.h"
+#include "offsets.h"
 #include "wave_sum.h"
 
 namespace sangam {
@@ -171,17 +172,6 @@ struct BuildArgs {
     int64_t rows;
 };
 
-// The last of n + 1 offsets (not decreasing) that is at most x; -1: none.
-__device__ __forceinline__ int find(const int32_t* indptr, int n, int64_t x) {
-    int lo = -1, hi = n + 1;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (indptr[mid] <= x) lo = mid;
-        else hi = mid;
-    }
-    return lo;
-}
-
 // Offsets of the items' pages into out[0, items]; a whole work-group.
 __device__ void page_offsets(const BuildArgs& a, int32_t* out, int64_t* part) {
     int64_t before = 0, total;
@@ -223,7 +213,7 @@ __global__ __launch_bounds__(kBuildThreads) void tables_build_kernel(BuildArgs a
     const int64_t step = int64_t(gridDim.x) * kBuildThreads, t0 = int64_t(blockIdx.x) * kBuildThreads + threadIdx.x;
     if (a.page_ids)
         for (int64_t k = t0; k < a.num_pages; k += step) {
-            const int i = find(indptr, a.items, k);
+            const int i = last_offset(indptr, a.items, k);
             int page = -1;
             if (i >= 0 && i < a.items) {
                 const int32_t* row = row_of(i);
@@ -233,7 +223,7 @@ __global__ __launch_bounds__(kBuildThreads) void tables_build_kernel(BuildArgs a
             a.page_ids[k] = page;
         }
     for (int64_t r = t0; r < a.rows; r += step) {
-        const int i = find(q_indptr, a.items, r);
+        const int i = last_offset(q_indptr, a.items, r);
         const bool in = i >= 0 && i < a.items;
         int pos = 0;
         int64_t slot = -1;

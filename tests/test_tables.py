@@ -2,6 +2,9 @@
 host lists: requests that grow and shrink over a stack of free pages, and the
 page list, positions, slots and items of a batch. Whole numbers: all equal."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -222,6 +225,19 @@ def test_streams_and_graphs(dev):
         b = dict(request=np.arange(8), kv_len=n[:8], q_indptr=np.arange(9) * 4, q_offset=np.zeros(8, np.int64), rows=40, pages=100, q_pos=None)
         want = expected(t[1].cpu().numpy(), b)
         assert [x.tolist() for x in (out.page_indptr, out.page_ids, out.positions, out.slots, out.items)] == [list(x) for x in want]
+
+
+def test_places_among_many_offsets(tmp_path):
+    """The search among the offsets of as many items as a batch may have, and of a few, on the host and without overflow."""
+    if not shutil.which("g++"):
+        pytest.skip("needs g++")
+    exe = str(tmp_path / "driver")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-fsanitize=undefined", "-fno-sanitize-recover=all",
+                    os.path.join(os.path.dirname(os.path.abspath(__file__)), "sanitize", "offsets_driver.cpp"), "-o", exe], check=True)
+    asked = [(n, x) for n in (1, 2, 7, 1000, 2 ** 30 - 1, 2 ** 30, 2 ** 31 - 2) for x in (-1, 0, 4, 5, 2 ** 40)]
+    r = subprocess.run([exe], input="".join(f"{n} {x}\n" for n, x in asked), capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, r.stderr
+    assert [int(v) for v in r.stdout.split()] == [-1 if x < 0 else n - 1 if x < 5 else n for n, x in asked]
 
 
 # ------------------------------------------------------------------ refusals
