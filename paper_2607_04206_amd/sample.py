@@ -13,7 +13,7 @@ import torch
 from ._lib import SampleDesc, UnmaskDesc, lib
 from .kvq import _launch, _new, _stream
 from .rope import DTYPES
-from .tables import _ints
+from .tables import MOST, _ints
 
 CONFIDENCES = {"probability": 0, "margin": 1, "entropy": 2}
 MAX_VOCAB = 1 << 18
@@ -103,8 +103,8 @@ def unmask(tokens: torch.Tensor, confidence: torch.Tensor, ids: torch.Tensor, ro
     s = _stream(dev, stream)
     indptr = _ints(row_indptr, "row_indptr", dev)
     blocks = row_indptr.shape[0] - 1
-    if blocks < 0:
-        raise ValueError("row_indptr must hold an entry more than blocks")
+    if not 0 <= blocks <= MOST:
+        raise ValueError(f"row_indptr must hold an entry more than blocks, which are at most {MOST}")
     n, n_all, _ = _each(count, "count", torch.int32, dev, blocks, 0, 2 ** 31 - 1)
     c, c_all, _ = _each(threshold, "threshold", torch.float32, dev, blocks, -math.inf, math.inf)
     out, to = _result(out, "out", rows, torch.int32, dev, stream)

@@ -14,6 +14,9 @@ from ._lib import BlockTable, TablesBatch, lib
 from .kvq import _launch, _new, _stream
 
 
+MOST = 2 ** 31 - 1  # sizes are 32 bits to the C calls
+
+
 @dataclass(eq=False)
 class Tables:
     """What the calls of a batch read: page_indptr int32 [items + 1]; page_ids
@@ -42,6 +45,8 @@ def _table(table) -> BlockTable:
     if not isinstance(table, torch.Tensor) or table.dtype is not torch.int32 or table.dim() != 2:
         raise TypeError("table must be a torch.Tensor [requests, max_pages] of int32")
     requests, pages = table.shape
+    if requests > MOST or pages > MOST:
+        raise ValueError(f"table must have at most {MOST} requests and pages of a request, got {list(table.shape)}")
     if table.numel() and ((table.stride(1) != 1 and pages > 1) or (table.stride(0) < pages and requests > 1)):
         raise ValueError("the pages of a request must be consecutive, and requests apart")
     return BlockTable(table.data_ptr(), max(table.stride(0), pages) if requests > 1 else pages, requests, pages)
@@ -60,6 +65,8 @@ def resize(table: torch.Tensor, held: torch.Tensor, lengths: torch.Tensor, free:
     h = _ints(held, "held", dev, c_table.requests)
     n = _ints(lengths, "lengths", dev, c_table.requests)
     f = _ints(free, "free", dev)
+    if free.numel() > MOST:
+        raise ValueError(f"free must have at most {MOST} entries, got {free.numel()}")
     m = _ints(num_free, "num_free", dev, 1)
     if short is None:
         short = _new((1,), torch.int32, dev, stream)
@@ -87,6 +94,8 @@ def build(table: torch.Tensor, request: Optional[torch.Tensor], kv_len: torch.Te
         raise ValueError("rows and pages must not be negative")
     k = _ints(kv_len, "kv_len", dev)
     items = kv_len.numel()
+    if items > MOST:
+        raise ValueError(f"kv_len must have at most {MOST} entries, got {items}")
     batch = TablesBatch(items, 0, None if request is None else _ints(request, "request", dev, items), k,
                         _ints(q_indptr, "q_indptr", dev, items + 1), _ints(q_offset, "q_offset", dev, items),
                         None if q_pos is None else _ints(q_pos, "q_pos", dev, rows))

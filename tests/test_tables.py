@@ -293,3 +293,19 @@ def test_python_refusals(dev):
             tables.build(**{**good, **kw})
     with pytest.raises(ValueError, match="GPU"):
         tables.resize(**{k: v.cpu() for k, v in dict(table=ints(4, 6), held=ints(4), lengths=ints(4), free=ints(30), num_free=ints(1)).items()})
+
+
+@pytest.mark.gpu
+def test_sizes_past_32_bits_are_refused(dev):
+    """Sizes that the C call takes in 32 bits are not cut down to them."""
+    ints = lambda *n: torch.zeros(n, dtype=torch.int32, device=dev)  # noqa: E731
+    many = torch.empty(2 ** 32 + 3, dtype=torch.int32, device=dev)  # 2 + 1 entries, modulo 2^32
+    with pytest.raises(ValueError, match="free"):
+        tables.resize(ints(2, 3), ints(2), ints(2), many, ints(1))
+    for table in (many.view(1, -1), many.view(-1, 1)):
+        with pytest.raises(ValueError, match="table"):
+            tables.resize(table, ints(table.shape[0] % 2 ** 32), ints(table.shape[0] % 2 ** 32), ints(9), ints(1))
+        with pytest.raises(ValueError, match="table"):
+            tables.build(table, None, ints(1), ints(2), ints(1), rows=1, pages=1)
+    with pytest.raises(ValueError, match="kv_len"):
+        tables.build(ints(2, 3), None, many[:-1], many, many[:-1], rows=1, pages=1, out=tables.Tables(many, ints(1), ints(1), ints(1).long(), ints(1)))

@@ -176,3 +176,11 @@ def test_python_refusals(dev):
                       (ValueError, dict(left=t["ids"])), (ValueError, dict(ids=t["ids"].cpu()))]:
         with pytest.raises(error):
             sample.unmask(**{**t, **kw})
+
+
+@pytest.mark.gpu
+def test_blocks_past_32_bits_are_refused(dev):
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=dev)  # noqa: E731
+    with pytest.raises(ValueError, match="row_indptr"):
+        sample.unmask(ints(1, 2), torch.ones(2, device=dev), ints(7, 7), torch.empty(2 ** 32 + 2, dtype=torch.int32, device=dev), mask_id=7,
+                      left=ints(0))
