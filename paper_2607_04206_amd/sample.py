@@ -105,6 +105,8 @@ def unmask(tokens: torch.Tensor, confidence: torch.Tensor, ids: torch.Tensor, ro
     blocks = row_indptr.shape[0] - 1
     if not 0 <= blocks <= MOST:
         raise ValueError(f"row_indptr must hold an entry more than blocks, which are at most {MOST}")
+    if not -MOST - 1 <= mask_id <= MOST:
+        raise ValueError(f"mask_id must fit 32 bits, got {mask_id}")
     n, n_all, _ = _each(count, "count", torch.int32, dev, blocks, 0, 2 ** 31 - 1)
     c, c_all, _ = _each(threshold, "threshold", torch.float32, dev, blocks, -math.inf, math.inf)
     out, to = _result(out, "out", rows, torch.int32, dev, stream)

@@ -179,6 +179,18 @@ def test_python_refusals(dev):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("mask_id", [2 ** 31, 2 ** 32 + 7, -2 ** 31 - 1, -2 ** 40])
+def test_mask_past_32_bits_is_refused(dev, mask_id):
+    """A mask that no id can be is not taken for the one that its last 32 bits are."""
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=dev)  # noqa: E731
+    with pytest.raises(ValueError, match="mask_id"):
+        sample.unmask(ints(1, 2), torch.ones(2, device=dev), ints(7, 7), ints(0, 2), mask_id=mask_id)
+    for edge in (2 ** 31 - 1, -2 ** 31):
+        out, left = sample.unmask(ints(1, 2), torch.ones(2, device=dev), ints(edge, 7), ints(0, 2), mask_id=edge, count=0)
+        assert out.tolist() == [edge, 7] and left.tolist() == [1]
+
+
+@pytest.mark.gpu
 def test_blocks_past_32_bits_are_refused(dev):
     ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=dev)  # noqa: E731
     with pytest.raises(ValueError, match="row_indptr"):
