@@ -5,12 +5,13 @@ refreshes the cache at the block boundary; Sec. 2.2, Sec. 4.3), each
 iteration's microbatch is composed by the deficit token-budget rule
 (Sec. 4.1, Alg. 1) and served by one sangam_attn_forward call over a paged KV
 pool (Sec. 5), or by one sangam_kvq_forward call over a quantised pool. With
-rotary positions, q and k are rotated at their rows' positions before it. The
-block table lies on the device and follows the requests' lengths (tables.resize),
-and each batch's page list, positions and slots are built there (tables.build).
-With sampling, each decode row takes a token from logits (sample.tokens), and the
-most confident rows of each block keep theirs (sample.unmask), which decides how
-many steps a block takes.
+rotary positions, q and k are rotated at their rows' positions before it. With
+sampling, each decode row takes a token from logits (sample.tokens), and the most
+confident rows of each block keep theirs (sample.unmask), which decides how many
+steps a block takes; the block table then lies on the device and follows the
+requests' lengths (tables.resize), and each batch's page list, positions and slots
+are built there (tables.build). Without it the slots are not read, and the host
+sends the page list and positions that it has.
 
 Only one attention layer is run per iteration (the model around it is out of
 scope), with synthetic Q / K / V values and logits: the loop exercises batch
@@ -129,7 +130,7 @@ class ServingLoop:
             self.free_pages = torch.tensor(self.pool._free, dtype=torch.int32, device=device)
             self.num_free = torch.tensor([self.pool.free], dtype=torch.int32, device=device)
             self._lengths = np.zeros(len(self.reqs), np.int32)
-            self._resized = True
+            self._changes = [[]]  # of the lengths, (request, length) by iteration, that the table does not follow yet
         self.sampling = None
         if sampling is not None:
             self._set_sampling(device, seed, **sampling)
@@ -244,19 +245,26 @@ class ServingLoop:
     def _resize(self, s: _State, length: int) -> None:
         """A request's length in the block table, from the next batch on."""
         if self.dev is not None:
-            self._lengths[self._rows[id(s)]] = length
-            self._resized = True
+            self._changes[-1].append((self._rows[id(s)], length))
 
     def _batch_tables(self, items, rows: int, pages: int) -> tables.Tables:
         """The block table after this iteration's requests, and what the batch's
         calls read of it: the host sends lengths and offsets."""
-        if self._resized:
-            tables.resize(self.table, self.held, torch.from_numpy(self._lengths.copy()).to(self.dev, non_blocking=True), self.free_pages, self.num_free)
-            self._resized = False
+        for change in self._changes:  # (pages go back and are taken in the host's order)
+            if change:
+                at, length = zip(*change)
+                self._lengths[list(at)] = length
+                tables.resize(self.table, self.held, torch.from_numpy(self._lengths.copy()).to(self.dev, non_blocking=True), self.free_pages, self.num_free)
+        self._changes = [[]]
         q_indptr, q_offset, kv_len, _ = self._desc
         n = len(items)
         sent = torch.from_numpy(np.concatenate([np.asarray([self._rows[id(s)] for s in items], np.int32), kv_len, q_offset, q_indptr])).to(self.dev, non_blocking=True)
         return tables.build(self.table, sent[:n], sent[n:2 * n], sent[3 * n:], sent[2 * n:3 * n], rows=rows, pages=pages)
+
+    def _positions(self) -> np.ndarray:
+        """Position of every row of the batch."""
+        q_indptr, q_offset, _, _ = self._desc
+        return np.arange(q_indptr[-1], dtype=np.int32) + np.repeat(q_offset - q_indptr[:-1], q_indptr[1:] - q_indptr[:-1])
 
     def _sample(self, b: tables.Tables, items) -> None:
         """A token for every row of the decodes' blocks, and the rows that keep
@@ -284,14 +292,21 @@ class ServingLoop:
         return torch.arange(0, BLOCK * blocks + 1, BLOCK, dtype=torch.int32, device=self.dev)
 
     def _run(self, p, page_ids, rows, timed, capture, items):
-        b = self._batch_tables(items, rows, len(page_ids))
-        pid = b.page_ids
+        b = None
+        if self.sampling is not None or capture:
+            b = self._batch_tables(items, rows, len(page_ids))
+            pid = b.page_ids
+        else:
+            pid = torch.from_numpy(page_ids).to(self.dev, non_blocking=True)
+            if self._changes[-1]:
+                self._changes.append([])
         stream = torch.cuda.current_stream(self.dev)
         snap = None
         nd = self._nd
         q, k_new, v_new = self.q[:rows], self.k_new[:rows], self.v_new[:rows]
         if self.rope is not None:
-            q, k_new = rope.rotate(self.rope, q, k_new, b.positions, q_out=self.q_rot[:rows], k_out=self.k_rot[:rows])
+            positions = b.positions if b is not None else torch.from_numpy(self._positions()).to(self.dev, non_blocking=True)
+            q, k_new = rope.rotate(self.rope, q, k_new, positions, q_out=self.q_rot[:rows], k_out=self.k_rot[:rows])
         if capture:
             q_indptr, q_offset, kv_len, page_indptr = self._desc
             snap = dict(q_indptr=q_indptr, q_offset=q_offset, kv_len=kv_len,

@@ -10,6 +10,7 @@ import pytest
 import torch
 
 import workloads
+from paper_2607_04206_amd import tables
 from paper_2607_04206_amd.serve import PAGE, ServingLoop
 from tests.test_sample import check
 from tests.test_unmask import definition
@@ -96,3 +97,39 @@ def test_sampling(how, threshold, loop_kw):
             steps += 1
         assert np.array_equal(after, expect), f"iteration {t}"
     assert steps > 5 and all(s.phase == "done" for s in loop.reqs) and loop.pool.free == loop.pool.num_pages
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rotary", [None, {}])
+def test_a_loop_that_reads_no_slots_makes_none(monkeypatch, rotary):
+    """Without sampling the host's page list and positions are sent, and no table kernel runs, until a step is captured: then the
+    block table has followed every request that came or went before."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    reqs = workloads.serving_trace(9, 40, 0.8, median=120)
+    loop = ServingLoop(reqs, hq=8, hkv=2, d=64, tau=2048, device=torch.device("cuda:0"), rotary=rotary)
+
+    def unread(*args, **kw):
+        raise AssertionError("a table that nothing reads")
+
+    checked = gone = 0
+    for t in range(600):
+        if not loop.busy():
+            break
+        capture = t % 7 == 6
+        with monkeypatch.context() as m:
+            if not capture:
+                m.setattr(tables, "resize", unread)
+                m.setattr(tables, "build", unread)
+            rec = loop.step(t, timed=False, capture=capture)
+        if rec is None or not capture:
+            continue
+        c = rec.captured
+        n = np.diff(c["q_indptr"])
+        positions = np.concatenate([o + np.arange(k) for o, k in zip(c["q_offset"], n)])
+        b = c["tables"]
+        assert np.array_equal(b.page_ids.cpu().numpy(), c["page_ids"]) and np.array_equal(b.positions.cpu().numpy(), positions)
+        assert np.array_equal(loop._positions(), positions)
+        checked += 1
+        gone = sum(s.phase == "done" for s in loop.reqs)
+    assert checked > 10 and gone > 5 and all(s.phase == "done" for s in loop.reqs)
