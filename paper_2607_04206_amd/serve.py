@@ -131,6 +131,7 @@ class ServingLoop:
             self.num_free = torch.tensor([self.pool.free], dtype=torch.int32, device=device)
             self._lengths = np.zeros(len(self.reqs), np.int32)
             self._changes = [[]]  # of the lengths, (request, length) by iteration, that the table does not follow yet
+            self._short = []  # requests that the table had no pages for, of each change: not looked at yet
         self.sampling = None
         if sampling is not None:
             self._set_sampling(device, seed, **sampling)
@@ -254,7 +255,8 @@ class ServingLoop:
             if change:
                 at, length = zip(*change)
                 self._lengths[list(at)] = length
-                tables.resize(self.table, self.held, torch.from_numpy(self._lengths.copy()).to(self.dev, non_blocking=True), self.free_pages, self.num_free)
+                self._short.append(tables.resize(self.table, self.held, torch.from_numpy(self._lengths.copy()).to(self.dev, non_blocking=True),
+                                                 self.free_pages, self.num_free))
         self._changes = [[]]
         q_indptr, q_offset, kv_len, _ = self._desc
         n = len(items)
@@ -286,7 +288,16 @@ class ServingLoop:
         out, left = sample.unmask(tokens, confidence, self.ids, self._indptr(self._nd), mask_id=self.mask_id, count=self.count, threshold=self.threshold,
                                   slots=b.slots[:rows])
         self.sampled = (tokens, confidence, out)
-        self._left = left.tolist()  # (the host waits here: the blocks that are done leave the next batch)
+        self._left = self._told(left)  # (the host waits here: the blocks that are done leave the next batch)
+
+    def _told(self, left: torch.Tensor) -> List[int]:
+        """A tensor's values on the host, and with them whether the device's free pages were as many as the host's."""
+        told = torch.cat([left, *self._short]).tolist() if self._short else left.tolist()
+        n = left.numel()
+        self._short = []
+        if any(told[n:]):
+            raise RuntimeError("the block table found too few free pages: it does not follow the host's pool any more")
+        return told[:n]
 
     def _indptr(self, blocks: int) -> torch.Tensor:
         return torch.arange(0, BLOCK * blocks + 1, BLOCK, dtype=torch.int32, device=self.dev)
@@ -370,4 +381,6 @@ class ServingLoop:
             rec = self.step(t, timed)
             if rec is not None:
                 log.append(rec)
+        if self.dev is not None and self._short:
+            self._told(self.num_free)
         return log

@@ -133,3 +133,28 @@ def test_a_loop_that_reads_no_slots_makes_none(monkeypatch, rotary):
         checked += 1
         gone = sum(s.phase == "done" for s in loop.reqs)
     assert checked > 10 and gone > 5 and all(s.phase == "done" for s in loop.reqs)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sampling", [None, dict(vocab=999)])
+def test_a_table_without_pages_is_noticed(monkeypatch, sampling):
+    """A block table that no longer follows the host's pool ends the run, at the next look at the device's numbers."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    resize, calls = tables.resize, []
+
+    def short(*args, **kw):  # the fourth call says that a request found none (all do: the pages are right)
+        calls.append(resize(*args, **kw))
+        if len(calls) == 4:
+            calls[-1].fill_(1)
+        return calls[-1]
+
+    monkeypatch.setattr(tables, "resize", short)
+    reqs = workloads.serving_trace(7, 12, 0.5, median=100, resp=64)
+    loop = ServingLoop(reqs, hq=8, hkv=2, d=64, tau=1024, device=torch.device("cuda:0"), sampling=sampling)
+    if sampling is None:  # (captured steps alone read the table then)
+        for t in range(30):
+            loop.step(t, timed=False, capture=True)
+    with pytest.raises(RuntimeError, match="free pages"):
+        loop.run(2000, timed=False)
+    assert len(calls) >= 4
