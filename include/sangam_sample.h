@@ -122,7 +122,7 @@ typedef struct sangam_unmask_desc {
     const float *thresholds;   /* [num_blocks], or NULL: threshold */
     int64_t rows;              /* 0 to 2^31 - 1 */
     int64_t num_ids;
-    int32_t num_blocks;        /* >= 0 */
+    int32_t num_blocks;        /* 0 to 4 (2^24 - 1) */
     int32_t mask_id;
     int32_t count;             /* >= 0 (in counts: below 0 counts as 0) */
     float threshold;           /* a number or infinity (in thresholds: no number is never reached) */

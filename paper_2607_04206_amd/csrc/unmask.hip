@@ -32,6 +32,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kKeys = 4;     // of a lane: blocks of up to 256 rows are a wave's (1024 take 15.1 us by a wave, 7.5 by a work-group)
+// A grid's threads are counted in 32 bits. (Blocks that have a work-group to themselves hold over 128 rows each on average: under 2^24 of them.)
+constexpr int kMostBlocks = kWaves * ((1 << 24) - 1);
 constexpr int kHeld = 4096;  // keys of a work-group: blocks of up to so many rows are looked at once
 
 struct UnmaskArgs {
@@ -344,8 +346,8 @@ sangam_status fail(sangam_status code, const std::string& msg) {
 
 sangam_status unmask(const sangam_unmask_desc* d, int32_t* out, int32_t* left, void* stream) {
     clear_error();
-    if (!d || d->rows < 0 || d->rows > INT32_MAX || d->num_blocks < 0 || d->num_ids < 0)
-        return fail(SANGAM_ERR_INVALID_ARG, "desc must not be NULL, rows 0 to 2^31 - 1, num_blocks and num_ids not negative");
+    if (!d || d->rows < 0 || d->rows > INT32_MAX || d->num_blocks < 0 || d->num_blocks > kMostBlocks || d->num_ids < 0)
+        return fail(SANGAM_ERR_INVALID_ARG, "desc must not be NULL, rows 0 to 2^31 - 1, num_blocks 0 to 4 (2^24 - 1), num_ids not negative");
     if (d->count < 0) return fail(SANGAM_ERR_INVALID_ARG, "count must not be negative");
     if (!d->thresholds && std::isnan(d->threshold)) return fail(SANGAM_ERR_INVALID_ARG, "threshold must be a number");
     if (!d->row_indptr) return fail(SANGAM_ERR_INVALID_ARG, "row_indptr must not be NULL");
@@ -364,7 +366,6 @@ sangam_status unmask(const sangam_unmask_desc* d, int32_t* out, int32_t* left, v
                     d->num_blocks, d->mask_id, d->count, d->threshold, out, left, each};
     void* kargs[] = {&args};
     const int64_t groups = std::max<int64_t>((int64_t(d->num_blocks) + args.each - 1) / args.each, std::min<int64_t>((d->rows + kThreads - 1) / kThreads, 64));
-    if (groups > (int64_t(1) << 24) - 1) return fail(SANGAM_ERR_INVALID_ARG, "too many blocks");
     const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&unmask_kernel), dim3(unsigned(std::max<int64_t>(groups, 1))), dim3(kThreads), kargs, 0,
                                          static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SANGAM_OK : fail(SANGAM_ERR_HIP, std::string("unmask launch: ") + hipGetErrorString(e));

@@ -196,3 +196,25 @@ def test_blocks_past_32_bits_are_refused(dev):
     with pytest.raises(ValueError, match="row_indptr"):
         sample.unmask(ints(1, 2), torch.ones(2, device=dev), ints(7, 7), torch.empty(2 ** 32 + 2, dtype=torch.int32, device=dev), mask_id=7,
                       left=ints(0))
+
+
+@pytest.mark.parametrize("rows", [0, 8, 2 ** 31 - 1])
+def test_more_blocks_than_a_launch_takes(rows):
+    """The header's limit, whatever the rows (a call without rows has a launch as well, for left)."""
+    assert _lib.lib.sangam_sample_unmask(ctypes.byref(c_desc(rows=rows, num_ids=rows, num_blocks=4 * (2 ** 24 - 1) + 1)), 4096, 4096, None) == -1
+    assert b"num_blocks" in _lib.lib.sangam_last_error()
+    assert _lib.lib.sangam_sample_unmask(ctypes.byref(c_desc(rows=0, num_ids=0, num_blocks=4 * (2 ** 24 - 1) + 1)), None, None, None) == -1
+
+
+@pytest.mark.gpu
+def test_as_many_blocks_as_a_launch_takes(dev):
+    blocks, n = 4 * (2 ** 24 - 1), 8
+    indptr = torch.zeros(blocks + 1, dtype=torch.int32, device=dev)
+    indptr[blocks // 2:] = 3
+    indptr[-1] = n
+    ids = torch.full((n,), MASK, dtype=torch.int32, device=dev)
+    conf = torch.tensor([0.1, 0.3, 0.2, 0.5, 0.4, 0.7, 0.6, 0.0], device=dev)
+    out, left = sample.unmask(torch.arange(n, dtype=torch.int32, device=dev), conf, ids, indptr, mask_id=MASK, count=1)
+    assert out.tolist() == [MASK, 1, MASK, MASK, MASK, 5, MASK, MASK]
+    at = left.nonzero()[:, 0]
+    assert at.tolist() == [blocks // 2 - 1, blocks - 1] and left[at].tolist() == [2, 4]
