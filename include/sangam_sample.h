@@ -53,6 +53,9 @@ extern "C" {
  * alike. Confidences come from the same sums, but for the first token of
  * everything of fp16 and fp32 rows (T = 0, nothing filtered): its weights are
  * computed in 32 bits and summed in 32 over a few, then in 64, to 2^-19 of the sum.
+ * Within that error these hang on the number of rows as well (rows are summed in
+ * parts where there are few), and with them which rows are at a threshold; all
+ * other confidences are a row's own, to the last bit.
  *
  * Parameters: an array has num_params entries, of which row r takes entry
  * params_of[r] (NULL: r); a NULL array stands for the value beside it. A row

@@ -556,6 +556,26 @@ def test_entropies_in_any_order(dev, dtype):
             assert torch.equal(one(x, 30).view(30, 9), want.expand(30, 9))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", list(sample.CONFIDENCES))
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_confidences_in_few_and_many_rows(dev, dtype, kind):
+    """A row's confidence is its own, to the last bit. That of the first token of everything in fp16 and fp32 rows is off by 2^-19
+    of the sum at most (entropy: times 2 + log(vocab)), in few rows and in many."""
+    gen = torch.Generator().manual_seed(28)
+    for how in ("normal", "peaked", "wide", "holes", "zeros"):
+        x = make((6, LONG), how, DTYPES[dtype], gen).to(dev)
+        u = torch.rand(6, generator=gen).to(dev)
+        for params in (dict(temperature=0.8), dict(temperature=1.0, top_k=40), dict(temperature=1.3, top_p=0.9), dict(temperature=0.0, min_p=0.01), dict(temperature=0.0)):
+            few, many = (sample.tokens(x.repeat(n, 1), u.repeat(n), confidence=kind, **params) for n in (1, 50))
+            assert torch.equal(many[0].view(50, 6), few[0].expand(50, 6))
+            if len(params) > 1 or params["temperature"] > 0 or dtype == "bf16":
+                assert torch.equal(many[1].view(50, 6), few[1].expand(50, 6))
+            else:
+                bar = 2 * 2.0 ** -19 * (2 + math.log(LONG) if kind == "entropy" else few[1].abs().double() + (1.0 if kind == "margin" else 0.0))
+                assert ((many[1].view(50, 6).double() - few[1].double()).abs() <= bar).all()
+
+
 def test_exact_sums(tmp_path):
     """The sum that these entropies take, on the host: the same bits in every order, of up to 2^18 numbers, each added to 2^-84."""
     if not shutil.which("g++"):
