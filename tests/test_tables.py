@@ -227,6 +227,45 @@ def test_streams_and_graphs(dev):
         assert [x.tolist() for x in (out.page_indptr, out.page_ids, out.positions, out.slots, out.items)] == [list(x) for x in want]
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("items,rows,pages", [(1, 7, 5), (6, 50, 40), (300, 5000, 3000), (1025, 4000, 999), (3000, 17, 0)])
+def test_build_of_wrong_contents(dev, items, rows, pages):
+    """Whatever the arrays hold: nothing around the outputs is written, no input changes, and what comes out is of the table."""
+    rng = np.random.default_rng(items)
+    requests, longest, kept = 9, 12, -987654
+    for trial in range(6):
+        held = rng.integers(0, 1 << 28, (requests, longest))
+        held[rng.random(held.shape) < 0.1] = -1
+        buffer = torch.full((requests + 2, longest + 5), 77777777, dtype=torch.int32, device=dev)
+        table = buffer[1:-1, 2:longest + 2]
+        table.copy_(put(dev, held))
+        before = buffer.clone()
+        wild = lambda n, lo, hi: put(dev, np.where(rng.random(n) < 0.5, rng.integers(lo, hi, n), rng.choice([-2 ** 31, 2 ** 31 - 1, -1, 0, 2 ** 30], n)))  # noqa: E731
+        inputs = dict(request=wild(items, -3, requests + 3), kv_len=wild(items, -50, 16 * longest + 90), q_indptr=wild(items + 1, -20, rows + 20),
+                      q_offset=wild(items, -100, 300), q_pos=wild(rows, -20, 16 * longest + 20) if trial % 2 else None)
+        if trial >= 3:  # in order
+            inputs["q_indptr"] = put(dev, np.sort(inputs["q_indptr"].cpu().numpy()))
+        copies = {k: None if v is None else v.clone() for k, v in inputs.items()}
+        sizes = dict(page_indptr=items + 1, page_ids=pages, positions=rows, slots=rows, items=rows)
+        around = {k: torch.full((n + 32,), kept, dtype=torch.int64 if k == "slots" else torch.int32, device=dev) for k, n in sizes.items()}
+        out = tables.Tables(**{k: around[k][16:16 + n] for k, n in sizes.items()})
+        tables.build(table, inputs["request"], inputs["kv_len"], inputs["q_indptr"], inputs["q_offset"], rows=rows, pages=pages, q_pos=inputs["q_pos"], out=out)
+        torch.cuda.synchronize()
+        for k, n in sizes.items():
+            assert (around[k][:16] == kept).all() and (around[k][16 + n:] == kept).all(), k
+            assert (out.__dict__[k] != kept).all(), k
+        assert torch.equal(buffer, before) and all(v is None or torch.equal(v, copies[k]) for k, v in inputs.items())
+        entries = set(held.ravel().tolist()) | {-1}
+        assert set(out.page_ids.tolist()) <= entries
+        slots, positions = out.slots.cpu().numpy(), out.positions.cpu().numpy()
+        there = slots >= 0
+        assert (slots[~there] == -1).all() and set((slots[there] // PAGE).tolist()) <= entries and (slots[there] % PAGE == positions[there] % PAGE).all()
+        assert ((out.items >= -1) & (out.items < items)).all()
+        n = inputs["kv_len"].cpu().numpy()
+        pages_of = np.minimum(np.where(n > 0, (n.astype(np.int64) + PAGE - 1) // PAGE, 0), longest)
+        assert out.page_indptr.tolist() == [0] + np.cumsum(pages_of).tolist()
+
+
 def test_places_among_many_offsets(tmp_path):
     """The search among the offsets of as many items as a batch may have, and of a few, on the host and without overflow."""
     if not shutil.which("g++"):

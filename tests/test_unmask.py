@@ -218,3 +218,50 @@ def test_as_many_blocks_as_a_launch_takes(dev):
     assert out.tolist() == [MASK, 1, MASK, MASK, MASK, 5, MASK, MASK]
     at = left.nonzero()[:, 0]
     assert at.tolist() == [blocks // 2 - 1, blocks - 1] and left[at].tolist() == [2, 4]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("slotted", [False, True])
+@pytest.mark.parametrize("blocks,rows", [(3, 24), (1, 700), (40, 9000), (500, 6000)])
+def test_wrong_contents(dev, blocks, rows, slotted):
+    """Whatever offsets, slots, counts and thresholds hold: nothing around the outputs is written, and a row's id afterwards is its
+    own, its token or, without a slot, -1."""
+    rng = np.random.default_rng(blocks)
+    kept, pool = -987654, 2 * rows
+    for trial in range(6):
+        indptr = np.where(rng.random(blocks + 1) < 0.6, rng.integers(-20, rows + 20, blocks + 1), rng.choice([-2 ** 31, 2 ** 31 - 1, -1, 0, 2 ** 30], blocks + 1))
+        if trial >= 3:
+            indptr = np.sort(indptr)
+        _, tokens, conf, ids = case([rows], trial, "odd")
+        counts, thresholds = rng.choice(np.array([-2 ** 31, -1, 0, 3, 2 ** 31 - 1]), blocks), rng.choice(np.array([math.nan, math.inf, -math.inf, 0.5]), blocks)
+        if slotted:
+            slots = rng.permutation(pool)[:rows]
+            wild = rng.random(rows) < 0.2
+            slots[wild] = rng.choice(np.array([-1, pool, 2 ** 62, -2 ** 63, 2 ** 40]), int(wild.sum()))
+            there = (slots >= 0) & (slots < pool)
+            held = rng.integers(5000, 6000, pool)
+            held[slots[there]] = ids[there]
+        else:
+            there, held = np.ones(rows, bool), ids
+        def guarded(n, x=None):  # noqa: E306
+            t = torch.full((n + 64,), kept, dtype=torch.int32, device=dev)
+            if x is not None:
+                t[32:32 + n] = torch.from_numpy(x.astype(np.int32)).to(dev)
+            return t
+        around = [guarded(len(held), held), guarded(rows), guarded(blocks)]
+        pool_ids, out, left = (t[32:-32] for t in around)
+        sample.unmask(*put(dev, tokens, conf), pool_ids, *put(dev, indptr.astype(np.int32)), mask_id=MASK, count=put(dev, counts.astype(np.int32))[0],
+                      threshold=put(dev, thresholds.astype(np.float32))[0], slots=put(dev, slots)[0] if slotted else None, out=out, left=left)
+        torch.cuda.synchronize()
+        assert all((t[:32] == kept).all() and (t[-32:] == kept).all() for t in around)
+        got = out.cpu().numpy()
+        assert ((got == ids) | ((ids == MASK) & (tokens >= 0) & (got == tokens)))[there].all() and (got[~there] == -1).all()
+        after = pool_ids.cpu().numpy()
+        if slotted:
+            assert ((after[slots[there]] == ids[there]) | ((ids == MASK) & (after[np.where(there, slots, 0)] == tokens))[there]).all()
+            rest = np.ones(pool, bool)
+            rest[slots[there]] = False
+            assert np.array_equal(after[rest], held[rest])
+        else:
+            assert np.array_equal(after, ids)
+        assert (left != kept).all()
