@@ -10,9 +10,9 @@ import pytest
 import torch
 
 import workloads
-from paper_2607_04206_amd import tables
+from paper_2607_04206_amd import sample, tables
 from paper_2607_04206_amd.serve import PAGE, ServingLoop
-from tests.test_sample import check
+from tests.test_sample import check, ranked
 from tests.test_unmask import definition
 
 
@@ -158,3 +158,34 @@ def test_a_table_without_pages_is_noticed(monkeypatch, sampling):
     with pytest.raises(RuntimeError, match="free pages"):
         loop.run(2000, timed=False)
     assert len(calls) >= 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("how", [dict(temperature=0.8, top_p=0.6), dict(temperature=1.5, top_k=3, confidence="margin"), dict(temperature=2.0, min_p=0.02, confidence="entropy"),
+                                 dict(temperature=3.0)])
+def test_drawn_tokens(monkeypatch, how):
+    """Tokens and confidences of drawn rows against their definition, from the uniform numbers that the loop gave. The parameters
+    of the hotter ones matter: of some rows the definition without them takes another token."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    calls, tokens_of = [], sample.tokens
+
+    def kept(logits, u, **kw):
+        got = tokens_of(logits, u, **kw)
+        calls.append((logits.double().cpu().numpy(), u.tolist(), got[0].tolist(), got[1].tolist()))
+        return got
+
+    monkeypatch.setattr(sample, "tokens", kept)
+    reqs = workloads.serving_trace(7, 6, 0.5, median=100, resp=64)
+    vocab = 1999
+    loop = ServingLoop(reqs, hq=8, hkv=2, d=64, tau=1024, device=torch.device("cuda:0"), sampling=dict(vocab=vocab, count=4, **how))
+    loop.run(2000, timed=False)
+    kind = how.get("confidence", "probability")
+    params = {k: v if k == "top_k" else float(np.float32(v)) for k, v in how.items() if k != "confidence"}
+    others = 0
+    for logits, u, tokens, confidence in calls[::max(1, len(calls) // 6)]:
+        for r in range(0, len(u), 5):
+            check(logits[r], tokens[r], confidence[r], u[r], kind=kind, forbid=vocab, **params)
+            order, w, _ = ranked(np.where(np.arange(vocab + 1) == vocab, -math.inf, logits[r]), 1.0)
+            others += int(tokens[r]) != int(order[min(int(np.searchsorted(np.cumsum(w), u[r] * w.sum(), side="right")), vocab - 1)])
+    assert len(calls) > 1 and (others > 0 or how["temperature"] < 1) and all(s.phase == "done" for s in loop.reqs)
