@@ -475,7 +475,9 @@ struct Bin {
         return scalar(lo);
     }
 
-    // The bin's first tokens up to a place, by digits of the keys; p.ties - 1 tokens with the last one's key are before it.
+    // The bin's first tokens up to a place, by digits of the keys; p.ties - 1 tokens with the last one's key are before it. (Few
+    // rows of a language model have so many in a bin. 126,464 equal logits, each look an atomic of one digit and then one
+    // after the other for the index, in fp32: a row 520 us, 300 rows 1,160, where normal ones take 48 and 97.)
     __device__ __forceinline__ void descend(Prefix& p, By by, int count, double weight, uint32_t cut, int most) {
         listed = -1;
         const int d = threadIdx.x, b = p.bin;
@@ -862,7 +864,9 @@ __device__ __forceinline__ void choose(Shared<E>& sh, const Row<T, E>& row, cons
     if (a.confidence == SANGAM_CONFIDENCE_MARGIN) {
         c = (double(top_weight) * 0x1p-33 - second) * unit;
     } else if (a.confidence == SANGAM_CONFIDENCE_ENTROPY) {
-        ExactSum sum{};  // (which thread gets which logits hangs on the order of LDS atomics)
+        // (which thread gets which logits hangs on the order of LDS atomics. Sums in doubles would do so, too, and take 600 rows
+        // of 50,257 in fp32 under a nucleus in 119 us instead of 123, 300 unfiltered ones of 126,464 in fp16 in 146 instead of 159)
+        ExactSum sum{};
         auto part = [&](double t) { return sh.bin_weight(int(t)) * double(kOne - miss_at(t - int(t))) * 0x1p-33 * t; };
         row.each_within(sh, row.lowest(min(kept.bin + 1, kBins)), INFINITY, [&](int, float x) {
             const double t = bin.place(x, 0);
@@ -1627,10 +1631,17 @@ __global__ __launch_bounds__(kThreads) void sample_join_kernel(SampleArgs a, Spl
     from_logits(sh, row, a, p, r);
 }
 
-// Rows from which a work-group takes a whole one. 256 rows, greedy, whole and in three parts: bf16 of 50,257 tokens 18.3 and
-// 22.9 us, of 126,464 27.2 and 28.7; under a nucleus fp32 of 50,257 33.1 and 39.0, fp16 28.3 and 36.3. (fp16 and fp32, greedy,
-// 320 rows of 126,464: 37.8 and 27.1, 47.2 and 39.2, as two work-groups fit a CU and a second round is short; at 512 rows
-// 39.5 and 40.3, 53.8 and 64.2.)
+// Rows from which a work-group takes a whole one, for all types. Whole / in parts, us, greedy, then under a nucleus:
+//                   256 rows                  384 rows                  640 rows
+//   bf16,  50,257   19.6 / 23.8, 22.3 / 26.8  25.8 / 31.0, 29.9 / 35.7  33.6 / 48.3, 39.0 / 54.8
+//   bf16, 126,464   34.2 / 32.9, 42.7 / 39.9  40.5 / 47.3, 50.9 / 56.1  50.2 / 68.9, 59.9 / 79.2
+//   fp32,  50,257   22.8 / 21.7, 39.3 / 41.5  27.3 / 27.7, 47.0 / 53.2  45.0 / 45.7, 75.7 / 80.7
+//   fp32, 126,464   44.3 / 35.0,  107 / 98    50.6 / 55.0,  113 / 119   90.4 / 79.1,  178 / 188
+//   fp16,  50,257   15.2 / 17.7, 28.2 / 37.3  27.4 / 21.9, 39.2 / 48.1  41.6 / 34.4, 58.9 / 71.5
+//   fp16, 126,464   28.2 / 25.4, 70.1 / 72.5  50.5 / 37.4, 80.7 / 93.1  75.7 / 53.1,  124 / 131
+// Whole rows win, but where few of them make a round more. Greedy fp16 rows would gain by parts up to 767 rows:
+// sample_whole_kernel takes 130 registers and more for them, so one work-group fits a CU and 257 rows are two rounds; of
+// fp32, with 92 to 109, two fit.
 constexpr int64_t kWholeRows = 256;
 // Work-groups that the parts make if they can: three a CU.
 constexpr int64_t kGroups = 3 * 256;

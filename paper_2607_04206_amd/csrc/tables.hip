@@ -6,7 +6,8 @@
 // of KB, 0.01 us of a copy), so what they cost is the launch and a chain of
 // dependent loads: sizes, their prefix sum, the entries. One launch each, the
 // prefix sums in LDS. A batch of 32 decodes or of 48 beside long prefills is
-// built in 4.8 to 5.3 us of the kernel, 13.5 from Python.
+// built in 4.8 to 5.3 us of the kernel, 13.5 from Python; 1024 items of 32 rows in
+// 6.4, 1025 by two launches in 9.4, 4096 (385,000 pages) in 15.4.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
